@@ -16,11 +16,14 @@ SABER_OK, SABER_EINVAL, SABER_ENOMEM, SABER_EDEVICE, SABER_ESTATE, SABER_ERANGE 
 _STATUS = {0: "SABER_OK", -1: "SABER_EINVAL", -2: "SABER_ENOMEM", -3: "SABER_EDEVICE", -4: "SABER_ESTATE",
            -5: "SABER_ERANGE"}
 
-# every symbol include/saber.h declares
+# every symbol the headers under include/ declare: saber.h and saber_measure.h
 EXPORTS = ["saber_set_hooks", "saber_options_default", "saber_init_ex", "saber_init", "saber_iterate", "saber_counts_nnz",
            "saber_counts", "saber_loglik", "saber_loglik_static", "saber_holdout_loglik", "saber_free", "saber_last_error", "saber_get_z", "saber_set_z",
            "saber_get_iteration", "saber_token_probs", "saber_get_phi", "saber_get_stats", "saber_reset_stats",
            "saber_get_stream", "saber_bandwidth_probe", "saber_alias_build_probe", "saber_get_alias"]
+# and include/saber_ops.h (called from ops/)
+EXPORTS += ["saber_ops_last_error", "saber_layer_norm_forward", "saber_layer_norm_backward_workspace", "saber_layer_norm_backward",
+            "saber_checkpoint8_save", "saber_checkpoint8_restore", "saber_linear_xent_forward", "saber_linear_xent_backward"]
 
 
 class SaberError(RuntimeError):
@@ -94,6 +97,16 @@ def load_library():
         "saber_bandwidth_probe": (ctypes.c_int, [i64, i32, vp]),
         "saber_alias_build_probe": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, vp]),
         "saber_get_alias": (ctypes.c_int, [vp, vp, i32, vp, vp]),
+        "saber_ops_last_error": (ctypes.c_char_p, []),
+        "saber_layer_norm_forward": (ctypes.c_int, [vp, i64, vp, vp, i64, i64, ctypes.c_int, ctypes.c_int, f32, vp, vp, vp, vp, vp, vp]),
+        "saber_layer_norm_backward_workspace": (ctypes.c_int, [i64, i64, vp]),
+        "saber_layer_norm_backward": (ctypes.c_int, [vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, i64, ctypes.c_int, ctypes.c_int,
+                                                     vp, vp, vp, vp, i64, vp]),
+        "saber_checkpoint8_save": (ctypes.c_int, [vp, i64, i64, i64, ctypes.c_int, vp, vp, vp]),
+        "saber_checkpoint8_restore": (ctypes.c_int, [vp, vp, i64, i64, ctypes.c_int, vp, vp]),
+        "saber_linear_xent_forward": (ctypes.c_int, [vp, i64, vp, i64, vp, ctypes.c_int, i64, i64, i64, ctypes.c_int, vp, vp, vp, vp, vp]),
+        "saber_linear_xent_backward": (ctypes.c_int, [vp, vp, i64, vp, i64, vp, ctypes.c_int, vp, i64, i64, i64, ctypes.c_int, vp, vp,
+                                                      vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

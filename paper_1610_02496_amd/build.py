@@ -8,9 +8,10 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsaber.so")
-SOURCES = [os.path.join(CSRC, "saber.hip")]
-# every header saber.hip includes: an edit to any of them marks the library stale
-DEPS = SOURCES + sorted(glob.glob(os.path.join(CSRC, "*.hpp"))) + sorted(glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
+OPS_CSRC = os.path.join(HERE, "ops", "csrc")
+SOURCES = [os.path.join(CSRC, "saber.hip"), os.path.join(OPS_CSRC, "saber_ops.hip")]
+# every header the sources include: an edit to any of them marks the library stale
+DEPS = SOURCES + sorted(glob.glob(os.path.join(CSRC, "*.hpp"))) + sorted(glob.glob(os.path.join(OPS_CSRC, "*.hpp"))) + sorted(glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -31,13 +32,26 @@ def build(force: bool = True) -> str:
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", tmp] + SOURCES
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(ln for ln in proc.stdout.splitlines() if "is not a recognized feature" not in ln)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    os.replace(tmp, LIB)
+    objects = ["%s.%d.o" % (tmp, i) for i in range(len(SOURCES))]
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    try:
+        _run([[hipcc] + flags + ["-c", "-o", o, src] for o, src in zip(objects, SOURCES)])
+        _run([[hipcc] + HIPCC_FLAGS + ["-o", tmp] + objects])
+        os.replace(tmp, LIB)
+    finally:
+        for path in objects + [tmp]:
+            if os.path.exists(path):
+                os.remove(path)
     return LIB
+
+
+def _run(commands):
+    """Runs the commands side by side; raises with the output of the first that fails."""
+    running = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in commands]
+    done = [(p.communicate()[0], p.returncode) for p in running]
+    for out, code in done:
+        if code != 0:
+            raise RuntimeError("hipcc failed:\n" + "\n".join(ln for ln in out.splitlines() if "is not a recognized feature" not in ln))
 
 
 if __name__ == "__main__":

@@ -1,0 +1,338 @@
+"""Operators of a head that is trained on a topic model's features, on torch tensors in device memory.
+
+``layer_norm``, ``linear_cross_entropy``   differentiable, for a training loop written with torch
+``layer_norm_forward`` / ``_backward``, ``linear_cross_entropy_forward`` / ``_backward``   the passes themselves
+``checkpoint8``                            an activation held in 8 bits
+
+The work is done by the HIP kernels behind the C ABI of ``include/saber_ops.h``; torch supplies memory, streams and
+the graph of gradients.  Everything is enqueued on torch's current stream of the tensors' device: nothing is waited
+for, and calls may be captured into a graph.  Arguments are checked on the host (ValueError, TypeError, or SaberError
+from the library).  There is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from ..binding import SABER_OK, SaberError, load_library
+
+__all__ = ["Checkpoint8", "NormSaved", "checkpoint8", "layer_norm", "layer_norm_backward", "layer_norm_forward",
+           "linear_cross_entropy", "linear_cross_entropy_backward", "linear_cross_entropy_forward"]
+
+BLOCK = 128   # columns that share a step of a checkpoint
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_int64 = ctypes.c_int64
+
+
+def _check(rc):
+    if rc != SABER_OK:
+        raise SaberError(rc, load_library().saber_ops_last_error().decode("utf-8", "replace"))
+
+
+def _type(name, t):
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError("%s must be float32, float16 or bfloat16, not %s" % (name, t.dtype))
+    return code
+
+
+def _on(name, t, device):
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+
+
+def _device(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be in device memory, not on %s" % (name, t.device))
+    return t.device
+
+
+def _rows(t, name):
+    """(rows, columns, elements between rows) of a tensor seen as a matrix of its last dimension, without a copy where the
+    layout allows it; the tensor itself, or a contiguous copy."""
+    if t.dim() == 2:
+        rows, cols = t.shape
+        if t.stride(1) == 1 or cols == 1:
+            stride = t.stride(0)
+            if stride >= cols:
+                return t, rows, cols, stride
+            if rows <= 1:
+                return t, rows, cols, cols
+        t = t.contiguous()
+        return t, rows, cols, cols
+    if t.dim() == 0:
+        raise ValueError("%s has no columns" % name)
+    cols = t.shape[-1]
+    t = t.contiguous()
+    return t, t.numel() // cols if cols else 0, cols, cols
+
+
+class _Launch:
+    """The stream to launch on, with the tensors' device current."""
+
+    __slots__ = ("device", "guard")
+
+    def __init__(self, device):
+        self.device = device
+        self.guard = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.device.index:
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _vector(t, name, cols, like, of):
+    _device(t, name)
+    _on(name, t, like)
+    if t.shape != (cols,):
+        raise ValueError("%s must hold %d values, one per column of %s" % (name, cols, of))
+    return t if t.is_contiguous() else t.contiguous()
+
+
+# ---- checkpoints in 8 bits -------------------------------------------------------------------------------------------
+
+class Checkpoint8:
+    """An activation in 8 bits: ``q`` (int8, the shape of the activation) times ``scale`` (float32, one step per 128
+    columns of a row).  An element is off by half a step at most, a 254th of its block's largest magnitude."""
+
+    __slots__ = ("q", "scale", "dtype")
+
+    def __init__(self, q, scale, dtype):
+        self.q, self.scale, self.dtype = q, scale, dtype
+
+    def restore(self, dtype=None):
+        """The activation, in its own type or another floating type."""
+        q = self.q
+        x = torch.empty(q.shape, dtype=dtype or self.dtype, device=q.device)
+        cols = q.shape[-1]
+        with _Launch(q.device) as stream:
+            _check(load_library().saber_checkpoint8_restore(q.data_ptr(), self.scale.data_ptr(), q.numel() // cols if cols else 0, cols,
+                                                            _type("dtype", x), x.data_ptr(), stream))
+        return x
+
+
+def _empty_checkpoint(x, rows, cols):
+    return Checkpoint8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                       torch.empty((rows, (cols + BLOCK - 1) // BLOCK), dtype=torch.float32, device=x.device), x.dtype)
+
+
+def checkpoint8(x) -> Checkpoint8:
+    """Holds ``x`` (any shape, blocks run along its last dimension) in 8 bits."""
+    device = _device(x, "x")
+    code = _type("x", x)
+    m, rows, cols, stride = _rows(x, "x")
+    c = _empty_checkpoint(x, rows, cols)
+    with _Launch(device) as stream:
+        _check(load_library().saber_checkpoint8_save(m.data_ptr(), stride, rows, cols, code, c.q.data_ptr(), c.scale.data_ptr(), stream))
+    return c
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+
+class NormSaved:
+    """What the backward pass of a layer norm needs: its input (or an 8-bit checkpoint of it), its weight, and mean and
+    1 / standard deviation of every row."""
+
+    __slots__ = ("x", "checkpoint", "weight", "bias", "mean", "rstd")
+
+    def __init__(self, x, checkpoint, weight, bias, mean, rstd):
+        self.x, self.checkpoint, self.weight, self.bias, self.mean, self.rstd = x, checkpoint, weight, bias, mean, rstd
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
+    """Layer norm over the last dimension: ``(y, saved)``.  ``weight`` and ``bias`` are vectors of one floating type (their
+    own or that of ``x``).  With ``checkpoint`` the input is held in 8 bits for the backward pass, written in the same
+    pass over ``x``; ``x`` itself is not kept."""
+    device = _device(x, "x")
+    code = _type("x", x)
+    m, rows, cols, stride = _rows(x, "x")
+    wcode = code
+    if weight is not None:
+        weight = _vector(weight, "weight", cols, device, "x")
+        wcode = _type("weight", weight)
+    if bias is not None:
+        bias = _vector(bias, "bias", cols, device, "x")
+        bcode = _type("bias", bias)
+        if weight is not None and bcode != wcode:
+            raise TypeError("weight and bias must have one type, not %s and %s" % (weight.dtype, bias.dtype))
+        wcode = bcode
+    y = torch.empty(x.shape, dtype=x.dtype, device=device)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=device)
+    mean, rstd = stats.unbind(0)
+    c = _empty_checkpoint(x, rows, cols) if checkpoint else None
+    with _Launch(device) as stream:
+        _check(load_library().saber_layer_norm_forward(
+            m.data_ptr(), stride, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), rows, cols,
+            code, wcode, eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), None if c is None else c.q.data_ptr(),
+            None if c is None else c.scale.data_ptr(), stream))
+    return y, NormSaved(None if checkpoint else m, c, weight, bias, mean, rstd)
+
+
+def layer_norm_backward(dy, saved, need_x=True, need_weight=True, need_bias=True):
+    """``(dx, dweight, dbias)`` of a layer norm for the gradient ``dy`` of its output; None where not needed or where the
+    norm has no weight or bias."""
+    device = _device(dy, "dy")
+    source = saved.x if saved.checkpoint is None else saved.checkpoint.q
+    dtype = saved.x.dtype if saved.checkpoint is None else saved.checkpoint.dtype
+    if dy.dtype != dtype:
+        raise TypeError("dy must be %s like the norm's input, not %s" % (dtype, dy.dtype))
+    _on("dy", dy, source.device)
+    code = _TYPES[dtype]
+    m, rows, cols, stride = _rows(dy, "dy")
+    if cols != source.shape[-1] or rows != saved.mean.shape[0]:
+        raise ValueError("dy must have the shape of the norm's input")
+    weight, bias = saved.weight, saved.bias
+    wcode = code if weight is None and bias is None else _TYPES[(bias if weight is None else weight).dtype]
+    dx = torch.empty(dy.shape, dtype=dtype, device=device) if need_x else None
+    dweight = torch.empty_like(weight) if need_weight and weight is not None else None
+    dbias = torch.empty_like(bias) if need_bias and bias is not None else None
+    L = load_library()
+    space, nbytes = None, 0
+    if dweight is not None or dbias is not None:
+        nbytes = _norm_space(L, rows, cols)
+        space = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    c = saved.checkpoint
+    x, x_stride = (None, 0) if c is not None else (saved.x.data_ptr(), _rows(saved.x, "x")[3])
+    with _Launch(device) as stream:
+        _check(L.saber_layer_norm_backward(
+            m.data_ptr(), stride, x, x_stride, None if c is None else c.q.data_ptr(), None if c is None else c.scale.data_ptr(),
+            saved.mean.data_ptr(), saved.rstd.data_ptr(), None if weight is None else weight.data_ptr(), rows, cols, code, wcode,
+            None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
+            None if dbias is None else dbias.data_ptr(), None if space is None else space.data_ptr(), nbytes, stream))
+    return dx, dweight, dbias
+
+
+def _norm_space(L, rows, cols):
+    n = _int64()
+    _check(L.saber_layer_norm_backward_workspace(rows, cols, ctypes.addressof(n)))
+    return n.value
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, checkpoint):
+        y, s = layer_norm_forward(x, weight, bias, eps, checkpoint)
+        c = s.checkpoint
+        ctx.save_for_backward(*([s.x] if c is None else [c.q, c.scale]), s.weight, s.bias, s.mean, s.rstd)
+        ctx.held, ctx.dtype = c is not None, x.dtype
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        t = list(ctx.saved_tensors)
+        weight, bias, mean, rstd = t[-4:]
+        c = Checkpoint8(t[0], t[1], ctx.dtype) if ctx.held else None
+        saved = NormSaved(None if ctx.held else t[0], c, weight, bias, mean, rstd)
+        dx, dw, db = layer_norm_backward(dy, saved, *ctx.needs_input_grad[:3])
+        return dx, dw, db, None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
+    """Layer norm over the last dimension, differentiable in ``x``, ``weight`` and ``bias``.  With ``checkpoint`` its input is
+    held in 8 bits between the passes (a quarter to a half of the memory); the gradients then are those at the held values."""
+    return _LayerNorm.apply(x, weight, bias, eps, checkpoint)
+
+
+# ---- softmax cross entropy with its projection ---------------------------------------------------------------------
+
+def _head(x, weight, target):
+    device = _device(x, "x")
+    code = _type("x", x)
+    _device(weight, "weight")
+    _on("weight", weight, device)
+    if weight.dtype != x.dtype:
+        raise TypeError("weight must be %s like x, not %s" % (x.dtype, weight.dtype))
+    if weight.dim() != 2 or weight.shape[1] != x.shape[-1]:
+        raise ValueError("weight must be [words, %d] for features of that width" % x.shape[-1])
+    _device(target, "target")
+    _on("target", target, device)
+    if target.dtype != torch.int64 and target.dtype != torch.int32:
+        raise TypeError("target must be int32 or int64, not %s" % target.dtype)
+    if target.shape != x.shape[:-1]:
+        raise ValueError("target must hold one word per row of x")
+    m, rows, cols, stride = _rows(x, "x")
+    w, vocab, _, w_stride = _rows(weight, "weight")
+    return device, code, m, rows, cols, stride, w, vocab, w_stride, target if target.is_contiguous() else target.contiguous()
+
+
+def _space(call, args, device):
+    """Work space of a pass: how much, and the memory."""
+    n = _int64()
+    _check(call(*args, None, ctypes.addressof(n), None))
+    return n, torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
+
+
+def linear_cross_entropy_forward(x, weight, target):
+    """``(loss, lse)`` per row of ``x``: minus log likelihood of the row's target word under softmax(x weight^T), and the
+    logarithm of the softmax' normaliser; float32, in the shape of ``target``.  The logits are not held.  A negative target
+    leaves its row out (loss 0); one beyond the vocabulary gives NaN."""
+    device, code, m, rows, cols, stride, w, vocab, w_stride, t = _head(x, weight, target)
+    both = torch.empty((2,) + tuple(target.shape), dtype=torch.float32, device=device)
+    loss, lse = both.unbind(0)
+    call = load_library().saber_linear_xent_forward
+    args = (m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), t.dtype == torch.int64, rows, vocab, cols, code, loss.data_ptr(),
+            lse.data_ptr())
+    with _Launch(device) as stream:
+        n, space = _space(call, args, device)
+        _check(call(*args, space.data_ptr(), ctypes.addressof(n), stream))
+    return loss, lse
+
+
+def linear_cross_entropy_backward(dloss, x, weight, target, lse, need_x=True, need_weight=True):
+    """``(dx, dweight)`` for the gradient ``dloss`` (float32) of every row's loss; None where not needed.  ``lse`` is what the
+    forward pass gave."""
+    device, code, m, rows, cols, stride, w, vocab, w_stride, t = _head(x, weight, target)
+    for name, v in (("dloss", dloss), ("lse", lse)):
+        _device(v, name)
+        _on(name, v, device)
+        if v.dtype != torch.float32 or v.shape != target.shape:
+            raise ValueError("%s must be float32, one value per row of x" % name)
+    dloss, lse = dloss.contiguous(), lse.contiguous()
+    dx = torch.empty(x.shape, dtype=x.dtype, device=device) if need_x else None
+    dweight = torch.empty((vocab, cols), dtype=x.dtype, device=device) if need_weight else None
+    call = load_library().saber_linear_xent_backward
+    args = (dloss.data_ptr(), m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), t.dtype == torch.int64, lse.data_ptr(), rows,
+            vocab, cols, code, None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr())
+    with _Launch(device) as stream:
+        n, space = _space(call, args, device)
+        _check(call(*args, space.data_ptr(), ctypes.addressof(n), stream))
+    return dx, dweight
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, target):
+        loss, lse = linear_cross_entropy_forward(x, weight, target)
+        ctx.save_for_backward(x, weight, target, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        x, weight, target, lse = ctx.saved_tensors
+        dx, dw = linear_cross_entropy_backward(dloss, x, weight, target, lse, *ctx.needs_input_grad[:2])
+        return dx, dw, None
+
+
+def linear_cross_entropy(x, weight, target, reduction="mean"):
+    """Softmax cross entropy of ``x weight^T`` against ``target``, differentiable in ``x`` and ``weight``, without the logits in
+    memory in either pass.  Rows with a negative target are left out; ``reduction``: "mean" over the rows counted (0 if
+    there is none), "sum" or "none"."""
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError("reduction must be mean, sum or none, not %r" % (reduction,))
+    loss = _LinearCrossEntropy.apply(x, weight, target)
+    if reduction == "none":
+        return loss
+    loss = loss.sum()
+    return loss / (target >= 0).sum().clamp_(min=1) if reduction == "mean" else loss

@@ -1,0 +1,145 @@
+// Element types, unaligned chunks of eight elements and wavefront sums of the head's operators (gfx950, wave64).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace saber_ops {
+
+constexpr int kChunk = 8;     // elements a lane handles at a time: 16 bytes of a 16-bit type, 32 of binary32
+constexpr int kBlock = 128;   // columns that share a scale of a checkpoint: the chunks of 16 lanes
+
+using f32 = float;
+using f16 = _Float16;
+using bf16 = __bf16;
+
+// 16 bytes at any alignment that the element type allows (global loads and stores of gfx950 take every address)
+struct __attribute__((packed, aligned(1))) Bytes16 { uint32_t v[4]; };
+struct __attribute__((packed, aligned(1))) Bytes8 { uint32_t v[2]; };
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// eight elements from p, of which the first n exist (the others become `fill`); n <= 0: none is read
+template <class T>
+__device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.f) {
+    f32x8 f;
+    if (n >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            typedef T V __attribute__((ext_vector_type(8)));
+            f = __builtin_convertvector(__builtin_bit_cast(V, *reinterpret_cast<const Bytes16 *>(p)), f32x8);
+        } else {
+            struct Two { Bytes16 lo, hi; };
+            f = __builtin_bit_cast(f32x8, *reinterpret_cast<const Two *>(p));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? (float)p[i] : fill;
+    }
+    return f;
+}
+
+// rounds to nearest even; the first n of eight elements
+template <class T>
+__device__ __forceinline__ void store8(T *p, int64_t n, f32x8 f) {
+    if (n >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            typedef T V __attribute__((ext_vector_type(8)));
+            *reinterpret_cast<Bytes16 *>(p) = __builtin_bit_cast(Bytes16, __builtin_convertvector(f, V));
+        } else {
+            struct Two { Bytes16 lo, hi; };
+            *reinterpret_cast<Two *>(p) = __builtin_bit_cast(Two, f);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (T)f[i];
+    }
+}
+
+// a weight or a gradient of one: its type is known at run time, the same for the whole launch
+enum : int { kF32 = 0, kF16 = 1, kBF16 = 2 };
+__device__ __forceinline__ f32x8 load8_as(const void *p, int type, int64_t at, int64_t n, float fill) {
+    if (!p) return f32x8{fill, fill, fill, fill, fill, fill, fill, fill};
+    if (type == kF32) return load8(static_cast<const f32 *>(p) + at, n);
+    if (type == kF16) return load8(static_cast<const f16 *>(p) + at, n);
+    return load8(static_cast<const bf16 *>(p) + at, n);
+}
+__device__ __forceinline__ void store_as(void *p, int type, int64_t at, float v) {
+    if (type == kF32) static_cast<f32 *>(p)[at] = v;
+    else if (type == kF16) static_cast<f16 *>(p)[at] = (f16)v;
+    else static_cast<bf16 *>(p)[at] = (bf16)v;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+
+// sum over each row of 16 lanes by rotations, then over the four rows by lane reads: the same value in every lane, always in
+// the same order
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp<0x128>(v);   // row_ror:8
+    v += dpp<0x124>(v);
+    v += dpp<0x122>(v);
+    v += dpp<0x121>(v);
+    const int b = __float_as_int(v);
+    const float r0 = __int_as_float(__builtin_amdgcn_readlane(b, 0)), r1 = __int_as_float(__builtin_amdgcn_readlane(b, 16));
+    const float r2 = __int_as_float(__builtin_amdgcn_readlane(b, 32)), r3 = __int_as_float(__builtin_amdgcn_readlane(b, 48));
+    return (r0 + r1) + (r2 + r3);
+}
+// largest of the 16 lanes of a row, as unsigned bits: for magnitudes this is the order of the floats, with NaN above infinity
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, dpp<0x128>(v));
+    v = max(v, dpp<0x124>(v));
+    v = max(v, dpp<0x122>(v));
+    v = max(v, dpp<0x121>(v));
+    return v;
+}
+
+// One lane's chunk of a block of 128 columns, in 8 bits: step c = max|x| / 127 of the block, whole numbers round(x / c), ties to
+// even.  A block of zeros has step 0.  A NaN or an infinity makes the step not finite: the block is restored as NaN.
+// All 16 lanes of the block call this together.
+__device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = row_max(top);
+    const float step = __uint_as_float(top) / 127.f;
+    int v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = rintf(x[i] / step);
+        v[i] = step > 0.f && step < INFINITY ? (int)fminf(fmaxf(t, -127.f), 127.f) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        q.v[k] = (uint32_t)(v[4 * k] & 255) | (uint32_t)(v[4 * k + 1] & 255) << 8 | (uint32_t)(v[4 * k + 2] & 255) << 16 |
+                  (uint32_t)(v[4 * k + 3] & 255) << 24;
+    return step;
+}
+__device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {
+    if (n >= 8) *reinterpret_cast<Bytes8 *>(p) = q;
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (int8_t)(q.v[i >> 2] >> (8 * (i & 3)));
+    }
+}
+__device__ __forceinline__ f32x8 load_q(const int8_t *p, int64_t n, float step) {
+    f32x8 f;
+    Bytes8 q = {{0, 0}};
+    if (n >= 8) q = *reinterpret_cast<const Bytes8 *>(p);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) q.v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)((int)(q.v[i >> 2] << (24 - 8 * (i & 3))) >> 24) * step;
+    return f;
+}
+
+}  // namespace saber_ops

@@ -1,0 +1,455 @@
+// Softmax cross entropy of a projection onto a large vocabulary, without the logits in memory, and its gradient.
+//
+//   l_nv = x_n . W_v,   lse_n = log sum_v exp l_nv,   loss_n = lse_n - l_n,t(n)
+//   d_nv = g_n (exp(l_nv - lse_n) - [v = t(n)]),   dx_n = sum_v d_nv W_v,   dW_v = sum_n d_nv x_n
+//
+// Forward: every tile of logits leaves a maximum and a sum of exponentials per row; one small kernel joins them.  Backward: the
+// logits are computed again, one piece of the vocabulary at a time; d of a piece, in the type of the features, is the operand of the
+// two products that follow.
+#pragma once
+#include "ops_product.hpp"
+
+namespace saber_ops {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Targets {
+    const void *p; int wide;   // int64 if wide, else int32
+    __device__ __forceinline__ int64_t at(int64_t n) const {
+        return wide ? static_cast<const int64_t *>(p)[n] : (int64_t)static_cast<const int32_t *>(p)[n];
+    }
+};
+
+// a running maximum and the sum of exponentials relative to it; an empty one is (-inf, 0)
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
+    const float top = fmaxf(m, m2);
+    // (a NaN sum stays NaN; where a maximum is -inf its sum counts as it is: nothing, or NaN)
+    const float a = m == top ? 1.f : expf(m - top), b = m2 == top ? 1.f : expf(m2 - top);
+    s = s * a + s2 * b;
+    m = top;
+}
+
+template <bool EXACT>
+__device__ __forceinline__ float exp_of(float l, float m) {
+    // EXACT: features of binary32.  Otherwise one fused multiply-add and the hardware's 2^x: the argument's rounding costs
+    // 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which the result is stored.
+    if constexpr (EXACT) return expf(l - m);
+    else return __builtin_amdgcn_exp2f((l - m) * kLog2e);
+}
+
+// ---- epilogues of the logits' tiles (m: words, n: rows of features) ----------------------------------------------------------
+
+template <bool EXACT>
+struct ScoreEpilogue {
+    float2 *partial; int64_t rows_pad;   // [tile of words][rows_pad]
+    float *at;                           // logit of the target
+    Targets target;
+    int64_t rows, words, word0;          // rows; words of this piece and the first one's number
+    int tile0;
+
+    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int wave, int, int tm,
+                                           void *lds) const {
+        float2 *join_lds = static_cast<float2 *>(lds);
+        const int first = wm + 4 * (lane >> 4);
+        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;   // words of this lane's rows that exist
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int col = wn + j * 16 + (lane & 15);
+            const int64_t n = n0 + col;
+            const int64_t t64 = n < rows ? target.at(n) - word0 - m0 - first : -1;
+            const int t = t64 < left ? (int)(t64 < -1 ? -1 : t64) : -1;
+            float m = -INFINITY, s = 0.f;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (i * 16 + r == t) at[n] = acc[i][j][r];
+                    if (i * 16 + r >= left) acc[i][j][r] = -INFINITY;
+                    m = fmaxf(m, acc[i][j][r]);
+                }
+            const float ref = m > -INFINITY ? m : 0.f;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s += exp_of<EXACT>(acc[i][j][r], ref);
+            join(m, s, __shfl_xor(m, 16), __shfl_xor(s, 16));
+            join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
+            if (lane < 16) join_lds[(wave / WN) * BN + col] = make_float2(m, s);
+        }
+        __syncthreads();
+        for (int col = threadIdx.x; col < BN; col += WM * WN * 64)
+            if (n0 + col < rows) {
+                float2 v = join_lds[col];
+#pragma unroll
+                for (int w = 1; w < WM; ++w) join(v.x, v.y, join_lds[w * BN + col].x, join_lds[w * BN + col].y);
+                partial[(int64_t)(tile0 + tm) * rows_pad + n0 + col] = v;
+            }
+    }
+};
+
+// d of the piece, [row][words of the piece], PLANES planes of 16 bits; words past the vocabulary are zeros
+template <class T, int PLANES>
+struct GradEpilogue {
+    T *d; int64_t stride, plane;
+    const float *lse, *dloss, *scale;    // scale: power of two that d is multiplied with, or null
+    Targets target;
+    int64_t rows, words, word0, vocab;
+
+    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
+        const int first = wm + 4 * (lane >> 4);
+        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first, room = (int)(stride - m0 < BM ? stride - m0 : BM) - first;
+        const float up = scale ? *scale : 1.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + wn + j * 16 + (lane & 15);
+            if (n >= rows) continue;
+            const int64_t target_n = target.at(n), t64 = target_n - word0 - m0 - first;
+            const int t = t64 < BM ? (int)(t64 < -1 ? -1 : t64) : -1;
+            const bool counted = target_n >= 0;
+            const float top = target_n < vocab ? lse[n] : NAN, g = dloss[n] * up;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                if (i * 16 >= room) continue;   // (the stride is a multiple of 8)
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float q = exp_of<PLANES == 3>(acc[i][j][r], top) - (i * 16 + r == t ? 1.f : 0.f);
+                    v[r] = counted && i * 16 + r < left ? q * g : 0.f;
+                }
+                T *to = d + n * stride + m0 + first + i * 16;
+                union { T t[4]; uint2 u; } out;
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (PLANES == 1) out.t[r] = (T)v[r];
+                        else {   // the upper half of the bits, then of what is left
+                            const uint32_t b = __float_as_uint(v[r]) & 0xffff0000u;
+                            out.t[r] = __builtin_bit_cast(T, (uint16_t)(b >> 16));
+                            const float rest = v[r] - __uint_as_float(b);
+                            v[r] = (b & 0x7f800000u) == 0x7f800000u ? 0.f : rest;
+                        }
+                    }
+                    *reinterpret_cast<uint2 *>(to + q * plane) = out.u;
+                }
+            }
+        }
+    }
+};
+
+// ---- epilogues of the gradients' products (m: columns of features) -----------------------------------------------------------
+
+// dx: [split][rows][stride] partial sums in binary32, over the pieces of the vocabulary
+struct SumEpilogue {
+    float *sums; int64_t stride, rows, cols;
+    int add;
+
+    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int split, int, void *) const {
+        float *to = sums + split * rows * stride;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + wn + j * 16 + (lane & 15);
+            if (n >= rows) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int64_t m = m0 + wm + i * 16 + 4 * (lane >> 4);
+                if (m >= cols) continue;   // cols is a multiple of 8
+                f32x4 *p = reinterpret_cast<f32x4 *>(to + n * stride + m);
+                *p = add ? *p + acc[i][j] : acc[i][j];
+            }
+        }
+    }
+};
+
+// dW: rows n (words) of cols columns in the type of W, any alignment
+template <class T>
+struct StoreEpilogue {
+    T *out; int64_t rows, cols;
+    const float *scale;
+
+    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
+        const float down = scale ? 1.f / *scale : 1.f;
+        const bool whole = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + wn + j * 16 + (lane & 15);
+            if (n >= rows) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int64_t m = m0 + wm + i * 16 + 4 * (lane >> 4);
+                if (m >= cols) continue;
+                T *to = out + n * cols + m;
+                if (whole) {
+                    struct alignas(4 * sizeof(T)) { T t[4]; } v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v.t[r] = (T)(acc[i][j][r] * down);
+                    *reinterpret_cast<decltype(v) *>(to) = v;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (m + r < cols) to[r] = (T)(acc[i][j][r] * down);
+                }
+            }
+        }
+    }
+};
+
+// ---- small kernels ---------------------------------------------------------------------------------------------------------
+
+// Rows of src as aligned rows of 16-bit planes, zeros up to the planes' stride.  Binary32 becomes three planes of bfloat16
+// (cut off, so that their sum is exact; an infinity or NaN stays whole in the first).  `mask`: rows without a target become zeros,
+// so that nothing in them, NaN included, reaches a product.
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, void *dst,
+                                                   int64_t stride, int64_t plane, Targets mask) {
+    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+    if (c >= stride) return;
+    for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
+        f32x8 v;
+        v = load8(src + row * src_stride + c, mask.p && mask.at(row) < 0 ? 0 : cols - c);
+        if constexpr (sizeof(T) == 2) store8(static_cast<T *>(dst) + row * stride + c, 8, v);
+        else {
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                uint32_t h[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t b = __float_as_uint(v[i]) & 0xffff0000u;
+                    const bool odd = (b & 0x7f800000u) == 0x7f800000u;
+                    // a NaN whose upper half would read as an infinity keeps a bit of it
+                    h[i] = (odd && (__float_as_uint(v[i]) & 0x7fffffu) ? b | 0x400000u : b) >> 16;
+                    const float rest = v[i] - __uint_as_float(b);
+                    v[i] = odd ? 0.f : rest;
+                }
+                u32x4 o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = h[2 * i] | h[2 * i + 1] << 16;
+                *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(dst) + q * plane + row * stride + c) = o;
+            }
+        }
+    }
+}
+
+// joins the partial sums of a row: 16 rows per workgroup, 64 groups of lanes over the parts
+__global__ __launch_bounds__(1024) void score_join_kernel(const float2 *partial, int64_t rows_pad, int parts, const float *at, Targets target,
+                                                          int64_t rows, int64_t vocab, float *loss, float *lse) {
+    __shared__ float2 lds[64][17];
+    const int64_t n = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+    const int grp = threadIdx.x >> 4;
+    float m = -INFINITY, s = 0.f;
+    if (n < rows)
+        for (int p = grp; p < parts; p += 64) {
+            const float2 v = partial[(int64_t)p * rows_pad + n];
+            join(m, s, v.x, v.y);
+        }
+    lds[grp][threadIdx.x & 15] = make_float2(m, s);
+    for (int half = 32; half; half >>= 1) {
+        __syncthreads();
+        if (grp < half) {
+            const float2 v = lds[grp + half][threadIdx.x & 15];
+            join(m, s, v.x, v.y);
+            lds[grp][threadIdx.x & 15] = make_float2(m, s);
+        }
+    }
+    if (grp == 0 && n < rows) {
+        const float l = m + logf(s);
+        const int64_t t = target.at(n);
+        lse[n] = l;
+        loss[n] = t < 0 ? 0.f : t < vocab ? l - at[n] : NAN;
+    }
+}
+
+// The power of two that brings the largest |dloss| to 2^14 .. 2^15: d of 16-bit floats, |d| <= |dloss|, then neither overflows nor
+// loses bits until it is 2^-29 of the largest.  1 where there is nothing to scale or the largest is not finite.
+__global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Targets target, int64_t rows, float *scale) {
+    __shared__ uint32_t lds[16];
+    uint32_t top = 0;
+    for (int64_t n = threadIdx.x; n < rows; n += 1024)
+        if (target.at(n) >= 0) top = max(top, __float_as_uint(dloss[n]) & 0x7fffffffu);
+    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) top = max(top, lds[i]);
+        const int e = (int)(top >> 23);   // biased exponent; 2^(e-127) <= top < 2^(e-126)
+        int up = 127 + (141 - e);         // of the scale; kept within the normal numbers, as its inverse is
+        up = up < 1 ? 1 : up > 253 ? 253 : up;
+        *scale = top == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)up << 23);
+    }
+}
+
+// dx = sum of the splits' partial sums, in a fixed order
+template <class T>
+__global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits, int64_t rows, int64_t stride, int64_t cols, const float *scale,
+                                                  T *dx) {
+    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+    if (c >= cols) return;
+    const float down = scale ? 1.f / *scale : 1.f;
+    for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
+        f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < splits; ++k) {
+            f32x8 u;
+            u = load8(sums + (k * rows + row) * stride + c, 8);  // (the stride is a multiple of 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += u[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= down;
+        store8(dx + row * cols + c, cols - c, v);
+    }
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------------
+
+// Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time,
+// any alignment; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its words; a workgroup leaves one
+// partial result per row.
+template <class T, int NT>
+__global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target, int64_t rows,
+                                                        int64_t vocab, int64_t cols, float2 *partial, int64_t rows_pad, float *at) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int PLANES = F32 ? 3 : 1;
+    using M = typename std::conditional<F32, bf16, T>::type;
+    extern __shared__ __attribute__((aligned(16))) char few_lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
+    const int64_t pad = (cols + 31) / 32 * 32, row_bytes = pad * 2 + 16, plane_bytes = rows * row_bytes;
+    // features: 16 bytes apart from a multiple of 128, so that eight rows lie in different banks
+    for (int64_t i = threadIdx.x; i < rows * (pad / 8); i += 256) {
+        const int64_t n = i / (pad / 8), c = (i - n * (pad / 8)) * 8;
+        f32x8 v;
+        v = load8(x + n * x_stride + c, cols - c);
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q) {
+            u32x4 o;
+            if constexpr (!F32) {
+                union { T t[8]; u32x4 u; } k;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) k.t[e] = (T)v[e];
+                o = k.u;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t two = 0;
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const uint32_t b = __float_as_uint(v[2 * e + f]) & 0xffff0000u;
+                        const bool odd = (b & 0x7f800000u) == 0x7f800000u;
+                        two |= ((odd && (__float_as_uint(v[2 * e + f]) & 0x7fffffu) ? b | 0x400000u : b) >> 16) << (16 * f);
+                        const float rest = v[2 * e + f] - __uint_as_float(b);
+                        v[2 * e + f] = odd ? 0.f : rest;
+                    }
+                    o[e] = two;
+                }
+            }
+            *reinterpret_cast<u32x4 *>(few_lds + q * plane_bytes + n * row_bytes + c * 2) = o;
+        }
+    }
+    __syncthreads();
+    float m[NT], s[NT];
+    int64_t t[NT];
+    const char *mine[NT];   // a lane beyond the last row takes the last one: its column is never used
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        m[j] = -INFINITY; s[j] = 0.f;
+        const int64_t n = j * 16 + (lane & 15);
+        t[j] = n < rows ? target.at(n) : -1;
+        mine[j] = few_lds + (n < rows ? n : rows - 1) * row_bytes + grp * 16;
+    }
+    const int64_t tiles = (vocab + 15) / 16;
+    for (int64_t tile = (int64_t)blockIdx.x * 4 + wave; tile < tiles; tile += (int64_t)gridDim.x * 4) {
+        const int64_t v0 = tile * 16, v = v0 + (lane & 15);
+        const T *row = w + (v < vocab ? v : vocab - 1) * w_stride + grp * 8;
+        f32x4 acc[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto step = [&](int64_t k, int64_t n) {
+            u32x4 a[PLANES];
+            if constexpr (!F32) {
+                if (n >= 8) {
+                    const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + k);
+                    a[0] = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
+                } else {
+                    f32x8 f;
+                    f = load8(row + k, n);
+                    union { T t[8]; u32x4 u; } o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o.t[e] = (T)f[e];
+                    a[0] = o.u;
+                }
+            } else {
+                f32x8 f;
+                f = load8(row + k, n);
+#pragma unroll
+                for (int q = 0; q < 3; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t two = 0;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t b = __float_as_uint(f[2 * e + h]) & 0xffff0000u;
+                            const bool odd = (b & 0x7f800000u) == 0x7f800000u;
+                            two |= ((odd && (__float_as_uint(f[2 * e + h]) & 0x7fffffu) ? b | 0x400000u : b) >> 16) << (16 * h);
+                            const float rest = f[2 * e + h] - __uint_as_float(b);
+                            f[2 * e + h] = odd ? 0.f : rest;
+                        }
+                        a[q][e] = two;
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                u32x4 b[PLANES];
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) b[q] = *reinterpret_cast<const u32x4 *>(mine[j] + q * plane_bytes + k * 2);
+                if constexpr (!F32) acc[j] = Mfma<M>::run(a[0], b[0], acc[j]);
+                else {
+#pragma unroll
+                    for (int q = 0; q < 6; ++q) acc[j] = Mfma<M>::run(a[(0x001012 >> (4 * q)) & 15], b[(0x010210 >> (4 * q)) & 15], acc[j]);
+                }
+            }
+        };
+        int64_t k = 0;
+        for (; k + 256 <= cols; k += 256) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) step(k + 32 * u, 8);
+        }
+        for (; k + 32 <= cols; k += 32) step(k, 8);
+        if (k < cols) step(k, cols - k - grp * 8);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t lane_v = v0 + 4 * grp;
+            float top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (lane_v + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
+                if (lane_v + r >= vocab) acc[j][r] = -INFINITY;
+                top = fmaxf(top, acc[j][r]);
+            }
+            const float ref = top > -INFINITY ? top : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += exp_of<F32>(acc[j][r], ref);
+            join(m[j], s[j], top, sum);
+        }
+    }
+    __syncthreads();   // the features have been read: LDS is free
+    float2 *lds = reinterpret_cast<float2 *>(few_lds);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        join(m[j], s[j], __shfl_xor(m[j], 16), __shfl_xor(s[j], 16));
+        join(m[j], s[j], __shfl_xor(m[j], 32), __shfl_xor(s[j], 32));
+        if (lane < 16) lds[wave * NT * 16 + j * 16 + lane] = make_float2(m[j], s[j]);
+    }
+    __syncthreads();
+    if (threadIdx.x < NT * 16 && threadIdx.x < rows) {
+        float2 p = lds[threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) join(p.x, p.y, lds[k * NT * 16 + threadIdx.x].x, lds[k * NT * 16 + threadIdx.x].y);
+        partial[(int64_t)blockIdx.x * rows_pad + threadIdx.x] = p;
+    }
+}
+
+}  // namespace saber_ops

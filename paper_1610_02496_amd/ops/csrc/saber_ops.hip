@@ -1,0 +1,488 @@
+// Host side of the head's operators (include/saber_ops.h): checks of arguments, choice of a kernel's variant, launches.  Nothing here
+// allocates, synchronises or keeps state between calls.
+#include <cstdarg>
+#include <cstdio>
+#include <type_traits>
+
+#include "../../../include/saber_ops.h"
+#include "ops_norm.hpp"
+#include "ops_xent.hpp"
+
+using namespace saber_ops;
+
+namespace {
+
+thread_local char g_err[512] = "";
+int fail(int code, const char *fmt, ...) {
+    va_list ap; va_start(ap, fmt); vsnprintf(g_err, sizeof(g_err), fmt, ap); va_end(ap);
+    return code;
+}
+#define OPS_HIP(expr)                                                                                       \
+    do {                                                                                                    \
+        hipError_t e_ = (expr);                                                                             \
+        if (e_ != hipSuccess)                                                                               \
+            return fail(e_ == hipErrorOutOfMemory ? SABER_ENOMEM : SABER_EDEVICE, "%s failed: %s", #expr, hipGetErrorString(e_)); \
+    } while (0)
+
+constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 20, kMaxWords = (int64_t)1 << 31;
+constexpr int kCus = 256;   // of gfx950: sizes of grids only
+
+size_t size_of(int type) { return type == SABER_F32 ? 4 : 2; }
+bool is_type(int type) { return type == SABER_F32 || type == SABER_F16 || type == SABER_BF16; }
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t parts_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// calls f(T{}) with the element type
+template <class F>
+int with_type(int type, F &&f) {
+    if (type == SABER_F32) return f(f32{});
+    if (type == SABER_F16) return f(f16{});
+    return f(bf16{});
+}
+
+int check_rows(const char *who, int64_t rows, int64_t cols, int dtype) {
+    if (!is_type(dtype)) return fail(SABER_EINVAL, "%s: unknown element type %d", who, dtype);
+    if (rows < 0 || cols < 1) return fail(SABER_EINVAL, "%s: %lld rows of %lld columns", who, (long long)rows, (long long)cols);
+    if (rows >= kMaxRows || cols > kMaxCols) return fail(SABER_ERANGE, "%s: %lld rows of %lld columns (limits 2^31 - 1 and 2^20)", who, (long long)rows, (long long)cols);
+    return SABER_OK;
+}
+int check_stride(const char *who, const char *what, int64_t stride, int64_t cols) {
+    if (stride < cols) return fail(SABER_EINVAL, "%s: rows of %s lie %lld elements apart, fewer than their %lld columns", who, what, (long long)stride, (long long)cols);
+    if (stride > (int64_t)1 << 40) return fail(SABER_ERANGE, "%s: stride of %s", who, what);
+    return SABER_OK;
+}
+int check_pointer(const char *who, const char *what, const void *p, size_t align) {
+    if (!p) return fail(SABER_EINVAL, "%s: %s is null", who, what);
+    if (!aligned(p, align)) return fail(SABER_EINVAL, "%s: %s is not aligned to its elements", who, what);
+    return SABER_OK;
+}
+#define OPS_TRY(expr) do { const int rc_ = (expr); if (rc_ != SABER_OK) return rc_; } while (0)
+
+// ---- layer norm --------------------------------------------------------------------------------------------------------------
+
+// Rows of up to 2,048 columns belong to a wavefront, up to 8,192 to a workgroup of 256 (at most 32 elements of a row per lane: three
+// such sets of the backward pass fit the registers); wider ones are read again for every sum.
+constexpr int64_t kNormCols = 8192;
+
+template <class F>
+int with_norm_shape(int64_t cols, F &&f) {
+    using C1 = std::integral_constant<int, 1>; using C2 = std::integral_constant<int, 2>; using C4 = std::integral_constant<int, 4>;
+    using W = std::integral_constant<int, 64>; using G = std::integral_constant<int, 256>;
+    if (cols <= 512) return f(W{}, C1{});
+    if (cols <= 1024) return f(W{}, C2{});
+    if (cols <= 2048) return f(W{}, C4{});
+    if (cols <= 4096) return f(G{}, C2{});
+    return f(G{}, C4{});
+}
+int64_t rows_per_group(int64_t cols) { return cols <= 2048 ? 4 : 1; }
+// workgroups of the backward pass: each leaves a partial row of both sums
+int64_t norm_parts(int64_t rows, int64_t cols) {
+    if (cols > kNormCols) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
+    const int64_t groups = parts_of(rows > 0 ? rows : 1, rows_per_group(cols));
+    return groups < 2 * kCus ? groups : 2 * kCus;
+}
+
+}  // namespace
+
+extern "C" const char *saber_ops_last_error(void) { return g_err; }
+
+extern "C" int saber_layer_norm_forward(const void *x, int64_t x_stride, const void *weight, const void *bias, int64_t rows, int64_t cols,
+                                        int dtype, int wtype, float eps, void *y, float *mean, float *rstd, int8_t *q, float *scale,
+                                        void *stream) {
+    const char *who = "saber_layer_norm_forward";
+    OPS_TRY(check_rows(who, rows, cols, dtype));
+    if (!is_type(wtype)) return fail(SABER_EINVAL, "%s: unknown type %d of weight and bias", who, wtype);
+    OPS_TRY(check_stride(who, "x", x_stride, cols));
+    if (!(eps >= 0.f)) return fail(SABER_EINVAL, "%s: eps must not be negative", who);
+    if (!q != !scale) return fail(SABER_EINVAL, "%s: q and scale are given together", who);
+    if (rows == 0) return SABER_OK;
+    OPS_TRY(check_pointer(who, "x", x, size_of(dtype)));
+    OPS_TRY(check_pointer(who, "y", y, size_of(dtype)));
+    OPS_TRY(check_pointer(who, "mean", mean, 4));
+    OPS_TRY(check_pointer(who, "rstd", rstd, 4));
+    if (weight) OPS_TRY(check_pointer(who, "weight", weight, size_of(wtype)));
+    if (bias) OPS_TRY(check_pointer(who, "bias", bias, size_of(wtype)));
+    if (scale) OPS_TRY(check_pointer(who, "scale", scale, 4));
+    const NormForward a{x, x_stride, weight, bias, wtype, rows, cols, eps, y, mean, rstd, q, scale};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        if (cols > kNormCols) norm_forward_wide_kernel<T><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+        else {
+            const int64_t groups = parts_of(rows, rows_per_group(cols));
+            const unsigned grid = (unsigned)(groups < 8 * kCus ? groups : 8 * kCus);
+            OPS_TRY(with_norm_shape(cols, [&](auto tpr, auto nc) -> int {
+                if (q) norm_forward_kernel<T, tpr.value, nc.value, true><<<grid, 256, 0, st>>>(a);
+                else norm_forward_kernel<T, tpr.value, nc.value, false><<<grid, 256, 0, st>>>(a);
+                return SABER_OK;
+            }));
+        }
+        OPS_HIP(hipGetLastError());
+        return SABER_OK;
+    });
+}
+
+extern "C" int saber_layer_norm_backward_workspace(int64_t rows, int64_t cols, int64_t *bytes) {
+    OPS_TRY(check_rows("saber_layer_norm_backward_workspace", rows, cols, SABER_F32));
+    if (!bytes) return fail(SABER_EINVAL, "saber_layer_norm_backward_workspace: bytes is null");
+    *bytes = norm_parts(rows, cols) * 2 * cols * 4;
+    return SABER_OK;
+}
+
+extern "C" int saber_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const int8_t *q,
+                                         const float *scale, const float *mean, const float *rstd, const void *weight, int64_t rows,
+                                         int64_t cols, int dtype, int wtype, void *dx, void *dweight, void *dbias, void *workspace,
+                                         int64_t workspace_bytes, void *stream) {
+    const char *who = "saber_layer_norm_backward";
+    OPS_TRY(check_rows(who, rows, cols, dtype));
+    if (!is_type(wtype)) return fail(SABER_EINVAL, "%s: unknown type %d of weight and bias", who, wtype);
+    if (!q != !scale) return fail(SABER_EINVAL, "%s: q and scale are given together", who);
+    if (x && q) return fail(SABER_EINVAL, "%s: either x or a checkpoint of it is given, not both", who);
+    OPS_TRY(check_stride(who, "dy", dy_stride, cols));
+    if (x) OPS_TRY(check_stride(who, "x", x_stride, cols));
+    const bool sums = dweight || dbias;
+    if (dweight) OPS_TRY(check_pointer(who, "dweight", dweight, size_of(wtype)));
+    if (dbias) OPS_TRY(check_pointer(who, "dbias", dbias, size_of(wtype)));
+    if (dx) OPS_TRY(check_pointer(who, "dx", dx, size_of(dtype)));
+    if (weight) OPS_TRY(check_pointer(who, "weight", weight, size_of(wtype)));
+    if (rows > 0) {
+        OPS_TRY(check_pointer(who, "dy", dy, size_of(dtype)));
+        if (q) OPS_TRY(check_pointer(who, "scale", scale, 4));
+        else OPS_TRY(check_pointer(who, "x (or its checkpoint)", x, size_of(dtype)));
+        OPS_TRY(check_pointer(who, "mean", mean, 4));
+        OPS_TRY(check_pointer(who, "rstd", rstd, 4));
+    }
+    const int64_t parts = rows > 0 ? norm_parts(rows, cols) : 0;
+    if (sums && parts) {
+        OPS_TRY(check_pointer(who, "workspace", workspace, 16));
+        if (workspace_bytes < parts * 2 * cols * 4) return fail(SABER_EINVAL, "%s: work space of %lld bytes, %lld are needed", who, (long long)workspace_bytes, (long long)(parts * 2 * cols * 4));
+    }
+    if (!sums && (!dx || rows == 0)) return SABER_OK;
+    const NormBackward a{dy, dy_stride, x, x_stride, q, scale, mean, rstd, weight, wtype, rows, cols, dx,
+                         sums ? static_cast<float *>(workspace) : nullptr, (int)parts};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    OPS_TRY(with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        if (rows == 0) return SABER_OK;
+        if (cols > kNormCols) {
+            if (dx) norm_backward_wide_kernel<T><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+            if (sums) norm_columns_wide_kernel<T><<<dim3((unsigned)parts_of(cols, 2048), (unsigned)parts), 256, 0, st>>>(a);
+        } else
+            OPS_TRY(with_norm_shape(cols, [&](auto tpr, auto nc) -> int {
+                if (q) norm_backward_kernel<T, tpr.value, nc.value, true><<<(unsigned)parts, 256, 0, st>>>(a);
+                else norm_backward_kernel<T, tpr.value, nc.value, false><<<(unsigned)parts, 256, 0, st>>>(a);
+                return SABER_OK;
+            }));
+        OPS_HIP(hipGetLastError());
+        return SABER_OK;
+    }));
+    if (sums) {   // (no rows: zeros)
+        norm_weight_kernel<<<dim3((unsigned)parts_of(cols, 32), 2), 1024, 0, st>>>(static_cast<const float *>(workspace), (int)parts, cols, dweight, dbias, wtype);
+        OPS_HIP(hipGetLastError());
+    }
+    return SABER_OK;
+}
+
+// ---- checkpoints in 8 bits ---------------------------------------------------------------------------------------------------
+
+namespace {
+struct Blocks { unsigned grid; int64_t step_rows, step_blocks; };
+Blocks blocks_of(int64_t rows, int64_t cols) {
+    const int64_t nb = parts_of(cols, kBlock), groups = parts_of(rows * nb, 16), grid = groups < 16 * kCus ? groups : 16 * kCus;
+    return {(unsigned)grid, grid * 16 / nb, grid * 16 % nb};
+}
+}  // namespace
+
+extern "C" int saber_checkpoint8_save(const void *x, int64_t x_stride, int64_t rows, int64_t cols, int dtype, int8_t *q, float *scale,
+                                      void *stream) {
+    const char *who = "saber_checkpoint8_save";
+    OPS_TRY(check_rows(who, rows, cols, dtype));
+    OPS_TRY(check_stride(who, "x", x_stride, cols));
+    if (rows == 0) return SABER_OK;
+    OPS_TRY(check_pointer(who, "x", x, size_of(dtype)));
+    OPS_TRY(check_pointer(who, "q", q, 1));
+    OPS_TRY(check_pointer(who, "scale", scale, 4));
+    const Blocks b = blocks_of(rows, cols);
+    return with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        checkpoint8_save_kernel<T><<<b.grid, 256, 0, static_cast<hipStream_t>(stream)>>>(static_cast<const T *>(x), x_stride, rows, cols, q, scale, b.step_rows, b.step_blocks);
+        OPS_HIP(hipGetLastError());
+        return SABER_OK;
+    });
+}
+
+extern "C" int saber_checkpoint8_restore(const int8_t *q, const float *scale, int64_t rows, int64_t cols, int dtype, void *x, void *stream) {
+    const char *who = "saber_checkpoint8_restore";
+    OPS_TRY(check_rows(who, rows, cols, dtype));
+    if (rows == 0) return SABER_OK;
+    OPS_TRY(check_pointer(who, "q", q, 1));
+    OPS_TRY(check_pointer(who, "scale", scale, 4));
+    OPS_TRY(check_pointer(who, "x", x, size_of(dtype)));
+    const Blocks b = blocks_of(rows, cols);
+    return with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        checkpoint8_restore_kernel<T><<<b.grid, 256, 0, static_cast<hipStream_t>(stream)>>>(q, scale, rows, cols, static_cast<T *>(x), b.step_rows, b.step_blocks);
+        OPS_HIP(hipGetLastError());
+        return SABER_OK;
+    });
+}
+
+// ---- softmax cross entropy with its projection -------------------------------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewLds = 150 * 1024;
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of d, and of packed words, per piece
+
+struct Xent {
+    const void *x; int64_t x_stride;
+    const void *w; int64_t w_stride;
+    int64_t rows, vocab, cols; int dtype;
+    int planes;               // 3 for binary32
+    bool pack_x, pack_w;
+    int64_t cols_pad;         // columns of packed rows
+};
+
+// 16-bit rows that start at multiples of 16 bytes and are whole pieces of 8 elements go to LDS as they lie
+bool direct(const void *p, int64_t stride, int64_t cols, int dtype) {
+    return dtype != SABER_F32 && cols % 8 == 0 && stride % 8 == 0 && aligned(p, 16) && stride <= (int64_t)1 << 21;
+}
+
+int check_xent(const char *who, Xent &c) {
+    OPS_TRY(check_rows(who, c.rows, c.cols, c.dtype));
+    if (c.vocab < 1) return fail(SABER_EINVAL, "%s: a vocabulary of %lld words", who, (long long)c.vocab);
+    if (c.vocab >= kMaxWords) return fail(SABER_ERANGE, "%s: a vocabulary of %lld words (limit 2^31 - 1)", who, (long long)c.vocab);
+    OPS_TRY(check_stride(who, "x", c.x_stride, c.cols));
+    OPS_TRY(check_stride(who, "weight", c.w_stride, c.cols));
+    OPS_TRY(check_pointer(who, "weight", c.w, size_of(c.dtype)));
+    if (c.rows) OPS_TRY(check_pointer(who, "x", c.x, size_of(c.dtype)));
+    c.planes = c.dtype == SABER_F32 ? 3 : 1;
+    c.pack_x = !direct(c.x, c.x_stride, c.cols, c.dtype);
+    c.pack_w = !direct(c.w, c.w_stride, c.cols, c.dtype);
+    c.cols_pad = up(c.cols, 8);
+    return SABER_OK;
+}
+
+// words of a piece: as even as the limit allows, whole tiles (and at most 2^20: offsets within a tile are 32 bits)
+int64_t piece_words(int64_t vocab, int64_t most) {
+    if (most > (int64_t)1 << 20) most = (int64_t)1 << 20;
+    most = most / 256 * 256;
+    if (most < 256) most = 256;
+    const int64_t pieces = parts_of(vocab, most);
+    const int64_t words = up(parts_of(vocab, pieces), 256);
+    return words < up(vocab, 8) ? words : up(vocab, 8);
+}
+
+bool few(const Xent &c) {
+    const int64_t lds = c.rows * (up(c.cols, 32) * 2 + 16) * c.planes;
+    return c.rows <= kFewRows && lds <= kFewLds;
+}
+
+// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself.
+bool large_tiles(int64_t m, int64_t n, int64_t splits) { return parts_of(m, 256) * parts_of(n, 256) * splits >= kCus; }
+
+struct Carve {   // a work space handed out piece by piece; base null: only counted
+    char *base; int64_t at = 0;
+    template <class T> T *take(int64_t n) {
+        T *p = base ? reinterpret_cast<T *>(base + at) : nullptr;
+        at += up(n * (int64_t)sizeof(T), 256);
+        return p;
+    }
+};
+
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; };
+ForwardSpace forward_space(const Xent &c, Carve &s) {
+    ForwardSpace f{};
+    f.rows_pad = up(c.rows, 16);
+    if (few(c)) {
+        const int64_t groups = parts_of(parts_of(c.vocab, 16), 4);
+        f.few_grid = f.parts = groups < 8 * kCus ? groups : 8 * kCus;
+    } else {
+        f.piece = c.pack_w ? piece_words(c.vocab, kPieceBytes / (c.cols_pad * 2 * c.planes)) : c.vocab;
+        f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
+        if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
+        if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * c.planes);
+    }
+    f.partial = s.take<float2>(f.parts * f.rows_pad);
+    f.at = s.take<float>(f.rows_pad);
+    return f;
+}
+
+struct BackwardSpace { float *scale; uint16_t *x, *w, *d; float *sums; int64_t piece; int splits; };
+BackwardSpace backward_space(const Xent &c, Carve &s) {
+    BackwardSpace b{};
+    const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceBytes / (row * 2 * c.planes), most_w = kPieceBytes / (c.cols_pad * 2 * c.planes);
+    b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w);
+    const int64_t steps = parts_of(b.piece, kStep) * (c.planes == 3 ? 6 : 1);
+    // workgroups for every CU: the products over the vocabulary have few tiles, so their steps are shared out
+    const int64_t large = parts_of(c.cols_pad, 256) * parts_of(row, 256), small = parts_of(c.cols_pad, 128) * parts_of(row, 128);
+    int64_t splits = large >= 32 ? parts_of(kCus, large) : parts_of(2 * kCus, small);
+    if (splits > steps / 8) splits = steps / 8;
+    if (splits < 1) splits = 1;
+    b.splits = (int)splits;
+    b.scale = s.take<float>(1);
+    b.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
+    if (c.pack_w) b.w = s.take<uint16_t>(b.piece * c.cols_pad * c.planes);
+    b.d = s.take<uint16_t>(c.rows * b.piece * c.planes);
+    b.sums = s.take<float>(b.splits * c.rows * c.cols_pad);
+    return b;
+}
+
+template <class T>
+int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, int64_t plane, Targets mask, hipStream_t st) {
+    const int64_t y = parts_of(rows, 4);
+    pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, plane, mask);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
+}
+
+template <class T, bool A_SLOW, bool B_SLOW, class E>
+int product(Operand a, Operand b, int64_t k, int planes, int splits, const E &e, hipStream_t st, bool large) {
+    Product p{a, b, k, planes == 3 ? 6 : 1, 0, 0, splits};
+    const int64_t tile = large ? 256 : 128;
+    p.tiles_m = (int)parts_of(a.major, tile);
+    p.tiles_n = (int)parts_of(b.major, tile);
+    const int64_t grid = (int64_t)p.tiles_m * p.tiles_n * splits;
+    if (grid >= (int64_t)1 << 31) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
+    if (large) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 4, E><<<(unsigned)grid, 512, 0, st>>>(p, e);
+    else product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
+}
+
+template <class T> struct MatrixType { using type = T; };
+template <> struct MatrixType<f32> { using type = bf16; };
+
+int check_targets(const char *who, const void *target, int target64) {
+    return check_pointer(who, "target", target, target64 ? 8 : 4);
+}
+
+template <class T, int NT>
+int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
+    int64_t lds = c.rows * (up(c.cols, 32) * 2 + 16) * c.planes;
+    if (lds < NT * 512) lds = NT * 512;
+    const auto kernel = score_few_kernel<T, NT>;
+    if (lds > 64 * 1024) OPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(unsigned)f.few_grid, 256, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
+}
+
+}  // namespace
+
+extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const void *weight, int64_t w_stride, const void *target,
+                                         int target64, int64_t rows, int64_t vocab, int64_t cols, int dtype, float *loss, float *lse,
+                                         void *workspace, int64_t *workspace_bytes, void *stream) {
+    const char *who = "saber_linear_xent_forward";
+    Xent c{x, x_stride, weight, w_stride, rows, vocab, cols, dtype, 0, false, false, 0};
+    OPS_TRY(check_xent(who, c));
+    if (!workspace_bytes) return fail(SABER_EINVAL, "%s: workspace_bytes is null", who);
+    Carve s{static_cast<char *>(workspace)};
+    const ForwardSpace f = forward_space(c, s);
+    if (!workspace) { *workspace_bytes = s.at; return SABER_OK; }
+    if (!aligned(workspace, 256)) return fail(SABER_EINVAL, "%s: the work space is not aligned to 256 bytes", who);
+    if (*workspace_bytes < s.at) return fail(SABER_EINVAL, "%s: work space of %lld bytes, %lld are needed", who, (long long)*workspace_bytes, (long long)s.at);
+    if (rows == 0) return SABER_OK;
+    OPS_TRY(check_targets(who, target, target64));
+    OPS_TRY(check_pointer(who, "loss", loss, 4));
+    OPS_TRY(check_pointer(who, "lse", lse, 4));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const Targets t{target, target64};
+    int64_t parts = 0;
+    OPS_TRY(with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        using M = typename MatrixType<T>::type;
+        if (few(c)) {
+            parts = f.parts;
+            if (rows <= 16) return launch_few<T, 1>(c, f, t, st);
+            if (rows <= 32) return launch_few<T, 2>(c, f, t, st);
+            return launch_few<T, 4>(c, f, t, st);
+        }
+        const int64_t plane_x = rows * c.cols_pad, plane_w = f.piece * c.cols_pad;
+        if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, f.x, plane_x, Targets{nullptr, 0}, st));
+        const Operand ox = c.pack_x ? Operand{f.x, c.cols_pad, plane_x, rows} : Operand{x, x_stride, 0, rows};
+        const bool large = large_tiles(f.piece, rows, 1);
+        for (int64_t v0 = 0; v0 < vocab; v0 += f.piece) {
+            const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
+            const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
+            if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, plane_w, Targets{nullptr, 0}, st));
+            const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
+            const ScoreEpilogue<std::is_same<T, f32>::value> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts};
+            OPS_TRY((product<M, false, false>(ow, ox, cols, c.planes, 1, ep, st, large)));
+            parts += parts_of(words, large ? 256 : 128);
+        }
+        return SABER_OK;
+    }));
+    score_join_kernel<<<(unsigned)parts_of(rows, 16), 1024, 0, st>>>(f.partial, f.rows_pad, (int)parts, f.at, t, rows, vocab, loss, lse);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
+}
+
+extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int64_t x_stride, const void *weight, int64_t w_stride,
+                                          const void *target, int target64, const float *lse, int64_t rows, int64_t vocab, int64_t cols,
+                                          int dtype, void *dx, void *dweight, void *workspace, int64_t *workspace_bytes, void *stream) {
+    const char *who = "saber_linear_xent_backward";
+    Xent c{x, x_stride, weight, w_stride, rows, vocab, cols, dtype, 0, false, false, 0};
+    OPS_TRY(check_xent(who, c));
+    if (!workspace_bytes) return fail(SABER_EINVAL, "%s: workspace_bytes is null", who);
+    Carve s{static_cast<char *>(workspace)};
+    const BackwardSpace b = backward_space(c, s);
+    if (!workspace) { *workspace_bytes = s.at; return SABER_OK; }
+    if (!aligned(workspace, 256)) return fail(SABER_EINVAL, "%s: the work space is not aligned to 256 bytes", who);
+    if (*workspace_bytes < s.at) return fail(SABER_EINVAL, "%s: work space of %lld bytes, %lld are needed", who, (long long)*workspace_bytes, (long long)s.at);
+    if (dx && rows) OPS_TRY(check_pointer(who, "dx", dx, size_of(dtype)));
+    if (dweight) OPS_TRY(check_pointer(who, "dweight", dweight, size_of(dtype)));
+    if (rows) {
+        OPS_TRY(check_targets(who, target, target64));
+        OPS_TRY(check_pointer(who, "dloss", dloss, 4));
+        OPS_TRY(check_pointer(who, "lse", lse, 4));
+    }
+    if (!dweight && (!dx || !rows)) return SABER_OK;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const Targets t{target, target64};
+    return with_type(dtype, [&](auto e) -> int {
+        using T = decltype(e);
+        using M = typename MatrixType<T>::type;
+        constexpr int PLANES = std::is_same<T, f32>::value ? 3 : 1;
+        const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.piece;
+        const float *scale = nullptr;
+        if (rows) {
+            OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, plane_x, t, st));
+            if (std::is_same<T, f16>::value) {
+                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, b.scale);
+                OPS_HIP(hipGetLastError());
+                scale = b.scale;
+            }
+        }
+        for (int64_t v0 = 0; v0 < vocab; v0 += b.piece) {
+            const int64_t words = vocab - v0 < b.piece ? vocab - v0 : b.piece;
+            const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
+            T *dw = dweight ? static_cast<T *>(dweight) + v0 * cols : nullptr;
+            if (rows) {
+                if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, plane_w, Targets{nullptr, 0}, st));
+                const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
+                const Operand ox{b.x, c.cols_pad, plane_x, rows};
+                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.piece, plane_d, lse, dloss, scale, t, rows, words, v0, vocab};
+                OPS_TRY((product<M, false, false>(ow, ox, cols, c.planes, 1, ep, st, large_tiles(words, rows, 1))));
+                if (dx) {
+                    const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
+                    const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.piece, plane_d, rows};
+                    OPS_TRY((product<M, true, false>(cw, od, words, c.planes, b.splits, sum, st, large_tiles(c.cols_pad, rows, b.splits))));
+                }
+            }
+            if (dweight) {   // (without rows: zeros)
+                const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.piece, plane_d, up(words, 8)};
+                const StoreEpilogue<T> store{dw, words, cols, scale};
+                OPS_TRY((product<M, true, true>(cx, cd, rows, c.planes, 1, store, st, large_tiles(cols, words, 1))));
+            }
+        }
+        if (dx && rows) {
+            const int64_t y = parts_of(rows, 4);
+            sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, scale, static_cast<T *>(dx));
+            OPS_HIP(hipGetLastError());
+        }
+        return SABER_OK;
+    });
+}

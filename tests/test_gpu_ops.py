@@ -1,0 +1,425 @@
+"""The head's operators on the GPU against plain implementations in 64 bits.
+
+Tolerances follow from the arithmetic: results are rounded once to their type (u = half a unit in the last place), sums are
+binary32 (2^-24 per addition, bounded by the sum of magnitudes), and between the products of the cross entropy's gradient d is
+held in the type of the features."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1610_02496_amd as pk
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+ROUND = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}   # (bfloat16: 2^-9, and the hardware's flush of what is tiny)
+TINY = {F32: 1e-37, F16: 2.0 ** -24, BF16: 1e-37}
+E = 2.0 ** -24
+
+
+def dev(a, dtype=None):
+    return torch.as_tensor(a).to(device="cuda", dtype=dtype)
+
+
+def make(seed, *shape, dtype=F32, scale=1.0, shift=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g, dtype=torch.float64) * scale + shift).to(dtype)
+
+
+def within(got, want, bound, what):
+    got, want, bound = got.double().cpu(), want.double().cpu(), bound.double().cpu()
+    assert got.shape == want.shape, what
+    off = (got - want).abs()
+    bad = ~(off <= bound)
+    assert not bool(bad.any()), "%s: %d of %d values, worst %.3g against a bound of %.3g" % (
+        what, int(bad.sum()), bad.numel(), float(off[bad].max()), float(bound.expand_as(off)[bad].min()))
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+
+def norm64(x, w, b, eps):
+    x = x.double()
+    m = x.mean(-1, keepdim=True)
+    r = 1 / ((x - m).square().mean(-1, keepdim=True) + eps).sqrt()
+    h = (x - m) * r
+    return h * w + b, m, r, h
+
+
+def steps64(x):
+    """What an 8-bit checkpoint stands for; steps are binary32."""
+    n, h = x.shape
+    out = torch.empty(n, h, dtype=torch.float64)
+    for a in range(0, h, 128):
+        p = x[:, a:a + 128].float()
+        c = p.abs().amax(1, keepdim=True) / torch.full((1,), 127.0)
+        q = torch.where(c > 0, torch.round(p / c), torch.zeros_like(p)).clamp(-127, 127)
+        out[:, a:a + 128] = (q * c).double()
+    return out
+
+
+SHAPES = [(1, 1), (1, 1000), (3, 7), (5, 128), (130, 129), (64, 512), (67, 513), (33, 1000), (21, 1025), (9, 2048), (10, 2049), (7, 4096),
+          (5, 4099), (6, 8192), (3, 8193), (2, 20001), (2100, 96), (4099, 40)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype,wtype,pad,held", [(F32, F32, 0, False), (BF16, BF16, 3, True), (F16, F32, 8, False), (BF16, F32, 0, False),
+                                                  (F32, F32, 5, True), (F16, F16, 1, True)])
+def test_layer_norm_both_passes(rows, cols, dtype, wtype, pad, held):
+    print("layer norm", rows, cols, dtype, wtype, pad, held, flush=True)
+    eps = 1e-5
+    wide = make(1, rows, cols + pad, dtype=dtype, scale=1.7, shift=0.4)
+    x = wide[:, :cols]
+    w, b = make(2, cols, dtype=wtype, scale=0.3, shift=1.0), make(3, cols, dtype=wtype, scale=0.2)
+    dy = make(4, rows, cols + pad, dtype=dtype)[:, :cols]
+    y, saved = pk.ops.layer_norm_forward(dev(wide)[:, :cols], dev(w), dev(b), eps, checkpoint=held)
+    y64, m64, r64, h64 = norm64(x, w.double(), b.double(), eps)
+    steps = 40.0   # additions that one value passes through, at most: 32 in a lane, then the wavefronts
+    amax = x.double().abs().amax(1, keepdim=True)
+    within(saved.mean[:, None], m64, steps * E * amax + 1e-40, "mean")
+    # r depends on the squares of the differences, each off by the mean's error and its own rounding
+    rel = 4 * steps * E * (1 + amax * r64)
+    within(saved.rstd[:, None], r64, rel * r64, "rstd")
+    h_err = rel * (1 + h64.abs())
+    within(y, y64, ROUND[dtype] * y64.abs() * 1.01 + TINY[dtype] + h_err * w.double().abs() + 4 * E * (h64.abs() * w.double().abs() + b.double().abs()), "y")
+    dx, dw, db = pk.ops.layer_norm_backward(dev(make(4, rows, cols + pad, dtype=dtype))[:, :cols], saved)
+    if held:
+        src = steps64(x)
+        assert torch.equal(saved.checkpoint.restore(F32).double().cpu(), src), "the checkpoint's values"
+        h64 = (src - m64) * r64
+    g = dy.double() * w.double()
+    mg, mgh = g.mean(1, keepdim=True), (g * h64).mean(1, keepdim=True)
+    dx64 = r64 * (g - mg - h64 * mgh)
+    h_err = rel * (1 + h64.abs())
+    size = g.abs() + g.abs().mean(1, keepdim=True) + h64.abs() * (g * h64).abs().mean(1, keepdim=True)
+    err = r64 * ((rel + 2 * steps * E) * size + h_err * mgh.abs() + h64.abs() * (g.abs() * h_err).mean(1, keepdim=True))
+    within(dx, dx64, ROUND[dtype] * dx64.abs() * 1.01 + TINY[dtype] + err, "dx")
+    dyd = dy.double()
+    adds = (rows / 4 + 64) * E
+    dw64, db64 = (dyd * h64).sum(0), dyd.sum(0)
+    within(dw, dw64, ROUND[wtype] * dw64.abs() * 1.01 + TINY[wtype] + adds * (dyd * h64).abs().sum(0) + (dyd.abs() * h_err).sum(0), "dweight")
+    within(db, db64, ROUND[wtype] * db64.abs() * 1.01 + TINY[wtype] + adds * dyd.abs().sum(0), "dbias")
+
+
+def test_layer_norm_parts_and_absent_vectors():
+    x, w, b, dy = make(1, 37, 300), make(2, 300), make(3, 300), make(4, 37, 300)
+    y, s = pk.ops.layer_norm_forward(dev(x))
+    within(y, norm64(x, 1.0, 0.0, 1e-5)[0], torch.full((1,), 2e-5), "y")
+    assert pk.ops.layer_norm_backward(dev(dy), s)[1:] == (None, None)
+    full = pk.ops.layer_norm_backward(dev(dy), pk.ops.layer_norm_forward(dev(x), dev(w), dev(b))[1])
+    s = pk.ops.layer_norm_forward(dev(x), dev(w), dev(b))[1]
+    for need in ((True, False, False), (False, True, False), (False, False, True), (False, False, False)):
+        got = pk.ops.layer_norm_backward(dev(dy), s, *need)
+        for n, a, f in zip(need, got, full):
+            assert torch.equal(a, f) if n else a is None
+    y, s = pk.ops.layer_norm_forward(dev(x), None, dev(b))
+    within(y, norm64(x, 1.0, b.double(), 1e-5)[0], torch.full((1,), 2e-5), "y without weight")
+    assert pk.ops.layer_norm_backward(dev(dy), s)[1] is None
+
+
+def test_layer_norm_no_rows_and_many_dimensions():
+    w = dev(make(1, 64))
+    y, s = pk.ops.layer_norm_forward(torch.empty(0, 64, device="cuda"), w, w)
+    dx, dw, db = pk.ops.layer_norm_backward(torch.empty(0, 64, device="cuda"), s)
+    assert y.shape == dx.shape == (0, 64) and float(dw.abs().sum()) == 0 and float(db.abs().sum()) == 0
+    x = make(2, 3, 5, 64)
+    y, _ = pk.ops.layer_norm_forward(dev(x).transpose(0, 1), w, w)
+    flat, _ = pk.ops.layer_norm_forward(dev(x).transpose(0, 1).reshape(15, 64), w, w)
+    assert torch.equal(y.reshape(15, 64), flat)
+
+
+def test_layer_norm_values_at_the_edge():
+    """Constant rows, rows far from zero, and rows that are not finite: they stay by themselves."""
+    x = torch.zeros(6, 300)
+    x[1] = 7.0
+    x[2] = 1000.0 + torch.arange(300) % 2
+    x[3, 5] = float("nan")
+    x[4, 6] = float("inf")
+    x[5] = make(1, 300)
+    y, s = pk.ops.layer_norm_forward(dev(x), checkpoint=True)
+    y, q = y.cpu(), s.checkpoint.restore().cpu()
+    assert float(y[:2].abs().max()) == 0
+    within(y[2], norm64(x[2:3], 1.0, 0.0, 1e-5)[0][0], torch.full((1,), 3e-4), "far from zero")   # 1000 * 2^-24 * steps / 0.5
+    assert bool(torch.isnan(y[3]).all()) and bool(torch.isnan(y[4]).all())
+    within(y[5], norm64(x[5:6], 1.0, 0.0, 1e-5)[0][0], torch.full((1,), 2e-5), "its own row")
+    assert bool(torch.isnan(q[3, :128]).all()) and bool(torch.isnan(q[4, :128]).all()) and bool((q[3, 128:] == 0).all())
+    assert bool((q[0] == 0).all()) and bool((q[1] == 7.0).all())
+
+
+def test_layer_norm_gradient_against_differences():
+    torch.manual_seed(0)
+    x, w, b = make(1, 4, 50), make(2, 50, shift=1.0), make(3, 50)
+    dy = make(4, 4, 50)
+
+    def f(x, w, b):
+        return float((norm64(x, w, b, 1e-5)[0] * dy.double()).sum())
+
+    xs, ws, bs = (dev(t).requires_grad_() for t in (x, w, b))
+    (pk.ops.layer_norm(xs, ws, bs) * dev(dy)).sum().backward()
+    for got, at in ((xs, 0), (ws, 1), (bs, 2)):
+        args = [t.double() for t in (x, w, b)]
+        for k in (0, 17, 49):
+            i = (1, k) if at == 0 else (k,)
+            up, down = [a.clone() for a in args], [a.clone() for a in args]
+            up[at][i] += 1e-5
+            down[at][i] -= 1e-5
+            want = (f(*up) - f(*down)) / 2e-5
+            assert abs(float(got.grad[i]) - want) < 1e-4 * max(1.0, abs(want)), (at, k)
+
+
+# ---- checkpoints -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (2, 127), (3, 129), (17, 777), (5, 4096), (3001, 130)])
+@pytest.mark.parametrize("dtype,pad", [(F32, 0), (F32, 3), (F16, 1), (BF16, 0), (BF16, 8)])
+def test_checkpoint8_holds_what_it_says(rows, cols, dtype, pad):
+    print("checkpoint8", rows, cols, dtype, pad, flush=True)
+    wide = make(rows + cols, rows, cols + pad, dtype=dtype, scale=3.0)
+    x = wide[:, :cols]
+    c = pk.ops.checkpoint8(dev(wide)[:, :cols])
+    assert c.q.dtype == torch.int8 and c.q.shape == (rows, cols) and c.scale.shape == (rows, (cols + 127) // 128)
+    want = steps64(x)
+    assert torch.equal(c.restore(F32).double().cpu(), want)
+    assert torch.equal(c.restore().cpu(), want.float().to(dtype))
+    step = c.scale.repeat_interleave(128, 1)[:, :cols].double().cpu()
+    assert bool(((want - x.double()).abs() <= step * (0.5 + 2 ** -15)).all())
+
+
+def test_checkpoint8_edges():
+    x = torch.tensor([[0.0] * 4, [1e-45, -1e-45, 0.0, 0.0], [3e38, -3e38, 1.0, 0.0], [127.0, 0.5, 1.5, -2.5]])
+    got = pk.ops.checkpoint8(dev(x)).restore().cpu()
+    assert bool((got[0] == 0).all()) and bool((got[1] == 0).all())
+    within(got[2], x[2], torch.full((1,), 3e38 / 127 / 2 * 1.001), "large")
+    assert got[3].tolist() == [127.0, 0.0, 2.0, -2.0]   # ties to even
+    assert pk.ops.checkpoint8(torch.empty(0, 5, device="cuda")).restore().shape == (0, 5)
+    big = pk.ops.checkpoint8(dev(make(5, 3, 4, 200)))
+    assert big.q.shape == (3, 4, 200) and big.scale.shape == (12, 2)
+
+
+# ---- cross entropy ---------------------------------------------------------------------------------------------------
+
+def xent64(x, w, t, g):
+    x, w = x.double(), w.double()
+    logits = x @ w.T
+    lse = torch.logsumexp(logits, 1)
+    i = torch.arange(len(t))
+    has = t >= 0
+    loss = torch.where(has, lse - logits[i, t.clamp(min=0)], 0.0)
+    d = (logits - lse[:, None]).exp()
+    d[i, t.clamp(min=0)] -= 1
+    d *= torch.where(has, g.double(), 0.0)[:, None]
+    return loss, lse, d @ w, d.T @ x, d, logits
+
+
+XENT = [(1, 1, 1), (1, 5, 8), (2, 300, 17), (16, 129, 32), (17, 1000, 64), (33, 257, 100), (64, 700, 777), (65, 515, 40), (70, 33, 1000),
+        (128, 256, 64), (129, 1025, 72), (300, 2000, 136), (257, 5003, 129), (1, 20000, 512), (5, 3001, 8200)]
+
+
+@pytest.mark.parametrize("rows,vocab,cols", XENT)
+@pytest.mark.parametrize("dtype,pad,wide_target", [(BF16, 0, True), (BF16, 5, False), (F16, 0, False), (F16, 8, True), (F32, 0, True), (F32, 3, False)])
+def test_linear_cross_entropy_both_passes(rows, vocab, cols, dtype, pad, wide_target):
+    print("cross entropy", rows, vocab, cols, dtype, pad, flush=True)
+    x = make(1, rows, cols + pad, dtype=dtype)
+    w = make(2, vocab, cols + pad, dtype=dtype, scale=1.5 / cols ** 0.5)
+    t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(3))
+    t[rows // 2:rows // 2 + rows // 8] = -1
+    g = make(4, rows).abs() + 0.1
+    xd, wd, td = dev(x)[:, :cols], dev(w)[:, :cols], dev(t, torch.int64 if wide_target else torch.int32)
+    x, w = x[:, :cols], w[:, :cols]
+    loss, lse = pk.ops.linear_cross_entropy_forward(xd, wd, td)
+    loss64, lse64, dx64, dw64, d64, logits = xent64(x, w, t, g)
+    mag = x.double().abs() @ w.double().abs().T
+    off = (cols + 8) * E * mag.amax(1) + (2 ** -20 if dtype != F32 else 2 ** -22) * (1 + logits.abs().amax(1))
+    within(lse, lse64, off, "lse")
+    within(loss, loss64, 2 * off, "loss")
+    dx, dw = pk.ops.linear_cross_entropy_backward(dev(g), xd, wd, td, lse)
+    hold = {F32: 2.0 ** -22, F16: 2.0 ** -11, BF16: 2.0 ** -8}[dtype]
+    p = (d64.abs() + 1e-30)
+    t_col = torch.zeros_like(p)
+    t_col[torch.arange(rows), t.clamp(min=0)] = 1.0
+    p_abs = p + t_col * torch.where(t >= 0, g.double(), 0.0)[:, None]           # p g + g at the target: what is rounded
+    d_err = hold * p * 1.01 + p_abs * (4 * off[:, None] + 2 ** -20) + float(g.max()) * 2.0 ** -37   # (binary16's smallest steps, scaled)
+    within(dx, dx64, ROUND[dtype] * dx64.abs() * 1.01 + TINY[dtype] + d_err @ w.double().abs() + (vocab + 8) * E * (p @ w.double().abs()), "dx")
+    within(dw, dw64, ROUND[dtype] * dw64.abs() * 1.01 + TINY[dtype] + d_err.T @ x.double().abs() + (rows + 8) * E * (p.T @ x.double().abs()), "dweight")
+    assert float(dx[td < 0].abs().sum()) == 0
+    only = pk.ops.linear_cross_entropy_backward(dev(g), xd, wd, td, lse, need_weight=False)
+    assert only[1] is None and torch.equal(only[0], dx)
+    only = pk.ops.linear_cross_entropy_backward(dev(g), xd, wd, td, lse, need_x=False)
+    assert only[0] is None and torch.equal(only[1], dw)
+
+
+def test_cross_entropy_in_several_pieces():
+    """Enough rows that the vocabulary is cut: 20,000 rows leave 6,656 words a piece."""
+    rows, vocab, cols = 20_000, 14_001, 40
+    x, w = make(1, rows, cols, dtype=BF16), make(2, vocab, cols, dtype=BF16, scale=0.2)
+    t = torch.randint(-1, vocab, (rows,), generator=torch.Generator().manual_seed(3))
+    xd, wd, td = dev(x), dev(w), dev(t)
+    loss, lse = pk.ops.linear_cross_entropy_forward(xd, wd, td)
+    g = torch.full((rows,), 1.0 / rows)
+    dx, dw = pk.ops.linear_cross_entropy_backward(dev(g), xd, wd, td, lse)
+    # in 64 bits on the device (sizes beyond the CPU's patience)
+    x64, w64 = xd.double(), wd.double()
+    logits = x64 @ w64.T
+    l64 = torch.logsumexp(logits, 1)
+    i = torch.arange(rows, device="cuda")
+    has = td >= 0
+    within(lse, l64, torch.full((1,), 1e-5), "lse")      # (40 + 8) 2^-24 * 10, and the exponentials' 2^-20
+    within(loss, torch.where(has, l64 - logits[i, td.clamp(min=0)], 0.0), torch.full((1,), 2e-5), "loss")
+    d = (logits - l64[:, None]).exp()
+    d[i, td.clamp(min=0)] -= 1
+    d *= (has / rows)[:, None]
+    mag = d.abs()
+    for got, want, size in ((dx, d @ w64, mag @ w64.abs()), (dw, d.T.contiguous() @ x64, mag.T.contiguous() @ x64.abs())):
+        within(got, want, 2 ** -8 * want.abs() + 2 ** -8 * size, "gradient")
+        assert float((got.double() - want).norm() / want.norm()) < 2 ** -8
+
+
+def test_cross_entropy_targets_left_out_and_values_that_are_not_finite():
+    rows, vocab, cols = 80, 300, 64
+    x, w = make(1, rows, cols, dtype=BF16), make(2, vocab, cols, dtype=BF16, scale=0.2)
+    t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(3))
+    g = torch.ones(rows)
+    t[10], t[11] = -1, -100
+    ref = pk.ops.linear_cross_entropy_forward(dev(x), dev(w), dev(t))
+    ref_grads = pk.ops.linear_cross_entropy_backward(dev(g), dev(x), dev(w), dev(t), ref[1])
+    x[10] = float("nan")
+    x[11, 3] = float("inf")
+    g[10] = float("nan")
+    loss, lse = pk.ops.linear_cross_entropy_forward(dev(x), dev(w), dev(t))
+    dx, dw = pk.ops.linear_cross_entropy_backward(dev(g), dev(x), dev(w), dev(t), lse)
+    assert float(loss[10]) == 0 and float(loss[11]) == 0 and torch.equal(loss, ref[0])
+    assert torch.equal(dx, ref_grads[0]) and torch.equal(dw, ref_grads[1])
+    # all rows left out
+    none = torch.full((rows,), -1)
+    loss, lse = pk.ops.linear_cross_entropy_forward(dev(x), dev(w), dev(none))
+    dx, dw = pk.ops.linear_cross_entropy_backward(dev(g), dev(x), dev(w), dev(none), lse)
+    assert float(loss.abs().sum()) == 0 and float(dx.float().abs().sum()) == 0 and float(dw.float().abs().sum()) == 0
+    # a word beyond the vocabulary is loud, and its row alone
+    bad = t.clone()
+    bad[5] = vocab
+    x = make(1, rows, cols, dtype=BF16)
+    loss, lse = pk.ops.linear_cross_entropy_forward(dev(x), dev(w), dev(bad))
+    assert bool(torch.isnan(loss[5])) and int(torch.isnan(loss).sum()) == 1
+    dx, _ = pk.ops.linear_cross_entropy_backward(dev(torch.ones(rows)), dev(x), dev(w), dev(bad), lse)
+    assert bool(torch.isnan(dx[5]).all()) and not bool(torch.isnan(dx[6:]).any())
+
+
+@pytest.mark.parametrize("rows", [3, 100])
+def test_cross_entropy_of_extreme_logits(rows):
+    """One word takes everything; a row whose other words' exponentials vanish; logits of the size of thousands."""
+    vocab, cols = 500, 32
+    x = torch.zeros(rows, cols)
+    x[:, 0] = 1.0
+    w = torch.zeros(vocab, cols)
+    w[:, 0] = -3000.0
+    w[7, 0] = 5000.0
+    t = torch.full((rows,), 7)
+    t[1] = 8
+    for dtype in (F32, BF16):
+        loss, lse = pk.ops.linear_cross_entropy_forward(dev(x, dtype), dev(w, dtype), dev(t))
+        a, b = float(w[7, 0].to(dtype)), float(w[8, 0].to(dtype))
+        assert float(loss[0]) == 0 and float(loss[1]) == a - b and float(lse[0]) == a
+        dx, dw = pk.ops.linear_cross_entropy_backward(torch.ones(rows, device="cuda"), dev(x, dtype), dev(w, dtype), dev(t), lse)
+        assert float(dx[0].float().abs().sum()) == 0 and float(dx[1, 0]) == float(torch.tensor(a - b).to(dtype))
+        assert float(dw[7, 0]) == 1.0 and float(dw[8, 0]) == -1.0
+
+
+def test_cross_entropy_gradient_against_differences():
+    x, w = make(1, 6, 20), make(2, 37, 20, scale=0.4)
+    t = torch.tensor([0, 36, -1, 5, 5, 17])
+
+    def f(x, w):
+        logits = x @ w.T
+        lse = torch.logsumexp(logits, 1)
+        return float(torch.where(t >= 0, lse - logits[torch.arange(6), t.clamp(min=0)], 0.0).sum() / 5)
+
+    xs, ws = dev(x).requires_grad_(), dev(w).requires_grad_()
+    loss = pk.ops.linear_cross_entropy(xs, ws, dev(t))
+    loss.backward()
+    assert abs(float(loss) - f(x.double(), w.double())) < 1e-5
+    for got, at, shape in ((xs, 0, (6, 20)), (ws, 1, (37, 20))):
+        for i in ((0, 0), (2, 3), (5, 19)) + (((36, 7),) if at else ()):
+            up, down = [x.double(), w.double()], [x.double(), w.double()]
+            up[at] = up[at].clone()
+            down[at] = down[at].clone()
+            up[at][i] += 1e-5
+            down[at][i] -= 1e-5
+            want = (f(*up) - f(*down)) / 2e-5
+            assert abs(float(got.grad[i]) - want) < 2e-5 * max(1.0, abs(want)), (at, i)
+
+
+def test_reductions_and_streams():
+    x, w, t = make(1, 90, 64, dtype=BF16), make(2, 700, 64, dtype=BF16, scale=0.2), torch.arange(90) * 7 % 700
+    t[3] = -1
+    xd, wd, td = dev(x), dev(w), dev(t, torch.int32)
+    each = pk.ops.linear_cross_entropy(xd, wd, td, "none")
+    assert float(pk.ops.linear_cross_entropy(xd, wd, td, "sum")) == float(each.sum())
+    assert float(pk.ops.linear_cross_entropy(xd, wd, td)) == float(each.sum() / 89)
+    assert float(pk.ops.linear_cross_entropy(xd, wd, torch.full_like(td, -1))) == 0
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        again = pk.ops.linear_cross_entropy(xd, wd, td, "none")
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(again, each)
+
+
+def test_the_same_bits_every_time():
+    x, w = dev(make(1, 400, 200, dtype=BF16)), dev(make(2, 3000, 200, dtype=BF16, scale=0.2))
+    t, g = dev(torch.arange(400) * 11 % 3000), dev(torch.ones(400))
+    nw = dev(torch.ones(200))
+    runs = []
+    for _ in range(3):
+        loss, lse = pk.ops.linear_cross_entropy_forward(x, w, t)
+        y, s = pk.ops.layer_norm_forward(x, nw, nw, checkpoint=True)
+        runs.append((loss, lse, y) + pk.ops.linear_cross_entropy_backward(g, x, w, t, lse) + pk.ops.layer_norm_backward(x, s))
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
+
+
+def test_captured_into_a_graph():
+    """A step of the head, replayed with other inputs between eager work, against the eager step."""
+    x, w, nw = dev(make(1, 200, 96, dtype=BF16)), dev(make(2, 1500, 96, dtype=BF16, scale=0.2)), dev(make(3, 96, dtype=BF16, shift=1.0))
+    t, g = dev(torch.arange(200) * 7 % 1500), dev(torch.full((200,), 0.01))
+
+    def step():
+        y, s = pk.ops.layer_norm_forward(x, nw, nw, checkpoint=True)
+        loss, lse = pk.ops.linear_cross_entropy_forward(y, w, t)
+        dy, dw = pk.ops.linear_cross_entropy_backward(g, y, w, t, lse)
+        return (loss, dw) + pk.ops.layer_norm_backward(dy, s)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        x.copy_(dev(make(10 + k, 200, 96, dtype=BF16)))
+        graph.replay()
+        got = [o.clone() for o in out]
+        torch.cuda.synchronize()
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+def test_refusals_on_tensors():
+    x, w, t = torch.zeros(4, 8, device="cuda"), torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    ops = pk.ops
+    for call, kind in ((lambda: ops.layer_norm_forward(x.cpu()), ValueError), (lambda: ops.layer_norm_forward(x.double()), TypeError),
+                       (lambda: ops.layer_norm_forward(x, w[0, :7]), ValueError), (lambda: ops.layer_norm_forward(x, w[0], w[0].half()), TypeError),
+                       (lambda: ops.layer_norm_forward(x, w[0].cpu()), ValueError), (lambda: ops.layer_norm_forward(x, eps=-1.0), pk.SaberError),
+                       (lambda: ops.layer_norm_forward(torch.zeros(4, 0, device="cuda")), pk.SaberError),
+                       (lambda: ops.checkpoint8(t), TypeError), (lambda: ops.checkpoint8([1.0]), TypeError),
+                       (lambda: ops.layer_norm_backward(x.half(), ops.layer_norm_forward(x)[1]), TypeError),
+                       (lambda: ops.layer_norm_backward(x[:2], ops.layer_norm_forward(x)[1]), ValueError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w[:, :7], t), ValueError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w.half(), t), TypeError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w, t[:3]), ValueError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w, t.float()), TypeError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w, t.cpu()), ValueError),
+                       (lambda: ops.linear_cross_entropy_forward(x, w[:0], t), pk.SaberError),
+                       (lambda: ops.linear_cross_entropy_backward(t.double(), x, w, t, x[:, 0]), ValueError),
+                       (lambda: ops.linear_cross_entropy(x, w, t, "max"), ValueError)):
+        with pytest.raises(kind):
+            call()
+    assert np.isfinite(float(ops.linear_cross_entropy(x, w, t)))   # and goes on working
