@@ -12,6 +12,9 @@
 // Operands of binary32 come as three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each); the six
 // products of planes whose weights exceed 2^-24 are added as further steps along k ("segments"), smallest first.
 #pragma once
+#include <type_traits>
+#include <utility>
+
 #include "ops_common.hpp"
 
 namespace saber_ops {
@@ -33,7 +36,7 @@ struct Operand {
 };
 struct Product {
     Operand a, b;
-    int64_t k;           // extent of k; where k is fastest the stored rows go on to the next multiple of 8, with zeros in one operand
+    uint32_t k;          // extent of k; where k is fastest the stored rows go on to the next multiple of 8, with zeros in one operand
     int segments;        // 1, or 6 for planes
     int tiles_m, tiles_n;
     int splits;          // parts of the steps along k, each a workgroup of its own
@@ -55,16 +58,41 @@ template <> struct Mfma<f16> {
     }
 };
 
+// f(0), f(1) .. f(N - 1) with the number as a constant
+template <int... I, class F>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F &&f) { each(std::make_integer_sequence<int, N>{}, f); }
+
+// One product.  With 64 of them a wave's sums are 256 registers, which have to stay in accumulation registers, each in its place; the
+// compiler moves them about, so here they are bound in assembly.  Two waits are the program's then: an operand that a vector
+// instruction wrote may be read two states later (FIRST: of a row of fragments; all of them come from LDS, which has a counter), and
+// the sums may be read seven states after their last product (settled()).
+template <class T, bool FIRST>
+__device__ __forceinline__ void mfma(u32x4 a, u32x4 b, f32x4 &c) {
+    if constexpr (FIRST) asm volatile("s_nop 1");
+    if constexpr (std::is_same<T, bf16>::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <int M, int N>
+__device__ __forceinline__ void settled(f32x4 (&c)[M][N]) {
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < N; j += 4) asm volatile("s_nop 7" : "+a"(c[i][j]), "+a"(c[i][j + 1]), "+a"(c[i][j + 2]), "+a"(c[i][j + 3]));
+}
+
 using LdsBytes = __attribute__((address_space(3))) char;
 
 __device__ __forceinline__ int slow_swizzle(int k) { return ((k & 3) | ((k & 8) >> 1)) << 1; }
 
 // 16 bytes per lane from the buffer to LDS, lane after lane from `lds` on, past the registers.  Nothing waits for it but a wait for
-// the vector memory counter; in assembly, because the compiler puts such a wait in front of every later read of LDS.  It has no
-// result register, so there is none that could be used too early.  s_nop: a write of m0 needs a state before its use.
-__device__ __forceinline__ void load_to_lds(u32x4 rsrc, LdsBytes *lds, uint32_t off) {
+// the vector memory counter; in assembly, because the compiler puts such a wait in front of every later read of LDS.  The load has no
+// result register, so there is none that could be used too early.  m0 needs a state between its write and its use: the addition.
+__device__ __forceinline__ void load_to_lds(u32x4 rsrc, LdsBytes *lds, uint32_t off, uint32_t more) {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(rsrc) : "memory");
+    uint32_t sum;
+    asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds" : "=&v"(sum) : "s"(at), "s"(more), "v"(off), "s"(rsrc) : "memory");
 }
 // a raw buffer: base, bytes; accesses outside read zeros
 __device__ __forceinline__ u32x4 buffer_of(const char *p, uint32_t bytes) {
@@ -73,29 +101,34 @@ __device__ __forceinline__ u32x4 buffer_of(const char *p, uint32_t bytes) {
                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
-// How a wave fetches its share of one operand's tile of W columns (or rows) of m.
+// LDS is a ring of units: 128 rows of m (n) by 64 k, in the layout above; 16 KB.
+constexpr int kUnit = 128, kUnitBytes = kUnit * kStep * 2;
+
+// How a wave fetches its share of one operand's tile of W columns (or rows) of m, unit by unit.
 template <bool SLOW, int W, int WAVES>
 struct Loader {
-    static constexpr int kEach = W * kStep * 2 / 1024 / WAVES;   // instructions of a wave per step, 1 KB each
-    static constexpr int kRows = SLOW ? 1024 / (W * 2) : 8;      // stored rows that one instruction covers
+    static constexpr int kEach = kUnitBytes / 1024 / WAVES;      // requests of a wave per unit, 1 KB each
+    static constexpr int kAll = kEach * (W / kUnit);             // and per step
+    static constexpr int kRows = SLOW ? 4 : 8;                   // stored rows that one request covers
+    static_assert(kEach == 4, "four waves");
     const char *base;        // first element of the tile, plane 0
     uint32_t stride_bytes;
     int64_t plane_bytes;
     uint32_t extent;         // k fastest: bytes from the tile's first row to its last one's start; k slowest: bytes of a row
-    uint32_t voff, vstep;    // of the wave's first instruction, and from one to the next
-    int piece_k;             // k fastest: first k of the lane's piece
+    uint32_t voff;           // of the wave's first request
+    int piece_k;             // k fastest: first k of the lane's piece; k slowest: its piece
+    int lane_k, wave_k;      // k slowest: the stored row of the lane's first piece, within 4, and of the wave's first
 
     __device__ __forceinline__ void init(const Operand &o, int64_t origin, int wave, int lane) {
         stride_bytes = (uint32_t)o.stride * 2;
         plane_bytes = o.plane * 2;
-        vstep = kRows * stride_bytes;
         if constexpr (SLOW) {
             base = static_cast<const char *>(o.p) + origin * 2;
             extent = (uint32_t)((o.major - origin < W ? o.major - origin : W) * 2);
-            constexpr int per_row = W / 8;                       // pieces of a row
-            const int k = wave * kEach * kRows + lane / per_row;
-            voff = k * stride_bytes;
-            piece_k = lane % per_row;
+            voff = (wave * kEach * kRows + (lane >> 4)) * stride_bytes;
+            piece_k = lane & 15;
+            lane_k = lane >> 4;
+            wave_k = wave * kEach * kRows;
         } else {
             base = static_cast<const char *>(o.p) + origin * (int64_t)stride_bytes;
             extent = (uint32_t)((o.major - origin < W ? o.major - origin : W) - 1) * stride_bytes;
@@ -104,55 +137,69 @@ struct Loader {
             voff = (wave * kEach * kRows + (lane >> 3)) * stride_bytes + c * 16;
         }
     }
-    __device__ __forceinline__ void fetch(LdsBytes *lds, int plane, int64_t k0, int64_t k_end, int wave, int lane) const {
+    // the step that is being asked for: its descriptor and the lane's offset in it (for a unit's first two requests, for the others)
+    u32x4 rsrc;
+    uint32_t off[2];
+    int left;                // steps of the segment from it on
+    __device__ __forceinline__ void begin(int plane, uint32_t k0, uint32_t k_end, bool any) {
         const char *p = base + plane * plane_bytes;
         uint32_t bytes, at = voff;
+        left = any ? (int)((k_end - k0 + kStep - 1) / kStep) : 0x7fffffff;
         if constexpr (SLOW) {
-            const uint32_t left = k_end - k0 < kStep ? (uint32_t)(k_end - k0) : kStep;
-            p += k0 * stride_bytes;
-            bytes = (left - 1) * stride_bytes + extent;
+            p += (uint64_t)k0 * stride_bytes;
+            bytes = ((k_end - k0 < kStep ? k_end - k0 : kStep) - 1) * stride_bytes + extent;
         } else {
             p += k0 * 2;
-            const uint32_t left = (uint32_t)((k_end + 7) / 8 * 8 - k0);
-            bytes = extent + left * 2;
-            if ((uint32_t)piece_k >= left) at = 0x80000000u;     // past the row's end: out of the descriptor's bounds
+            const uint32_t more = (k_end + 7) / 8 * 8 - k0;
+            bytes = extent + more * 2;
+            if ((uint32_t)piece_k >= more) at = 0x80000000u;     // past the row's end: out of the descriptor's bounds
         }
-        const u32x4 rsrc = buffer_of(p, bytes);
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            uint32_t off = at + j * vstep;
-            if constexpr (SLOW) {
-                const int k = (wave * kEach + j) * kRows + lane / (W / 8);
-                off += (uint32_t)(piece_k ^ slow_swizzle(k)) * 16;
-            }
-            load_to_lds(rsrc, lds + (wave * kEach + j) * 1024, off);
+        rsrc = buffer_of(p, any ? bytes : 0);                    // past the last step: zeros that nobody uses
+        off[0] = off[1] = at;
+        if constexpr (SLOW) {                                    // the permutation is one for the first two requests, one for the others
+            off[0] += (uint32_t)(piece_k ^ slow_swizzle(lane_k + wave_k)) * 16;
+            off[1] += (uint32_t)(piece_k ^ slow_swizzle(lane_k + wave_k + 2 * kRows)) * 16;
         }
+    }
+    // the next step of a segment that has one after it which is whole
+    __device__ __forceinline__ void next() {
+        uint64_t p = rsrc[0] | (uint64_t)rsrc[1] << 32;
+        p += SLOW ? kStep * (uint64_t)stride_bytes : kStep * 2;
+        rsrc[0] = (uint32_t)p;
+        rsrc[1] = (uint32_t)(p >> 32);
+        if constexpr (!SLOW) rsrc[2] -= kStep * 2;
+        --left;
+    }
+    // request j of the step; lds: the wave's place in the unit that it belongs to
+    __device__ __forceinline__ void one(LdsBytes *lds, int j) const {
+        const int u = j / kEach, i = j % kEach;
+        load_to_lds(rsrc, lds + i * 1024, off[SLOW ? i >> 1 : 0], i * kRows * stride_bytes + (SLOW ? u * kUnit * 2 : u * kUnit * stride_bytes));
     }
 };
 
 // Fragments of 16 rows of m by 32 values of k: lane l holds row l % 16, k 8 (l / 16) .. + 7.  The addresses of a lane differ between
 // fragments by constants, up to the permutation: a register per distinct one, the rest are the instructions' own offsets.
-template <bool SLOW, int W, int N>
+template <bool SLOW, int N>
 struct Reader {
     uint32_t at[SLOW ? N : 2];
-    __device__ __forceinline__ void init(int row, int lane) {
+    __device__ __forceinline__ void init(int row, int lane) {   // row: of the unit
         if constexpr (SLOW) {
             // lane l of 16 addresses row k + l / 4 of four, columns 4 (l % 4) .. + 3; it receives column l of the four rows
             const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), col = row + 4 * (lane & 3);
 #pragma unroll
-            for (int i = 0; i < N; ++i) at[i] = k * W * 2 + (((col + 16 * i) * 2) ^ (slow_swizzle(k) * 16));
+            for (int i = 0; i < N; ++i) at[i] = k * kUnit * 2 + (((col + 16 * i) * 2) ^ (slow_swizzle(k) * 16));
         } else {
             at[0] = (row + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
             at[1] = at[0] ^ 64;
         }
     }
-    // fragment i along m; kk: 0 or 32
+    // fragment i along m of the unit at lds; kk: 0 or 32
     __device__ __forceinline__ u32x4 get(const LdsBytes *lds, int i, int kk) const {
         if constexpr (SLOW) {   // (k + 4 and k + 32 are permuted like k)
             using P = __attribute__((address_space(3))) s16x4 *;
             union { s16x4 h[2]; u32x4 v; } u;
-            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + kk * W * 2));
-            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + (kk + 4) * W * 2));
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + kk * kUnit * 2));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + (kk + 4) * kUnit * 2));
             return u.v;
         } else
             return *(const __attribute__((address_space(3))) u32x4 *)(lds + at[kk / 32] + i * 16 * 128);
@@ -163,8 +210,9 @@ template <class T, bool A_SLOW, bool B_SLOW, int BM, int BN, int WM, int WN, cla
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilogue e) {
 #if defined(__HIP_DEVICE_COMPILE__)   // (the host pass knows neither the matrix instructions nor their types)
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int kA = BM * kStep * 2, kB = BN * kStep * 2;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * (kA + kB)];
+    constexpr int UA = BM / kUnit, UB = BN / kUnit, UNITS = UA + UB, RING = UNITS * 5 / 2;   // units of a step, and in LDS
+    static_assert(UA == UB, "the order of requests");
+    __shared__ __attribute__((aligned(1024))) char smem[RING * kUnitBytes];
     LdsBytes *const lds = (LdsBytes *)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -189,15 +237,16 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
     la.init(p.a, m0, wave, lane);
     lb.init(p.b, n0, wave, lane);
     const int wm = (wave / WN) * TM * 16, wn = (wave % WN) * TN * 16;
-    Reader<A_SLOW, BM, TM> ra;
-    Reader<B_SLOW, BN, TN> rb;
-    ra.init(wm, lane);
-    rb.init(wn, lane);
+    Reader<A_SLOW, TM> ra;
+    Reader<B_SLOW, TN> rb;
+    ra.init(wm % kUnit, lane);
+    rb.init(wn % kUnit, lane);
 
     const int per_seg = (int)((p.k + kStep - 1) / kStep), steps = per_seg * p.segments;
     const int first = (int)((int64_t)steps * split / p.splits), last = (int)((int64_t)steps * (split + 1) / p.splits);
-    int seg = first / per_seg;                         // of the step that is fetched next
-    int64_t k0 = (int64_t)(first - seg * per_seg) * kStep;
+
+    typename Epilogue::template State<TN> state;       // what the epilogue reads of its columns: on its way during the loop
+    e.prepare(state, n0 + wn + (lane & 15));
 
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -205,46 +254,113 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    auto fetch = [&](int buf) {
-        la.fetch(lds + buf * kA, plane_a(seg, p.segments), k0, p.k, wave, lane);
-        lb.fetch(lds + 2 * kA + buf * kB, plane_b(seg, p.segments), k0, p.k, wave, lane);
-        k0 += kStep;
-        if (k0 >= p.k) { k0 = 0; ++seg; }
+    // A step has two halves of 32 k: while the matrix cores work on one half's fragments, the next half's are read.  It goes in GROUPS
+    // groups of one row of fragments each, with one request for data to come in each group: the path from memory to LDS serves
+    // requests at just the pace of the products, and a wave that has to wait for it is one that multiplies nothing.
+    // Before group FREE everyone has read all of step s.  The ring has room for two and a half steps, so B of step s + 2 then goes where
+    // A of step s was, and A of step s + 3 where B of step s was.  Before group NEED step s + 1 has arrived.
+    constexpr int LA = Loader<A_SLOW, BM, WAVES>::kAll, LB = Loader<B_SLOW, BN, WAVES>::kAll, EACH = Loader<A_SLOW, BM, WAVES>::kEach;
+    constexpr int GROUPS = 2 * TM, FREE = TM / 2 + 1, NEED = TM + TM / 2;
+    static_assert(LA + LB == GROUPS, "one request per group");
+    constexpr int READ1 = (TM + TN + FREE - 2) / (FREE - 1);                 // reads per group: of k 32 .. 63, in groups 0 .. FREE - 2
+    constexpr int READ0 = (TM + TN + GROUPS - NEED - 1) / (GROUPS - NEED);   // of the next step's k 0 .. 31, from group NEED on
+    constexpr int AHEAD = GROUPS - FREE - LB;                                // requests for A of step s + 2 before step s begins
+    u32x4 fa[2][TM], fb[2][TN];
+    // where a step's data is asked for: the next step of its segment, or, rarely, another segment, a step that ends in mid-air, or none
+    int seg_a = first / per_seg, seg_b = seg_a, todo_a = last - first, todo_b = todo_a;
+    const uint32_t k_first = (uint32_t)(first - seg_a * per_seg) * kStep;
+    la.begin(plane_a(seg_a, p.segments), k_first, p.k, todo_a > 0);
+    lb.begin(plane_b(seg_b, p.segments), k_first, p.k, todo_b > 0);
+    auto next_a = [&] {
+        --todo_a;
+        if (la.left > 2) la.next();
+        else if (la.left == 2) la.begin(plane_a(seg_a, p.segments), (per_seg - 1) * kStep, p.k, todo_a > 0);
+        else { seg_a += todo_a > 0; la.begin(plane_a(seg_a, p.segments), 0, p.k, todo_a > 0); }
+        if (todo_a <= 0) la.rsrc[2] = 0;
     };
-    auto step = [&](int buf, int s) {
-        if (s + 1 < last) {
-            fetch(buf ^ 1);
-            __builtin_amdgcn_s_waitcnt(0x0f70 | (la.kEach + lb.kEach));   // all but what has just been asked for
-        } else
-            __builtin_amdgcn_s_waitcnt(0x0f70);
+    auto next_b = [&] {
+        --todo_b;
+        if (lb.left > 2) lb.next();
+        else if (lb.left == 2) lb.begin(plane_b(seg_b, p.segments), (per_seg - 1) * kStep, p.k, todo_b > 0);
+        else { seg_b += todo_b > 0; lb.begin(plane_b(seg_b, p.segments), 0, p.k, todo_b > 0); }
+        if (todo_b <= 0) lb.rsrc[2] = 0;
+    };
+    // places in the ring; the wave's own part of a unit
+    auto after = [&](LdsBytes *q, int units) { q += units * kUnitBytes; return q >= lds + RING * kUnitBytes ? q - RING * kUnitBytes : q; };
+    const int own = wave * EACH * 1024;
+    LdsBytes *to_a = lds, *to_b = lds + UA * kUnitBytes;                     // of the step that is asked for
+    auto request_a = [&](int j) { la.one((UA > 1 && j >= EACH ? after(to_a, 1) : to_a) + own, j); };
+    auto request_b = [&](int j) { lb.one((UB > 1 && j >= EACH ? after(to_b, 1) : to_b) + own, j); };
+    LdsBytes *from_a = lds + wm / kUnit * kUnitBytes, *from_b = lds + (UA + wn / kUnit) * kUnitBytes;   // of the step that is read
+    auto read = [&](int set, int j, int kk) {
+        if (j < TN) fb[set][j] = rb.get(from_b, j, kk);
+        else if (j < TN + TM) fa[set][j - TN] = ra.get(from_a, j - TN, kk);
+    };
+    auto barrier = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-        const LdsBytes *a = lds + buf * kA, *b = lds + 2 * kA + buf * kB;
-#pragma unroll
-        for (int kk = 0; kk < kStep; kk += 32) {
-            u32x4 fb[TN];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = rb.get(b, j, kk);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const u32x4 fa = ra.get(a, i, kk);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = Mfma<T>::run(fa, fb[j], acc[i][j]);
-            }
-            __builtin_amdgcn_sched_barrier(0);   // the fragments of one half at a time: both do not fit the registers
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-        __builtin_amdgcn_s_barrier();   // the buffer may be written again
     };
-    static_assert(Loader<A_SLOW, BM, WAVES>::kEach + Loader<B_SLOW, BN, WAVES>::kEach < 16, "the wait's count");
-    if (first < last) fetch(0);
-    int s = first;
-    for (; s + 1 < last; s += 2) {
-        step(0, s);
-        step(1, s + 1);
+    // all but the last n requests have arrived
+#define SABER_OPS_ARRIVED(n) __builtin_amdgcn_s_waitcnt(0x0f70 | ((n) & 15) | ((n) >> 4) << 14)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int j = 0; j < LA; ++j) request_a(j);
+#pragma unroll
+        for (int j = 0; j < LB; ++j) request_b(j);
+        next_a();
+        to_a = after(to_a, UNITS);
+        if (q == 0) {
+            next_b();
+            to_b = after(to_b, UNITS);
+        }
     }
-    if (s < last) step(0, s);
-    e.template finish<BM, BN, WM, WN>(acc, m0, n0, wm, wn, lane, wave, split, tm, (void *)smem);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) request_a(j);
+    SABER_OPS_ARRIVED(LA + LB + AHEAD);
+    barrier();
+#pragma unroll
+    for (int j = 0; j < TM + TN; ++j) read(0, j, 0);
+    for (int s = first; s < last; ++s) {
+        each<GROUPS>([&](auto group) {
+            constexpr int g = group.value;
+            if constexpr (g == FREE) barrier();
+            if constexpr (g == NEED) {
+                SABER_OPS_ARRIVED(NEED + GROUPS - FREE - LB);
+                barrier();
+                from_a = after(from_a, UNITS);
+                from_b = after(from_b, UNITS);
+            }
+            // a product, then one other instruction or two while it is at work
+            each<TN>([&](auto col) {
+                constexpr int j = col.value;
+                mfma<T, j == 0>(fa[g / TM][g % TM], fb[g / TM][j], acc[g % TM][j]);
+                if constexpr (g < FREE - 1) {
+#pragma unroll
+                    for (int r = j; r < READ1; r += TN) read(1, g * READ1 + r, 32);
+                }
+                if constexpr (g >= NEED) {
+#pragma unroll
+                    for (int r = j; r < READ0; r += TN) read(0, (g - NEED) * READ0 + r, 0);   // (after the last step: zeros, never used)
+                }
+                if constexpr (j == TN - 3 && g == FREE - 1) { next_b(); to_b = after(to_b, UNITS); }
+                if constexpr (j == TN - 3 && g == FREE + LB - 1) { next_a(); to_a = after(to_a, UNITS); }
+                if constexpr (j == TN - 1) {
+                    if constexpr (g < FREE) request_a(AHEAD + g);
+                    else if constexpr (g < FREE + LB) request_b(g - FREE);
+                    else request_a(g - FREE - LB);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    }
+#undef SABER_OPS_ARRIVED
+    settled(acc);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                    // nothing is on its way to LDS any more: the epilogue may use it
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    e.template finish<BM, BN, WM, WN>(acc, state, m0, n0, wm, wn, lane, wave, split, tm, (void *)smem);
 #endif
 }
 

@@ -29,15 +29,25 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
     m = top;
 }
 
+// exp(l - m) by the hardware's 2^x.  The difference is rounded before it is scaled, so logits of any size keep their precision; the
+// scaling costs 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which a result of 16 bits is stored.  EXACT: features of binary32.
 template <bool EXACT>
-__device__ __forceinline__ float exp_of(float l, float m) {
-    // EXACT: features of binary32.  Otherwise one fused multiply-add and the hardware's 2^x: the argument's rounding costs
-    // 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which the result is stored.
-    if constexpr (EXACT) return expf(l - m);
-    else return __builtin_amdgcn_exp2f((l - m) * kLog2e);
-}
+struct Exp {
+    float m;
+    __device__ __forceinline__ explicit Exp(float top) : m(top) {}
+    __device__ __forceinline__ float operator()(float l) const {
+        if constexpr (EXACT) return expf(l - m);
+        else return __builtin_amdgcn_exp2f((l - m) * kLog2e);
+    }
+};
 
 // ---- epilogues of the logits' tiles (m: words, n: rows of features) ----------------------------------------------------------
+
+// A column's target relative to the tile, clipped to -1 and what a tile cannot hold.
+__device__ __forceinline__ int within_tile(int64_t target, int64_t first_word) {
+    const int64_t t = target - first_word;
+    return t < 0 ? -1 : t > 4096 ? 4096 : (int)t;
+}
 
 template <bool EXACT>
 struct ScoreEpilogue {
@@ -47,32 +57,49 @@ struct ScoreEpilogue {
     int64_t rows, words, word0;          // rows; words of this piece and the first one's number
     int tile0;
 
+    template <int TN> struct State { int64_t target[TN]; };
+    template <int TN>
+    __device__ __forceinline__ void prepare(State<TN> &s, int64_t n) const {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) s.target[j] = n + j * 16 < rows ? target.at(n + j * 16) : -1;
+    }
     template <int BM, int BN, int WM, int WN, int TM, int TN>
-    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int wave, int, int tm,
-                                           void *lds) const {
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int wave,
+                                           int, int tm, void *lds) const {
         float2 *join_lds = static_cast<float2 *>(lds);
         const int first = wm + 4 * (lane >> 4);
         const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;   // words of this lane's rows that exist
+        if (words - m0 < BM) {   // (the vocabulary's last tile alone)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (i * 16 + r >= left)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) acc[i][j][r] = -INFINITY;
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int col = wn + j * 16 + (lane & 15);
-            const int64_t n = n0 + col;
-            const int64_t t64 = n < rows ? target.at(n) - word0 - m0 - first : -1;
-            const int t = t64 < left ? (int)(t64 < -1 ? -1 : t64) : -1;
+            const int t = within_tile(st.target[j], word0 + m0 + first);
+            const bool here = t < left && t < TM * 16 && (t & 12) == 0;      // (t = -1 has all bits)
+            if (__builtin_amdgcn_ballot_w64(here)) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (i * 16 + r == t && here) at[n0 + col] = acc[i][j][r];
+            }
             float m = -INFINITY, s = 0.f;
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (i * 16 + r == t) at[n] = acc[i][j][r];
-                    if (i * 16 + r >= left) acc[i][j][r] = -INFINITY;
-                    m = fmaxf(m, acc[i][j][r]);
-                }
-            const float ref = m > -INFINITY ? m : 0.f;
+                for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
+            const Exp<EXACT> power(m > -INFINITY ? m : 0.f);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s += exp_of<EXACT>(acc[i][j][r], ref);
+                for (int r = 0; r < 4; ++r) s += power(acc[i][j][r]);
             join(m, s, __shfl_xor(m, 16), __shfl_xor(s, 16));
             join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
             if (lane < 16) join_lds[(wave / WN) * BN + col] = make_float2(m, s);
@@ -96,43 +123,68 @@ struct GradEpilogue {
     Targets target;
     int64_t rows, words, word0, vocab;
 
-    template <int BM, int BN, int WM, int WN, int TM, int TN>
-    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
-        const int first = wm + 4 * (lane >> 4);
-        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first, room = (int)(stride - m0 < BM ? stride - m0 : BM) - first;
+    template <int TN> struct State { int64_t target[TN]; float top[TN], g[TN]; };
+    template <int TN>
+    __device__ __forceinline__ void prepare(State<TN> &s, int64_t n) const {
         const float up = scale ? *scale : 1.f;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
+            const bool row = n + j * 16 < rows;
+            s.target[j] = row ? target.at(n + j * 16) : -1;
+            s.top[j] = row ? lse[n + j * 16] : 0.f;
+            s.g[j] = row ? dloss[n + j * 16] * up : 0.f;
+        }
+    }
+    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int,
+                                           void *) const {
+        const int first = wm + 4 * (lane >> 4);
+        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first, room = (int)(stride - m0 < BM ? stride - m0 : BM) - first;
+        const bool whole = words - m0 >= BM;                                 // all but the vocabulary's last tile
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + (lane & 15);
-            if (n >= rows) continue;
-            const int64_t target_n = target.at(n), t64 = target_n - word0 - m0 - first;
-            const int t = t64 < BM ? (int)(t64 < -1 ? -1 : t64) : -1;
-            const bool counted = target_n >= 0;
-            const float top = target_n < vocab ? lse[n] : NAN, g = dloss[n] * up;
+            const int t = within_tile(st.target[j], word0 + m0 + first);
+            const bool here = t < TM * 16 && (t & 12) == 0;
+            const bool counted = st.target[j] >= 0;
+            const Exp<PLANES == 3> power(counted ? (st.target[j] < vocab ? st.top[j] : NAN) : INFINITY);
+            const float g = counted ? st.g[j] : 0.f;
+            const bool any = __builtin_amdgcn_ballot_w64(here || !counted) != 0;
+            T *to = d + n * stride + m0 + first;
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                if (i * 16 >= room) continue;   // (the stride is a multiple of 8)
                 float v[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float q = exp_of<PLANES == 3>(acc[i][j][r], top) - (i * 16 + r == t ? 1.f : 0.f);
-                    v[r] = counted && i * 16 + r < left ? q * g : 0.f;
+                for (int r = 0; r < 4; ++r) v[r] = power(acc[i][j][r]);
+                if (any) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (i * 16 + r == t) v[r] -= 1.f;
+                        if (!counted) v[r] = 0.f;
+                    }
                 }
-                T *to = d + n * stride + m0 + first + i * 16;
-                union { T t[4]; uint2 u; } out;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    v[r] *= g;
+                    if (!whole && i * 16 + r >= left) v[r] = 0.f;
+                }
+                union { T t[4]; uint2 u; } out[PLANES];
 #pragma unroll
                 for (int q = 0; q < PLANES; ++q) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        if constexpr (PLANES == 1) out.t[r] = (T)v[r];
+                        if constexpr (PLANES == 1) out[q].t[r] = (T)v[r];
                         else {   // the upper half of the bits, then of what is left
                             const uint32_t b = __float_as_uint(v[r]) & 0xffff0000u;
-                            out.t[r] = __builtin_bit_cast(T, (uint16_t)(b >> 16));
+                            out[q].t[r] = __builtin_bit_cast(T, (uint16_t)(b >> 16));
                             const float rest = v[r] - __uint_as_float(b);
                             v[r] = (b & 0x7f800000u) == 0x7f800000u ? 0.f : rest;
                         }
                     }
-                    *reinterpret_cast<uint2 *>(to + q * plane) = out.u;
+                }
+                if (n < rows && i * 16 < room) {   // (the stride is a multiple of 8)
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) *reinterpret_cast<uint2 *>(to + i * 16 + q * plane) = out[q].u;
                 }
             }
         }
@@ -146,8 +198,10 @@ struct SumEpilogue {
     float *sums; int64_t stride, rows, cols;
     int add;
 
+    template <int TN> struct State {};
+    template <int TN> __device__ __forceinline__ void prepare(State<TN> &, int64_t) const {}
     template <int BM, int BN, int WM, int WN, int TM, int TN>
-    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int split, int, void *) const {
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int split, int, void *) const {
         float *to = sums + split * rows * stride;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -170,8 +224,10 @@ struct StoreEpilogue {
     T *out; int64_t rows, cols;
     const float *scale;
 
+    template <int TN> struct State {};
+    template <int TN> __device__ __forceinline__ void prepare(State<TN> &, int64_t) const {}
     template <int BM, int BN, int WM, int WN, int TM, int TN>
-    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
+    __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
         const float down = scale ? 1.f / *scale : 1.f;
         const bool whole = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
 #pragma unroll
@@ -428,10 +484,10 @@ __global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_st
                 if (lane_v + r >= vocab) acc[j][r] = -INFINITY;
                 top = fmaxf(top, acc[j][r]);
             }
-            const float ref = top > -INFINITY ? top : 0.f;
+            const Exp<F32> power(top > -INFINITY ? top : 0.f);
             float sum = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += exp_of<F32>(acc[j][r], ref);
+            for (int r = 0; r < 4; ++r) sum += power(acc[j][r]);
             join(m[j], s[j], top, sum);
         }
     }

@@ -310,7 +310,7 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
     return f;
 }
 
-struct BackwardSpace { float *scale; uint16_t *x, *w, *d; float *sums; int64_t piece; int splits; };
+struct BackwardSpace { float *scale; uint16_t *x, *w, *d; float *sums; int64_t piece, stride; int splits; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
     const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceBytes / (row * 2 * c.planes), most_w = kPieceBytes / (c.cols_pad * 2 * c.planes);
@@ -325,7 +325,8 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
     b.scale = s.take<float>(1);
     b.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
     if (c.pack_w) b.w = s.take<uint16_t>(b.piece * c.cols_pad * c.planes);
-    b.d = s.take<uint16_t>(c.rows * b.piece * c.planes);
+    b.stride = up(b.piece, 64) | 64;
+    b.d = s.take<uint16_t>(c.rows * b.stride * c.planes);
     b.sums = s.take<float>(b.splits * c.rows * c.cols_pad);
     return b;
 }
@@ -340,13 +341,13 @@ int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *ds
 
 template <class T, bool A_SLOW, bool B_SLOW, class E>
 int product(Operand a, Operand b, int64_t k, int planes, int splits, const E &e, hipStream_t st, bool large) {
-    Product p{a, b, k, planes == 3 ? 6 : 1, 0, 0, splits};
+    Product p{a, b, (uint32_t)k, planes == 3 ? 6 : 1, 0, 0, splits};
     const int64_t tile = large ? 256 : 128;
     p.tiles_m = (int)parts_of(a.major, tile);
     p.tiles_n = (int)parts_of(b.major, tile);
     const int64_t grid = (int64_t)p.tiles_m * p.tiles_n * splits;
     if (grid >= (int64_t)1 << 31) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
-    if (large) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 4, E><<<(unsigned)grid, 512, 0, st>>>(p, e);
+    if (large) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
     else product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
@@ -446,7 +447,7 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
         using T = decltype(e);
         using M = typename MatrixType<T>::type;
         constexpr int PLANES = std::is_same<T, f32>::value ? 3 : 1;
-        const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.piece;
+        const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.stride;
         const float *scale = nullptr;
         if (rows) {
             OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, plane_x, t, st));
@@ -464,16 +465,16 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
                 if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, plane_w, Targets{nullptr, 0}, st));
                 const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
                 const Operand ox{b.x, c.cols_pad, plane_x, rows};
-                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.piece, plane_d, lse, dloss, scale, t, rows, words, v0, vocab};
+                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab};
                 OPS_TRY((product<M, false, false>(ow, ox, cols, c.planes, 1, ep, st, large_tiles(words, rows, 1))));
                 if (dx) {
                     const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
-                    const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.piece, plane_d, rows};
+                    const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};
                     OPS_TRY((product<M, true, false>(cw, od, words, c.planes, b.splits, sum, st, large_tiles(c.cols_pad, rows, b.splits))));
                 }
             }
             if (dweight) {   // (without rows: zeros)
-                const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.piece, plane_d, up(words, 8)};
+                const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.stride, plane_d, up(words, 8)};
                 const StoreEpilogue<T> store{dw, words, cols, scale};
                 OPS_TRY((product<M, true, true>(cx, cd, rows, c.planes, 1, store, st, large_tiles(cols, words, 1))));
             }
