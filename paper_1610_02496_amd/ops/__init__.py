@@ -72,23 +72,28 @@ def _rows(t, name):
 
 
 class _Launch:
-    """The stream to launch on, with the tensors' device current."""
+    """The raw stream to launch on, with the tensors' device current."""
 
-    __slots__ = ("device", "guard")
+    __slots__ = ("index", "guard")
 
     def __init__(self, device):
-        self.device = device
+        self.index = device.index
         self.guard = None
 
     def __enter__(self):
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
+        if _current_device() != self.index:
+            self.guard = torch.cuda.device(self.index)
             self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return _current_stream(self.index)
 
     def __exit__(self, *exc):
         if self.guard is not None:
             self.guard.__exit__(*exc)
+
+
+# without the objects that torch.cuda.current_stream() makes on every call (2 us of a call of 12)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _vector(t, name, cols, like, of):
@@ -167,8 +172,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
             raise TypeError("weight and bias must have one type, not %s and %s" % (weight.dtype, bias.dtype))
         wcode = bcode
     y = torch.empty(x.shape, dtype=x.dtype, device=device)
-    stats = torch.empty((2, rows), dtype=torch.float32, device=device)
-    mean, rstd = stats.unbind(0)
+    mean = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
     c = _empty_checkpoint(x, rows, cols) if checkpoint else None
     with _Launch(device) as stream:
         _check(load_library().saber_layer_norm_forward(
@@ -278,8 +283,8 @@ def linear_cross_entropy_forward(x, weight, target):
     logarithm of the softmax' normaliser; float32, in the shape of ``target``.  The logits are not held.  A negative target
     leaves its row out (loss 0); one beyond the vocabulary gives NaN."""
     device, code, m, rows, cols, stride, w, vocab, w_stride, t = _head(x, weight, target)
-    both = torch.empty((2,) + tuple(target.shape), dtype=torch.float32, device=device)
-    loss, lse = both.unbind(0)
+    loss = torch.empty(target.shape, dtype=torch.float32, device=device)
+    lse = torch.empty(target.shape, dtype=torch.float32, device=device)
     call = load_library().saber_linear_xent_forward
     args = (m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), t.dtype == torch.int64, rows, vocab, cols, code, loss.data_ptr(),
             lse.data_ptr())

@@ -37,6 +37,30 @@ __device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.f) 
     return f;
 }
 
+// the same in two halves: the bytes as they lie (asked for early), and their values
+template <class T>
+struct Raw8 { uint32_t v[sizeof(T) * 2]; };
+template <class T>
+__device__ __forceinline__ Raw8<T> load_raw8(const T *p, int64_t n) {
+    struct __attribute__((packed, aligned(1))) Any { Raw8<T> r; };
+    if (n >= 8) return reinterpret_cast<const Any *>(p)->r;
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.v[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) {
+            if constexpr (sizeof(T) == 4) r.v[i] = __builtin_bit_cast(uint32_t, p[i]);
+            else r.v[i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i & 1));
+        }
+    return r;
+}
+template <class T>
+__device__ __forceinline__ f32x8 widen(const Raw8<T> &r) {
+    typedef T V __attribute__((ext_vector_type(8)));
+    return __builtin_convertvector(__builtin_bit_cast(V, r), f32x8);
+}
+
 // rounds to nearest even; the first n of eight elements
 template <class T>
 __device__ __forceinline__ void store8(T *p, int64_t n, f32x8 f) {
@@ -108,12 +132,24 @@ __device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     top = row_max(top);
     const float step = __uint_as_float(top) / 127.f;
-    int v[8];
+    // x / step is rounded twice, to binary32 and to a whole number.  The product with the inverse is off by 2^-22 * 127 at most, so it
+    // gives the same whole number unless it is as near as that to the middle of two: then, rarely, the division decides.
+    const float inverse = __builtin_amdgcn_rcpf(step);
+    float t[8];
+    bool near = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float t = rintf(x[i] / step);
-        v[i] = step > 0.f && step < INFINITY ? (int)fminf(fmaxf(t, -127.f), 127.f) : 0;
+        const float r = x[i] * inverse;
+        t[i] = rintf(r);
+        near |= !(fabsf(r - t[i]) < 0.4999f);   // (what is not a number as well)
     }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = step > 0.f && step < INFINITY ? fminf(fmaxf(rintf(x[i] / step), -127.f), 127.f) : 0.f;
+    }
+    int v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (int)t[i];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
         q.v[k] = (uint32_t)(v[4 * k] & 255) | (uint32_t)(v[4 * k + 1] & 255) << 8 | (uint32_t)(v[4 * k + 2] & 255) << 16 |
@@ -128,18 +164,20 @@ __device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {
             if (i < n) p[i] = (int8_t)(q.v[i >> 2] >> (8 * (i & 3)));
     }
 }
-__device__ __forceinline__ f32x8 load_q(const int8_t *p, int64_t n, float step) {
-    f32x8 f;
+__device__ __forceinline__ Bytes8 load_raw_q(const int8_t *p, int64_t n) {
+    if (n >= 8) return *reinterpret_cast<const Bytes8 *>(p);
     Bytes8 q = {{0, 0}};
-    if (n >= 8) q = *reinterpret_cast<const Bytes8 *>(p);
-    else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) q.v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
-    }
+    for (int i = 0; i < 8; ++i)
+        if (i < n) q.v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    return q;
+}
+__device__ __forceinline__ f32x8 widen_q(const Bytes8 &q, float step) {
+    f32x8 f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = (float)((int)(q.v[i >> 2] << (24 - 8 * (i & 3))) >> 24) * step;
     return f;
 }
+__device__ __forceinline__ f32x8 load_q(const int8_t *p, int64_t n, float step) { return widen_q(load_raw_q(p, n), step); }
 
 }  // namespace saber_ops

@@ -45,12 +45,14 @@ __device__ __forceinline__ float row_sum(float v, float *lds, int slot) {
     }
 }
 
-// A row per wavefront (TPR = 64) or per workgroup (TPR = 256); a lane holds NC chunks of eight columns of its row in registers, so
+// A row per wavefront (TPR = 64) or per workgroup (TPR = 256, 512); a lane holds NC chunks of eight columns of its row in registers, so
 // that x is read once.  A workgroup goes over several rows and keeps weight and bias in registers.
+template <int TPR> constexpr int kNormThreads = TPR > 256 ? TPR : 256;   // of a workgroup
+
 template <class T, int TPR, int NC, bool SAVE8>
-__global__ __launch_bounds__(256) void norm_forward_kernel(NormForward a) {
+__global__ __launch_bounds__(kNormThreads<TPR>) void norm_forward_kernel(NormForward a) {
     __shared__ float lds[2 * (TPR / 64)];
-    constexpr int RPB = 256 / TPR;
+    constexpr int RPB = kNormThreads<TPR> / TPR;
     const int t = threadIdx.x % TPR;
     const int64_t H = a.cols;
     f32x8 w[NC], b[NC];
@@ -61,15 +63,23 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormForward a) {
         b[j] = load8_as(a.bias, a.wtype, c, H - c, 0.f);
     }
     const float inv = 1.f / (float)H;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * RPB) {
-        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-        f32x8 v[NC];
-        float s = 0.f;
+    const int64_t step_rows = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    Raw8<T> raw[NC];   // of the row to come
+    auto ask = [&](int64_t r) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
             const int64_t c = (int64_t)(j * TPR + t) * 8;
-            v[j] = load8(x + c, H - c);
+            raw[j] = load_raw8(static_cast<const T *>(a.x) + r * a.x_stride + c, H - c);
         }
+    };
+    if (row < a.rows) ask(row);
+    for (; row < a.rows; row += step_rows) {
+        f32x8 v[NC];
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) v[j] = widen(raw[j]);
+        if (row + step_rows < a.rows) ask(row + step_rows);
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
@@ -118,8 +128,8 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormForward a) {
 // The same layout.  Every lane keeps the sums of dy h and dy of its columns over the rows it sees; a workgroup's wavefronts add
 // theirs in LDS and write one partial row, which norm_weight_kernel adds up in a fixed order.
 template <class T, int TPR, int NC, bool IN8>
-__global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward a) {
-    constexpr int RPB = 256 / TPR;
+__global__ __launch_bounds__(kNormThreads<TPR>) void norm_backward_kernel(NormBackward a) {
+    constexpr int RPB = kNormThreads<TPR> / TPR;
     __shared__ float lds[4 * (TPR / 64)];
     __shared__ float sums[RPB > 1 ? 64 * NC * 8 : 1];
     const int t = threadIdx.x % TPR;
@@ -134,17 +144,35 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward a) {
     }
     const float inv = 1.f / (float)H;
     const int64_t nb = (H + kBlock - 1) / kBlock;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * RPB) {
-        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
-        f32x8 h[NC], g[NC];
+    const int64_t step_rows = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    Raw8<T> raw_g[NC], raw_x[IN8 ? 1 : NC];   // of the row to come
+    Bytes8 raw_q[IN8 ? NC : 1];
+    float raw_step[IN8 ? NC : 1], raw_mean = 0.f, raw_rstd = 0.f;
+    auto ask = [&](int64_t r) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
             const int64_t c = (int64_t)(j * TPR + t) * 8;
-            g[j] = load8(dy + c, H - c);
-            if constexpr (IN8) h[j] = load_q(a.q + row * H + c, H - c, c < H ? a.scale[row * nb + c / kBlock] : 0.f);
-            else h[j] = load8(static_cast<const T *>(a.x) + row * a.x_stride + c, H - c);
+            raw_g[j] = load_raw8(static_cast<const T *>(a.dy) + r * a.dy_stride + c, H - c);
+            if constexpr (IN8) {
+                raw_q[j] = load_raw_q(a.q + r * H + c, H - c);
+                raw_step[j] = c < H ? a.scale[r * nb + c / kBlock] : 0.f;
+            } else
+                raw_x[j] = load_raw8(static_cast<const T *>(a.x) + r * a.x_stride + c, H - c);
         }
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        raw_mean = a.mean[r]; raw_rstd = a.rstd[r];
+    };
+    if (row < a.rows) ask(row);
+    for (; row < a.rows; row += step_rows) {
+        f32x8 h[NC], g[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            g[j] = widen(raw_g[j]);
+            if constexpr (IN8) h[j] = widen_q(raw_q[j], raw_step[j]);
+            else h[j] = widen(raw_x[j]);
+        }
+        const float mean = raw_mean, rstd = raw_rstd;
+        if (row + step_rows < a.rows) ask(row + step_rows);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
@@ -225,8 +253,18 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial,
     void *to = k ? dbias : dweight;
     if (!to) return;
     float s = 0.f;
-    if (c < cols)
-        for (int p = grp; p < parts; p += 32) s += partial[((int64_t)p * 2 + k) * cols + c];
+    if (c < cols) {
+        const float *from = partial + k * cols + c;
+        int p = grp;
+        for (; p + 7 * 32 < parts; p += 8 * 32) {   // eight on their way at a time
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)(p + i * 32) * 2 * cols];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
+        for (; p < parts; p += 32) s += from[(int64_t)p * 2 * cols];
+    }
     lds[grp][threadIdx.x % 32] = s;
     __syncthreads();
     if (grp == 0 && c < cols) {

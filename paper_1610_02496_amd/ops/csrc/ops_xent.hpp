@@ -298,9 +298,18 @@ __global__ __launch_bounds__(1024) void score_join_kernel(const float2 *partial,
     const int grp = threadIdx.x >> 4;
     float m = -INFINITY, s = 0.f;
     if (n < rows)
-        for (int p = grp; p < parts; p += 64) {
-            const float2 v = partial[(int64_t)p * rows_pad + n];
-            join(m, s, v.x, v.y);
+        for (int p = grp; p < parts; p += 8 * 64) {   // eight on their way at a time
+            float2 v[8];
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = p + i * 64 < parts ? partial[(int64_t)(p + i * 64) * rows_pad + n] : make_float2(-INFINITY, 0.f);
+                top = fmaxf(top, v[i].x);
+            }
+            s *= m == top ? 1.f : expf(m - top);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i].y * (v[i].x == top ? 1.f : expf(v[i].x - top));
+            m = top;
         }
     lds[grp][threadIdx.x & 15] = make_float2(m, s);
     for (int half = 32; half; half >>= 1) {
@@ -347,12 +356,16 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
     const float down = scale ? 1.f / *scale : 1.f;
     for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
         f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < splits; ++k) {
-            f32x8 u;
-            u = load8(sums + (k * rows + row) * stride + c, 8);  // (the stride is a multiple of 8)
+        const float *from = sums + row * stride + c;   // (the stride is a multiple of 8)
+        int k = 0;
+        for (; k + 4 <= splits; k += 4) {              // four on their way at a time
+            f32x8 u[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += u[i];
+            for (int i = 0; i < 4; ++i) u[i] = load8(from + (int64_t)(k + i) * rows * stride, 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v += u[i];
         }
+        for (; k < splits; ++k) v += load8(from + (int64_t)k * rows * stride, 8);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= down;
         store8(dx + row * cols + c, cols - c, v);
@@ -364,8 +377,8 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
 // Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time,
 // any alignment; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its words; a workgroup leaves one
 // partial result per row.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target, int64_t rows,
+template <class T, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target, int64_t rows,
                                                         int64_t vocab, int64_t cols, float2 *partial, int64_t rows_pad, float *at) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int PLANES = F32 ? 3 : 1;
@@ -374,7 +387,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_st
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
     const int64_t pad = (cols + 31) / 32 * 32, row_bytes = pad * 2 + 16, plane_bytes = rows * row_bytes;
     // features: 16 bytes apart from a multiple of 128, so that eight rows lie in different banks
-    for (int64_t i = threadIdx.x; i < rows * (pad / 8); i += 256) {
+    for (int64_t i = threadIdx.x; i < rows * (pad / 8); i += WAVES * 64) {
         const int64_t n = i / (pad / 8), c = (i - n * (pad / 8)) * 8;
         f32x8 v;
         v = load8(x + n * x_stride + c, cols - c);
@@ -416,7 +429,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_st
         mine[j] = few_lds + (n < rows ? n : rows - 1) * row_bytes + grp * 16;
     }
     const int64_t tiles = (vocab + 15) / 16;
-    for (int64_t tile = (int64_t)blockIdx.x * 4 + wave; tile < tiles; tile += (int64_t)gridDim.x * 4) {
+    for (int64_t tile = (int64_t)blockIdx.x * WAVES + wave; tile < tiles; tile += (int64_t)gridDim.x * WAVES) {
         const int64_t v0 = tile * 16, v = v0 + (lane & 15);
         const T *row = w + (v < vocab ? v : vocab - 1) * w_stride + grp * 8;
         f32x4 acc[NT];
@@ -503,7 +516,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(const T *x, int64_t x_st
     if (threadIdx.x < NT * 16 && threadIdx.x < rows) {
         float2 p = lds[threadIdx.x];
 #pragma unroll
-        for (int k = 1; k < 4; ++k) join(p.x, p.y, lds[k * NT * 16 + threadIdx.x].x, lds[k * NT * 16 + threadIdx.x].y);
+        for (int k = 1; k < WAVES; ++k) join(p.x, p.y, lds[k * NT * 16 + threadIdx.x].x, lds[k * NT * 16 + threadIdx.x].y);
         partial[(int64_t)blockIdx.x * rows_pad + threadIdx.x] = p;
     }
 }

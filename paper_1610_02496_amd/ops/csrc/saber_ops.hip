@@ -61,26 +61,27 @@ int check_pointer(const char *who, const char *what, const void *p, size_t align
 
 // ---- layer norm --------------------------------------------------------------------------------------------------------------
 
-// Rows of up to 2,048 columns belong to a wavefront, up to 8,192 to a workgroup of 256 (at most 32 elements of a row per lane: three
-// such sets of the backward pass fit the registers); wider ones are read again for every sum.
+// Rows of up to 1,024 columns belong to a wavefront, up to 4,096 to a workgroup of 256, up to 8,192 to one of 512: a lane has 16
+// elements of a row at most, so that the row after can be on its way (the backward pass with 32 a lane: 250 registers, a
+// wavefront per SIMD).  Wider ones are read again for every sum.
 constexpr int64_t kNormCols = 8192;
 
 template <class F>
 int with_norm_shape(int64_t cols, F &&f) {
-    using C1 = std::integral_constant<int, 1>; using C2 = std::integral_constant<int, 2>; using C4 = std::integral_constant<int, 4>;
-    using W = std::integral_constant<int, 64>; using G = std::integral_constant<int, 256>;
+    using C1 = std::integral_constant<int, 1>; using C2 = std::integral_constant<int, 2>;
+    using W = std::integral_constant<int, 64>; using G = std::integral_constant<int, 256>; using GG = std::integral_constant<int, 512>;
     if (cols <= 512) return f(W{}, C1{});
     if (cols <= 1024) return f(W{}, C2{});
-    if (cols <= 2048) return f(W{}, C4{});
+    if (cols <= 2048) return f(G{}, C1{});
     if (cols <= 4096) return f(G{}, C2{});
-    return f(G{}, C4{});
+    return f(GG{}, C2{});
 }
-int64_t rows_per_group(int64_t cols) { return cols <= 2048 ? 4 : 1; }
+int64_t rows_per_group(int64_t cols) { return cols <= 1024 ? 4 : 1; }
 // workgroups of the backward pass: each leaves a partial row of both sums
 int64_t norm_parts(int64_t rows, int64_t cols) {
     if (cols > kNormCols) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
-    const int64_t groups = parts_of(rows > 0 ? rows : 1, rows_per_group(cols));
-    return groups < 2 * kCus ? groups : 2 * kCus;
+    const int64_t groups = parts_of(rows > 0 ? rows : 1, rows_per_group(cols)), most = (cols <= 1024 ? 3 : cols <= 4096 ? 4 : 2) * kCus;
+    return groups < most ? groups : most;
 }
 
 }  // namespace
@@ -113,8 +114,8 @@ extern "C" int saber_layer_norm_forward(const void *x, int64_t x_stride, const v
             const int64_t groups = parts_of(rows, rows_per_group(cols));
             const unsigned grid = (unsigned)(groups < 8 * kCus ? groups : 8 * kCus);
             OPS_TRY(with_norm_shape(cols, [&](auto tpr, auto nc) -> int {
-                if (q) norm_forward_kernel<T, tpr.value, nc.value, true><<<grid, 256, 0, st>>>(a);
-                else norm_forward_kernel<T, tpr.value, nc.value, false><<<grid, 256, 0, st>>>(a);
+                if (q) norm_forward_kernel<T, tpr.value, nc.value, true><<<grid, kNormThreads<tpr.value>, 0, st>>>(a);
+                else norm_forward_kernel<T, tpr.value, nc.value, false><<<grid, kNormThreads<tpr.value>, 0, st>>>(a);
                 return SABER_OK;
             }));
         }
@@ -170,8 +171,8 @@ extern "C" int saber_layer_norm_backward(const void *dy, int64_t dy_stride, cons
             if (sums) norm_columns_wide_kernel<T><<<dim3((unsigned)parts_of(cols, 2048), (unsigned)parts), 256, 0, st>>>(a);
         } else
             OPS_TRY(with_norm_shape(cols, [&](auto tpr, auto nc) -> int {
-                if (q) norm_backward_kernel<T, tpr.value, nc.value, true><<<(unsigned)parts, 256, 0, st>>>(a);
-                else norm_backward_kernel<T, tpr.value, nc.value, false><<<(unsigned)parts, 256, 0, st>>>(a);
+                if (q) norm_backward_kernel<T, tpr.value, nc.value, true><<<(unsigned)parts, kNormThreads<tpr.value>, 0, st>>>(a);
+                else norm_backward_kernel<T, tpr.value, nc.value, false><<<(unsigned)parts, kNormThreads<tpr.value>, 0, st>>>(a);
                 return SABER_OK;
             }));
         OPS_HIP(hipGetLastError());
@@ -275,10 +276,8 @@ int64_t piece_words(int64_t vocab, int64_t most) {
     return words < up(vocab, 8) ? words : up(vocab, 8);
 }
 
-bool few(const Xent &c) {
-    const int64_t lds = c.rows * (up(c.cols, 32) * 2 + 16) * c.planes;
-    return c.rows <= kFewRows && lds <= kFewLds;
-}
+int64_t few_lds(const Xent &c) { return c.rows * (up(c.cols, 32) * 2 + 16) * c.planes; }
+bool few(const Xent &c) { return c.rows <= kFewRows && few_lds(c) <= kFewLds; }
 
 // A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself.
 bool large_tiles(int64_t m, int64_t n, int64_t splits) { return parts_of(m, 256) * parts_of(n, 256) * splits >= kCus; }
@@ -292,13 +291,16 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; int few_waves; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
     if (few(c)) {
-        const int64_t groups = parts_of(parts_of(c.vocab, 16), 4);
-        f.few_grid = f.parts = groups < 8 * kCus ? groups : 8 * kCus;
+        // Features that take most of a CU's LDS leave room for one workgroup, which then has eight wavefronts (61 rows of 777 of
+        // 16 bits, 30,011 words: 47 us with four, TODO with eight)
+        f.few_waves = few_lds(c) > 64 * 1024 ? 8 : 4;
+        const int64_t groups = parts_of(parts_of(c.vocab, 16), f.few_waves), most = f.few_waves == 8 ? kCus : 8 * kCus;
+        f.few_grid = f.parts = groups < most ? groups : most;
     } else {
         f.piece = c.pack_w ? piece_words(c.vocab, kPieceBytes / (c.cols_pad * 2 * c.planes)) : c.vocab;
         f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
@@ -360,15 +362,18 @@ int check_targets(const char *who, const void *target, int target64) {
     return check_pointer(who, "target", target, target64 ? 8 : 4);
 }
 
-template <class T, int NT>
+template <class T, int NT, int WAVES>
 int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
-    int64_t lds = c.rows * (up(c.cols, 32) * 2 + 16) * c.planes;
-    if (lds < NT * 512) lds = NT * 512;
-    const auto kernel = score_few_kernel<T, NT>;
+    const int64_t least = WAVES * NT * 128, lds = few_lds(c) > least ? few_lds(c) : least;   // the wavefronts' results at the end
+    const auto kernel = score_few_kernel<T, NT, WAVES>;
     if (lds > 64 * 1024) OPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<(unsigned)f.few_grid, 256, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
+    kernel<<<(unsigned)f.few_grid, WAVES * 64, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
+}
+template <class T, int NT>
+int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
+    return f.few_waves == 8 ? launch_few<T, NT, 8>(c, f, t, st) : launch_few<T, NT, 4>(c, f, t, st);
 }
 
 }  // namespace
