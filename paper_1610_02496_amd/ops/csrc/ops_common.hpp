@@ -18,35 +18,19 @@ struct __attribute__((packed, aligned(1))) Bytes8 { uint32_t v[2]; };
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-// eight elements from p, of which the first n exist (the others become `fill`); n <= 0: none is read
-template <class T>
-__device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.f) {
-    f32x8 f;
-    if (n >= 8) {
-        if constexpr (sizeof(T) == 2) {
-            typedef T V __attribute__((ext_vector_type(8)));
-            f = __builtin_convertvector(__builtin_bit_cast(V, *reinterpret_cast<const Bytes16 *>(p)), f32x8);
-        } else {
-            struct Two { Bytes16 lo, hi; };
-            f = __builtin_bit_cast(f32x8, *reinterpret_cast<const Two *>(p));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < n ? (float)p[i] : fill;
-    }
-    return f;
-}
-
-// the same in two halves: the bytes as they lie (asked for early), and their values
+// Eight elements from p, of which the first n exist (the others are zeros; n <= 0: none is read), in two halves: the bytes as they
+// lie, which may be asked for early, and their values.
 template <class T>
 struct Raw8 { uint32_t v[sizeof(T) * 2]; };
 template <class T>
 __device__ __forceinline__ Raw8<T> load_raw8(const T *p, int64_t n) {
     struct __attribute__((packed, aligned(1))) Any { Raw8<T> r; };
     if (n >= 8) return reinterpret_cast<const Any *>(p)->r;
+    constexpr int kDwords = sizeof(T) * 2;
     Raw8<T> r;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.v[i] = 0;
+    for (int i = 0; i < kDwords; ++i) r.v[i] = 0;
+    if (n <= 0) return r;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) {
@@ -60,6 +44,9 @@ __device__ __forceinline__ f32x8 widen(const Raw8<T> &r) {
     typedef T V __attribute__((ext_vector_type(8)));
     return __builtin_convertvector(__builtin_bit_cast(V, r), f32x8);
 }
+
+template <class T>
+__device__ __forceinline__ f32x8 load8(const T *p, int64_t n) { return widen(load_raw8(p, n)); }
 
 // rounds to nearest even; the first n of eight elements
 template <class T>
@@ -134,26 +121,25 @@ __device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
     const float step = __uint_as_float(top) / 127.f;
     // x / step is rounded twice, to binary32 and to a whole number.  The product with the inverse is off by 2^-22 * 127 at most, so it
     // gives the same whole number unless it is as near as that to the middle of two: then, rarely, the division decides.
+    // Adding 1.5 * 2^23 rounds to a whole number, which the sum's low byte then holds in two's complement.
+    constexpr float kWhole = 12582912.f;
     const float inverse = __builtin_amdgcn_rcpf(step);
-    float t[8];
+    uint32_t v[8];
     bool near = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float r = x[i] * inverse;
-        t[i] = rintf(r);
-        near |= !(fabsf(r - t[i]) < 0.4999f);   // (what is not a number as well)
+        const float t = fmaf(x[i], inverse, kWhole);
+        near |= !(fabsf(fmaf(x[i], inverse, kWhole - t)) < 0.4999f);   // (what is not a number as well)
+        v[i] = __float_as_uint(t);
     }
     if (near) {
+        const bool sound = step > 0.f && step < INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = step > 0.f && step < INFINITY ? fminf(fmaxf(rintf(x[i] / step), -127.f), 127.f) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = __float_as_uint((sound ? fminf(fmaxf(rintf(x[i] / step), -127.f), 127.f) : 0.f) + kWhole);
     }
-    int v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (int)t[i];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-        q.v[k] = (uint32_t)(v[4 * k] & 255) | (uint32_t)(v[4 * k + 1] & 255) << 8 | (uint32_t)(v[4 * k + 2] & 255) << 16 |
-                  (uint32_t)(v[4 * k + 3] & 255) << 24;
+        q.v[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[4 * k + 3], v[4 * k + 2], 0x0c0c0400), __builtin_amdgcn_perm(v[4 * k + 1], v[4 * k], 0x0c0c0400), 0x05040100);
     return step;
 }
 __device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {
@@ -167,6 +153,7 @@ __device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {
 __device__ __forceinline__ Bytes8 load_raw_q(const int8_t *p, int64_t n) {
     if (n >= 8) return *reinterpret_cast<const Bytes8 *>(p);
     Bytes8 q = {{0, 0}};
+    if (n <= 0) return q;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) q.v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));

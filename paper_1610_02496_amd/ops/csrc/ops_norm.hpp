@@ -299,9 +299,9 @@ __global__ __launch_bounds__(1024) void norm_forward_wide_kernel(NormForward a) 
     float ss = 0.f;
     for (int64_t c = (int64_t)threadIdx.x * 8; c < H; c += 8192) {
         f32x8 v;
-        v = load8(x + c, H - c, mean);
+        v = load8(x + c, H - c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(v[i] - mean, v[i] - mean, ss);
+        for (int i = 0; i < 8; ++i) ss = c + i < H ? fmaf(v[i] - mean, v[i] - mean, ss) : ss;
     }
     const float rstd = 1.f / sqrtf(row_sum<1024>(ss, lds, 1) / (float)H + a.eps);
     for (int64_t c = (int64_t)threadIdx.x * 8; c < H; c += 8192) {

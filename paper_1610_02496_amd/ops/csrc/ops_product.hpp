@@ -46,18 +46,6 @@ struct Product {
 __device__ __forceinline__ int plane_a(int seg, int segments) { return segments == 1 ? 0 : (0x001012 >> (4 * seg)) & 15; }
 __device__ __forceinline__ int plane_b(int seg, int segments) { return segments == 1 ? 0 : (0x010210 >> (4 * seg)) & 15; }
 
-template <class T> struct Mfma;
-template <> struct Mfma<bf16> {
-    static __device__ __forceinline__ f32x4 run(u32x4 a, u32x4 b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    }
-};
-template <> struct Mfma<f16> {
-    static __device__ __forceinline__ f32x4 run(u32x4 a, u32x4 b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    }
-};
-
 // f(0), f(1) .. f(N - 1) with the number as a constant
 template <int... I, class F>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }

@@ -41,6 +41,31 @@ struct Exp {
     }
 };
 
+// Values of two neighbouring tiles of sums, i and i + 1, of which lane group g = lane / 16 holds rows 4 g .. + 3: afterwards a lane has
+// eight rows that follow each other, 8 (g / 2) .. + 7 of tile i + g % 2; `lo` and `hi` are their halves.
+template <int N>
+__device__ __forceinline__ void pair_rows(uint32_t (&lo)[N], uint32_t (&hi)[N]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const auto p = __builtin_amdgcn_permlane16_swap(lo[i], hi[i], false, false);
+        lo[i] = p[0];
+        hi[i] = p[1];
+    }
+#endif
+}
+__device__ __forceinline__ int paired_row(int lane) { return 16 * (lane >> 4 & 1) + 8 * (lane >> 5); }
+
+// the largest, the sum of a value over the four lane groups that hold the same column: the same in all of them
+__device__ __forceinline__ float groups_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float groups_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
 // ---- epilogues of the logits' tiles (m: words, n: rows of features) ----------------------------------------------------------
 
 // A column's target relative to the tile, clipped to -1 and what a tile cannot hold.
@@ -95,13 +120,13 @@ struct ScoreEpilogue {
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
+            m = groups_max(m);
             const Exp<EXACT> power(m > -INFINITY ? m : 0.f);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s += power(acc[i][j][r]);
-            join(m, s, __shfl_xor(m, 16), __shfl_xor(s, 16));
-            join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
+            s = groups_sum(s);
             if (lane < 16) join_lds[(wave / WN) * BN + col] = make_float2(m, s);
         }
         __syncthreads();
@@ -139,7 +164,8 @@ struct GradEpilogue {
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int,
                                            void *) const {
         const int first = wm + 4 * (lane >> 4);
-        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first, room = (int)(stride - m0 < BM ? stride - m0 : BM) - first;
+        const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;
+        const int out0 = wm + paired_row(lane), room = (int)(stride - m0 < BM ? stride - m0 : BM) - out0;
         const bool whole = words - m0 >= BM;                                 // all but the vocabulary's last tile
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -150,41 +176,49 @@ struct GradEpilogue {
             const Exp<PLANES == 3> power(counted ? (st.target[j] < vocab ? st.top[j] : NAN) : INFINITY);
             const float g = counted ? st.g[j] : 0.f;
             const bool any = __builtin_amdgcn_ballot_w64(here || !counted) != 0;
-            T *to = d + n * stride + m0 + first;
+            T *to = d + n * stride + m0 + out0;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                float v[4];
+            for (int i = 0; i < TM; i += 2) {
+                uint32_t out[2][PLANES][2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = power(acc[i][j][r]);
-                if (any) {
+                for (int h = 0; h < 2; ++h) {
+                    float v[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (i * 16 + r == t) v[r] -= 1.f;
-                        if (!counted) v[r] = 0.f;
-                    }
-                }
+                    for (int r = 0; r < 4; ++r) v[r] = power(acc[i + h][j][r]);
+                    if (any) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    v[r] *= g;
-                    if (!whole && i * 16 + r >= left) v[r] = 0.f;
-                }
-                union { T t[4]; uint2 u; } out[PLANES];
-#pragma unroll
-                for (int q = 0; q < PLANES; ++q) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if constexpr (PLANES == 1) out[q].t[r] = (T)v[r];
-                        else {   // the upper half of the bits, then of what is left
-                            const uint32_t b = __float_as_uint(v[r]) & 0xffff0000u;
-                            out[q].t[r] = __builtin_bit_cast(T, (uint16_t)(b >> 16));
-                            const float rest = v[r] - __uint_as_float(b);
-                            v[r] = (b & 0x7f800000u) == 0x7f800000u ? 0.f : rest;
+                        for (int r = 0; r < 4; ++r) {
+                            if ((i + h) * 16 + r == t) v[r] -= 1.f;
+                            if (!counted) v[r] = 0.f;
                         }
                     }
-                }
-                if (n < rows && i * 16 < room) {   // (the stride is a multiple of 8)
 #pragma unroll
-                    for (int q = 0; q < PLANES; ++q) *reinterpret_cast<uint2 *>(to + i * 16 + q * plane) = out[q].u;
+                    for (int r = 0; r < 4; ++r) {
+                        v[r] *= g;
+                        if (!whole && (i + h) * 16 + r >= left) v[r] = 0.f;
+                    }
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) {
+                        union { T t[4]; uint32_t u[2]; } o;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            if constexpr (PLANES == 1) o.t[r] = (T)v[r];
+                            else {   // the upper half of the bits, then of what is left
+                                const uint32_t b = __float_as_uint(v[r]) & 0xffff0000u;
+                                o.t[r] = __builtin_bit_cast(T, (uint16_t)(b >> 16));
+                                const float rest = v[r] - __uint_as_float(b);
+                                v[r] = (b & 0x7f800000u) == 0x7f800000u ? 0.f : rest;
+                            }
+                        }
+                        out[h][q][0] = o.u[0];
+                        out[h][q][1] = o.u[1];
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) {
+                    pair_rows(out[0][q], out[1][q]);
+                    if (n < rows && i * 16 < room)   // (the stride is a multiple of 8)
+                        *reinterpret_cast<u32x4 *>(to + i * 16 + q * plane) = u32x4{out[0][q][0], out[0][q][1], out[1][q][0], out[1][q][1]};
                 }
             }
         }
@@ -206,13 +240,18 @@ struct SumEpilogue {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + (lane & 15);
-            if (n >= rows) continue;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int64_t m = m0 + wm + i * 16 + 4 * (lane >> 4);
-                if (m >= cols) continue;   // cols is a multiple of 8
-                f32x4 *p = reinterpret_cast<f32x4 *>(to + n * stride + m);
-                *p = add ? *p + acc[i][j] : acc[i][j];
+            for (int i = 0; i < TM; i += 2) {
+                uint32_t v[2][4];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r / 4][r % 4] = __float_as_uint(acc[i + r / 4][j][r % 4]);
+                pair_rows(v[0], v[1]);
+                const int64_t m = m0 + wm + i * 16 + paired_row(lane);
+                if (n >= rows || m >= cols) continue;   // cols is a multiple of 8
+                f32x8 *p = reinterpret_cast<f32x8 *>(to + n * stride + m), u;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) u[r] = __uint_as_float(v[r / 4][r % 4]);
+                *p = add ? *p + u : u;
             }
         }
     }
@@ -229,25 +268,26 @@ struct StoreEpilogue {
     template <int BM, int BN, int WM, int WN, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
         const float down = scale ? 1.f / *scale : 1.f;
-        const bool whole = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
+        const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + (lane & 15);
-            if (n >= rows) continue;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int64_t m = m0 + wm + i * 16 + 4 * (lane >> 4);
-                if (m >= cols) continue;
+            for (int i = 0; i < TM; i += 2) {
+                constexpr int DWORDS = sizeof(T);        // of four values
+                union Four { T t[4]; uint32_t u[DWORDS]; } v[2];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r / 4].t[r % 4] = (T)(acc[i + r / 4][j][r % 4] * down);
+                pair_rows(v[0].u, v[1].u);
+                const int64_t m = m0 + wm + i * 16 + paired_row(lane);
+                if (n >= rows || m >= cols) continue;
                 T *to = out + n * cols + m;
-                if (whole) {
-                    struct alignas(4 * sizeof(T)) { T t[4]; } v;
+                struct alignas(16) Eight { Four f[2]; };
+                if (whole) *reinterpret_cast<Eight *>(to) = Eight{{v[0], v[1]}};
+                else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v.t[r] = (T)(acc[i][j][r] * down);
-                    *reinterpret_cast<decltype(v) *>(to) = v;
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (m + r < cols) to[r] = (T)(acc[i][j][r] * down);
+                    for (int r = 0; r < 8; ++r)
+                        if (m + r < cols) to[r] = v[r / 4].t[r % 4];
                 }
             }
         }
@@ -256,8 +296,33 @@ struct StoreEpilogue {
 
 // ---- small kernels ---------------------------------------------------------------------------------------------------------
 
-// Rows of src as aligned rows of 16-bit planes, zeros up to the planes' stride.  Binary32 becomes three planes of bfloat16
-// (cut off, so that their sum is exact; an infinity or NaN stays whole in the first).  `mask`: rows without a target become zeros,
+// The bits of eight values as operands of the matrix cores: one of 16 bits, or three of bfloat16 whose sum is the value of 32
+// (cut off, so that it is exact; an infinity or NaN stays whole in the first).
+template <class T>
+__device__ __forceinline__ void planes_of(const Raw8<T> &r, u32x4 (&o)[sizeof(T) == 4 ? 3 : 1]) {
+    if constexpr (sizeof(T) == 2) o[0] = u32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+    else {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.v[i]);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            uint32_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t all = __float_as_uint(v[i]), b = all & 0xffff0000u;
+                const bool odd = (b & 0x7f800000u) == 0x7f800000u;
+                // a NaN whose upper half would read as an infinity keeps a bit of it
+                h[i] = odd && (all & 0x7fffffu) ? b | 0x400000u : b;
+                v[i] = odd ? 0.f : v[i] - __uint_as_float(b);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[q][i] = __builtin_amdgcn_perm(h[2 * i + 1], h[2 * i], 0x07060302);
+        }
+    }
+}
+
+// Rows of src as aligned rows of 16-bit planes, zeros up to the planes' stride.  `mask`: rows without a target become zeros,
 // so that nothing in them, NaN included, reaches a product.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, void *dst,
@@ -265,28 +330,11 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_str
     const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
     if (c >= stride) return;
     for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
-        f32x8 v;
-        v = load8(src + row * src_stride + c, mask.p && mask.at(row) < 0 ? 0 : cols - c);
-        if constexpr (sizeof(T) == 2) store8(static_cast<T *>(dst) + row * stride + c, 8, v);
-        else {
+        u32x4 o[sizeof(T) == 4 ? 3 : 1];
+        planes_of<T>(load_raw8(src + row * src_stride + c, mask.p && mask.at(row) < 0 ? 0 : cols - c), o);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
-                uint32_t h[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t b = __float_as_uint(v[i]) & 0xffff0000u;
-                    const bool odd = (b & 0x7f800000u) == 0x7f800000u;
-                    // a NaN whose upper half would read as an infinity keeps a bit of it
-                    h[i] = (odd && (__float_as_uint(v[i]) & 0x7fffffu) ? b | 0x400000u : b) >> 16;
-                    const float rest = v[i] - __uint_as_float(b);
-                    v[i] = odd ? 0.f : rest;
-                }
-                u32x4 o;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = h[2 * i] | h[2 * i + 1] << 16;
-                *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(dst) + q * plane + row * stride + c) = o;
-            }
-        }
+        for (int q = 0; q < (int)(sizeof(o) / sizeof(o[0])); ++q)
+            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(dst) + q * plane + row * stride + c) = o[q];
     }
 }
 
@@ -374,127 +422,115 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
 
 // ---- few rows --------------------------------------------------------------------------------------------------------------
 
-// Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time,
-// any alignment; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its words; a workgroup leaves one
-// partial result per row.
-template <class T, int NT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target, int64_t rows,
-                                                        int64_t vocab, int64_t cols, float2 *partial, int64_t rows_pad, float *at) {
+template <class T>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (std::is_same<T, bf16>::value)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+
+// Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time, any
+// alignment, a batch ahead of its use; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its
+// words; a workgroup leaves one partial result per row.
+constexpr int kFewWaves = 8;
+
+template <class T, int NT>
+__global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target,
+                                                                   int64_t rows, int64_t vocab, int64_t cols, float2 *partial,
+                                                                   int64_t rows_pad, float *at) {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int PLANES = F32 ? 3 : 1;
+    constexpr int PLANES = F32 ? 3 : 1, BATCH = F32 ? 4 : 8;
     using M = typename std::conditional<F32, bf16, T>::type;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
-    const int64_t pad = (cols + 31) / 32 * 32, row_bytes = pad * 2 + 16, plane_bytes = rows * row_bytes;
+    const int pad = (int)((cols + 31) / 32 * 32), row_bytes = pad * 2 + 16, plane_bytes = (int)rows * row_bytes;
+    const int64_t tiles = (vocab + 15) / 16;
+    int64_t tile = (int64_t)blockIdx.x * kFewWaves + wave;
+    int k = 0;                           // first column of the batch to come
+    Raw8<T> raw[BATCH];
+    auto ask = [&] {
+        const int64_t v = tile * 16 + (lane & 15);
+        const T *from = w + (v < vocab ? v : vocab - 1) * w_stride + k + grp * 8;
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            if (k + 32 * u + 32 <= cols) raw[u] = load_raw8(from + 32 * u, 8);
+            else raw[u] = load_raw8(from + 32 * u, cols - k - 32 * u - grp * 8);   // (none: zeros)
+        }
+    };
+    if (tile < tiles) ask();
     // features: 16 bytes apart from a multiple of 128, so that eight rows lie in different banks
-    for (int64_t i = threadIdx.x; i < rows * (pad / 8); i += WAVES * 64) {
-        const int64_t n = i / (pad / 8), c = (i - n * (pad / 8)) * 8;
-        f32x8 v;
-        v = load8(x + n * x_stride + c, cols - c);
+    for (int c = (threadIdx.x & 127) * 8; c < pad; c += 1024) {
+        for (int n = threadIdx.x >> 7; n < rows; n += kFewWaves / 2 * BATCH) {
+            Raw8<T> f[BATCH];
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q) {
-            u32x4 o;
-            if constexpr (!F32) {
-                union { T t[8]; u32x4 u; } k;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) k.t[e] = (T)v[e];
-                o = k.u;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t two = 0;
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        const uint32_t b = __float_as_uint(v[2 * e + f]) & 0xffff0000u;
-                        const bool odd = (b & 0x7f800000u) == 0x7f800000u;
-                        two |= ((odd && (__float_as_uint(v[2 * e + f]) & 0x7fffffu) ? b | 0x400000u : b) >> 16) << (16 * f);
-                        const float rest = v[2 * e + f] - __uint_as_float(b);
-                        v[2 * e + f] = odd ? 0.f : rest;
-                    }
-                    o[e] = two;
-                }
+            for (int i = 0; i < BATCH; ++i) {
+                const int m = n + i * (kFewWaves / 2);
+                f[i] = load_raw8(x + (int64_t)(m < rows ? m : n) * x_stride + c, cols - c);
             }
-            *reinterpret_cast<u32x4 *>(few_lds + q * plane_bytes + n * row_bytes + c * 2) = o;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const int m = n + i * (kFewWaves / 2);
+                u32x4 o[PLANES];
+                planes_of<T>(f[i], o);
+                if (m < rows)
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) *reinterpret_cast<u32x4 *>(few_lds + q * plane_bytes + m * row_bytes + c * 2) = o[q];
+            }
         }
     }
     __syncthreads();
     float m[NT], s[NT];
     int64_t t[NT];
     const char *mine[NT];   // a lane beyond the last row takes the last one: its column is never used
+    f32x4 acc[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         m[j] = -INFINITY; s[j] = 0.f;
         const int64_t n = j * 16 + (lane & 15);
         t[j] = n < rows ? target.at(n) : -1;
-        mine[j] = few_lds + (n < rows ? n : rows - 1) * row_bytes + grp * 16;
+        mine[j] = few_lds + (int)(n < rows ? n : rows - 1) * row_bytes + grp * 16;
+        acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int64_t tiles = (vocab + 15) / 16;
-    for (int64_t tile = (int64_t)blockIdx.x * WAVES + wave; tile < tiles; tile += (int64_t)gridDim.x * WAVES) {
-        const int64_t v0 = tile * 16, v = v0 + (lane & 15);
-        const T *row = w + (v < vocab ? v : vocab - 1) * w_stride + grp * 8;
-        f32x4 acc[NT];
+    while (tile < tiles) {
+        const int64_t v0 = tile * 16 + 4 * grp;
+        const int k_now = k;
+        Raw8<T> now[BATCH];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto step = [&](int64_t k, int64_t n) {
+        for (int u = 0; u < BATCH; ++u) now[u] = raw[u];
+        k += 32 * BATCH;
+        const bool done = k >= pad;
+        if (done) { k = 0; tile += (int64_t)gridDim.x * kFewWaves; }
+        if (tile < tiles) ask();
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            if (k_now + 32 * u >= pad) break;
             u32x4 a[PLANES];
-            if constexpr (!F32) {
-                if (n >= 8) {
-                    const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + k);
-                    a[0] = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
-                } else {
-                    f32x8 f;
-                    f = load8(row + k, n);
-                    union { T t[8]; u32x4 u; } o;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o.t[e] = (T)f[e];
-                    a[0] = o.u;
-                }
-            } else {
-                f32x8 f;
-                f = load8(row + k, n);
-#pragma unroll
-                for (int q = 0; q < 3; ++q)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t two = 0;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t b = __float_as_uint(f[2 * e + h]) & 0xffff0000u;
-                            const bool odd = (b & 0x7f800000u) == 0x7f800000u;
-                            two |= ((odd && (__float_as_uint(f[2 * e + h]) & 0x7fffffu) ? b | 0x400000u : b) >> 16) << (16 * h);
-                            const float rest = f[2 * e + h] - __uint_as_float(b);
-                            f[2 * e + h] = odd ? 0.f : rest;
-                        }
-                        a[q][e] = two;
-                    }
-            }
+            planes_of<T>(now[u], a);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 u32x4 b[PLANES];
 #pragma unroll
-                for (int q = 0; q < PLANES; ++q) b[q] = *reinterpret_cast<const u32x4 *>(mine[j] + q * plane_bytes + k * 2);
-                if constexpr (!F32) acc[j] = Mfma<M>::run(a[0], b[0], acc[j]);
+                for (int q = 0; q < PLANES; ++q) b[q] = *reinterpret_cast<const u32x4 *>(mine[j] + q * plane_bytes + (k_now + 32 * u) * 2);
+                if constexpr (!F32) acc[j] = mfma16<M>(a[0], b[0], acc[j]);
                 else {
 #pragma unroll
-                    for (int q = 0; q < 6; ++q) acc[j] = Mfma<M>::run(a[(0x001012 >> (4 * q)) & 15], b[(0x010210 >> (4 * q)) & 15], acc[j]);
+                    for (int q = 0; q < 6; ++q) acc[j] = mfma16<M>(a[(0x001012 >> (4 * q)) & 15], b[(0x010210 >> (4 * q)) & 15], acc[j]);
                 }
             }
-        };
-        int64_t k = 0;
-        for (; k + 256 <= cols; k += 256) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) step(k + 32 * u, 8);
         }
-        for (; k + 32 <= cols; k += 32) step(k, 8);
-        if (k < cols) step(k, cols - k - grp * 8);
+        if (!done) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int64_t lane_v = v0 + 4 * grp;
             float top = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (lane_v + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
-                if (lane_v + r >= vocab) acc[j][r] = -INFINITY;
+                if (v0 + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
+                if (v0 + r >= vocab) acc[j][r] = -INFINITY;
                 top = fmaxf(top, acc[j][r]);
             }
             const Exp<F32> power(top > -INFINITY ? top : 0.f);
@@ -502,6 +538,7 @@ __global__ __launch_bounds__(WAVES * 64) void score_few_kernel(const T *x, int64
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum += power(acc[j][r]);
             join(m[j], s[j], top, sum);
+            acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
     __syncthreads();   // the features have been read: LDS is free
@@ -516,7 +553,7 @@ __global__ __launch_bounds__(WAVES * 64) void score_few_kernel(const T *x, int64
     if (threadIdx.x < NT * 16 && threadIdx.x < rows) {
         float2 p = lds[threadIdx.x];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) join(p.x, p.y, lds[k * NT * 16 + threadIdx.x].x, lds[k * NT * 16 + threadIdx.x].y);
+        for (int i = 1; i < kFewWaves; ++i) join(p.x, p.y, lds[i * NT * 16 + threadIdx.x].x, lds[i * NT * 16 + threadIdx.x].y);
         partial[(int64_t)blockIdx.x * rows_pad + threadIdx.x] = p;
     }
 }

@@ -266,21 +266,33 @@ int check_xent(const char *who, Xent &c) {
     return SABER_OK;
 }
 
-// words of a piece: as even as the limit allows, whole tiles (and at most 2^20: offsets within a tile are 32 bits)
-int64_t piece_words(int64_t vocab, int64_t most) {
+// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself.
+bool large_tiles(int64_t m, int64_t n, int64_t splits) { return parts_of(m, 256) * parts_of(n, 256) * splits >= kCus; }
+
+// Words of a piece, at most `most` (and 2^20: offsets within a tile are 32 bits), whole tiles.  Either all pieces are even, or all but
+// the last fill the CUs with whole rounds of tiles: of d (words x rows), and of the weight's gradient (words x columns), whichever
+// takes fewer rounds in all.  (4,096 rows of 1,024 columns, 100,000 words: 36 rounds even, 32 the other way, 3.4 -> TODO ms.)
+int64_t piece_words(int64_t vocab, int64_t most, int64_t rows, int64_t cols) {
     if (most > (int64_t)1 << 20) most = (int64_t)1 << 20;
     most = most / 256 * 256;
     if (most < 256) most = 256;
-    const int64_t pieces = parts_of(vocab, most);
-    const int64_t words = up(parts_of(vocab, pieces), 256);
-    return words < up(vocab, 8) ? words : up(vocab, 8);
+    if (vocab <= most) return up(vocab, 8);
+    const int64_t row_tiles = parts_of(rows, 256), col_tiles = parts_of(cols, 256);
+    auto rounds = [&](int64_t words) {
+        int64_t sum = 0;
+        for (int64_t v0 = 0; v0 < vocab; v0 += words) {
+            const int64_t tiles = parts_of(vocab - v0 < words ? vocab - v0 : words, 256);
+            sum += parts_of(tiles * row_tiles, kCus) + parts_of(tiles * col_tiles, kCus);
+        }
+        return sum;
+    };
+    const int64_t even = up(parts_of(vocab, parts_of(vocab, most)), 256);
+    const int64_t round = row_tiles <= kCus ? kCus / row_tiles * 256 : 256, filled = most / round * round;
+    return filled > 0 && rounds(filled) < rounds(even) ? filled : even;
 }
 
 int64_t few_lds(const Xent &c) { return c.rows * (up(c.cols, 32) * 2 + 16) * c.planes; }
 bool few(const Xent &c) { return c.rows <= kFewRows && few_lds(c) <= kFewLds; }
-
-// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself.
-bool large_tiles(int64_t m, int64_t n, int64_t splits) { return parts_of(m, 256) * parts_of(n, 256) * splits >= kCus; }
 
 struct Carve {   // a work space handed out piece by piece; base null: only counted
     char *base; int64_t at = 0;
@@ -291,18 +303,15 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; int few_waves; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
     if (few(c)) {
-        // Features that take most of a CU's LDS leave room for one workgroup, which then has eight wavefronts (61 rows of 777 of
-        // 16 bits, 30,011 words: 47 us with four, TODO with eight)
-        f.few_waves = few_lds(c) > 64 * 1024 ? 8 : 4;
-        const int64_t groups = parts_of(parts_of(c.vocab, 16), f.few_waves), most = f.few_waves == 8 ? kCus : 8 * kCus;
+        const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), most = few_lds(c) > 64 * 1024 ? kCus : 4 * kCus;
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
-        f.piece = c.pack_w ? piece_words(c.vocab, kPieceBytes / (c.cols_pad * 2 * c.planes)) : c.vocab;
+        f.piece = c.pack_w ? piece_words(c.vocab, kPieceBytes / (c.cols_pad * 2 * c.planes), c.rows, c.cols) : c.vocab;
         f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
         if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
         if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * c.planes);
@@ -316,7 +325,7 @@ struct BackwardSpace { float *scale; uint16_t *x, *w, *d; float *sums; int64_t p
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
     const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceBytes / (row * 2 * c.planes), most_w = kPieceBytes / (c.cols_pad * 2 * c.planes);
-    b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w);
+    b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w, row, c.cols);
     const int64_t steps = parts_of(b.piece, kStep) * (c.planes == 3 ? 6 : 1);
     // workgroups for every CU: the products over the vocabulary have few tiles, so their steps are shared out
     const int64_t large = parts_of(c.cols_pad, 256) * parts_of(row, 256), small = parts_of(c.cols_pad, 128) * parts_of(row, 128);
@@ -362,18 +371,14 @@ int check_targets(const char *who, const void *target, int target64) {
     return check_pointer(who, "target", target, target64 ? 8 : 4);
 }
 
-template <class T, int NT, int WAVES>
-int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
-    const int64_t least = WAVES * NT * 128, lds = few_lds(c) > least ? few_lds(c) : least;   // the wavefronts' results at the end
-    const auto kernel = score_few_kernel<T, NT, WAVES>;
-    if (lds > 64 * 1024) OPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<(unsigned)f.few_grid, WAVES * 64, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
-    OPS_HIP(hipGetLastError());
-    return SABER_OK;
-}
 template <class T, int NT>
 int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
-    return f.few_waves == 8 ? launch_few<T, NT, 8>(c, f, t, st) : launch_few<T, NT, 4>(c, f, t, st);
+    const int64_t least = kFewWaves * NT * 128, lds = few_lds(c) > least ? few_lds(c) : least;   // the wavefronts' results at the end
+    const auto kernel = score_few_kernel<T, NT>;
+    if (lds > 64 * 1024) OPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(unsigned)f.few_grid, kFewWaves * 64, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
 }
 
 }  // namespace
