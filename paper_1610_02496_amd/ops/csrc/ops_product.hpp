@@ -9,8 +9,10 @@
 //              a lane's 8 values of k come through two transposing reads of 4 rows x 16 columns each.
 // Rows and columns outside the operands are read as zeros (the bounds of the buffer descriptors), so no tile reads out of range.
 //
-// Operands of binary32 come as three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each); the six
-// products of planes whose weights exceed 2^-24 are added as further steps along k ("segments"), smallest first.
+// Operands of binary32 come as planes, and the products of planes that matter are added as further steps along k ("segments"):
+//   three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each), six segments, any range of values;
+//   two planes of binary16, x = x1 + x2 to 2^-24, three segments, for operands whose rows were brought to one magnitude.
+// What is left out is below 2^-23 of the product of two magnitudes.
 #pragma once
 #include <type_traits>
 #include <utility>
@@ -37,14 +39,14 @@ struct Operand {
 struct Product {
     Operand a, b;
     uint32_t k;          // extent of k; where k is fastest the stored rows go on to the next multiple of 8, with zeros in one operand
-    int segments;        // 1, or 6 for planes
+    int segments;        // 1, or 6 or 3 for planes
     int tiles_m, tiles_n;
     int splits;          // parts of the steps along k, each a workgroup of its own
 };
 
-// planes of the six segments: (0,0) last, as it is the largest
-__device__ __forceinline__ int plane_a(int seg, int segments) { return segments == 1 ? 0 : (0x001012 >> (4 * seg)) & 15; }
-__device__ __forceinline__ int plane_b(int seg, int segments) { return segments == 1 ? 0 : (0x010210 >> (4 * seg)) & 15; }
+// planes that a segment multiplies: the largest two last
+__device__ __forceinline__ int plane_a(int seg, int segments) { return ((segments == 6 ? 0x001012 : segments == 3 ? 0x001 : 0) >> (4 * seg)) & 15; }
+__device__ __forceinline__ int plane_b(int seg, int segments) { return ((segments == 6 ? 0x010210 : segments == 3 ? 0x010 : 0) >> (4 * seg)) & 15; }
 
 // f(0), f(1) .. f(N - 1) with the number as a constant
 template <int... I, class F>

@@ -30,14 +30,20 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
 }
 
 // exp(l - m) by the hardware's 2^x.  The difference is rounded before it is scaled, so logits of any size keep their precision; the
-// scaling costs 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which a result of 16 bits is stored.  EXACT: features of binary32.
+// scaling costs 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which a result of 16 bits is stored.  EXACT, for features of
+// binary32: what the scaling's rounding left is put back, exp(d) = 2^h (1 + ln 2 (d log2 e - h)), to about an ulp (a call of expf, of
+// whose range little is needed, took a third of the logits' kernel).
 template <bool EXACT>
 struct Exp {
     float m;
     __device__ __forceinline__ explicit Exp(float top) : m(top) {}
     __device__ __forceinline__ float operator()(float l) const {
-        if constexpr (EXACT) return expf(l - m);
-        else return __builtin_amdgcn_exp2f((l - m) * kLog2e);
+        const float d = l - m, h = d * kLog2e, p = __builtin_amdgcn_exp2f(h);
+        if constexpr (!EXACT) return p;
+        else {
+            const float rest = fmaf(d, 1.92596299e-8f, fmaf(d, kLog2e, -h));   // log2(e) is kLog2e + 1.926e-8
+            return h > -200.f ? fmaf(p, rest * 0.693147181f, p) : p;           // (below: 0, of an infinity as well)
+        }
     }
 };
 
@@ -68,10 +74,26 @@ __device__ __forceinline__ float groups_sum(float v) {
 
 // ---- epilogues of the logits' tiles (m: words, n: rows of features) ----------------------------------------------------------
 
+// Rows of binary32 are multiplied after they were brought to one magnitude: the sums' powers of two, of the words and of the rows.
+struct Powers { const int *words, *rows; };
+
 // A column's target relative to the tile, clipped to -1 and what a tile cannot hold.
 __device__ __forceinline__ int within_tile(int64_t target, int64_t first_word) {
     const int64_t t = target - first_word;
     return t < 0 ? -1 : t > 4096 ? 4096 : (int)t;
+}
+
+// sums of this lane's words from `words` on, of which `left` exist
+template <int TM, int TN>
+__device__ __forceinline__ void scale_sums(f32x4 (&acc)[TM][TN], const int (&rows)[TN], const int *words, int left) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int w = i * 16 + r < left ? words[i * 16 + r] : 0;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j][r] = __builtin_amdgcn_ldexpf(acc[i][j][r], w + rows[j]);
+        }
 }
 
 template <bool EXACT>
@@ -81,12 +103,16 @@ struct ScoreEpilogue {
     Targets target;
     int64_t rows, words, word0;          // rows; words of this piece and the first one's number
     int tile0;
+    Powers powers;                       // EXACT
 
-    template <int TN> struct State { int64_t target[TN]; };
+    template <int TN> struct State { int64_t target[TN]; int power[EXACT ? TN : 1]; };
     template <int TN>
     __device__ __forceinline__ void prepare(State<TN> &s, int64_t n) const {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) s.target[j] = n + j * 16 < rows ? target.at(n + j * 16) : -1;
+        for (int j = 0; j < TN; ++j) {
+            s.target[j] = n + j * 16 < rows ? target.at(n + j * 16) : -1;
+            if constexpr (EXACT) s.power[j] = n + j * 16 < rows ? powers.rows[n + j * 16] : 0;
+        }
     }
     template <int BM, int BN, int WM, int WN, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int wave,
@@ -94,6 +120,7 @@ struct ScoreEpilogue {
         float2 *join_lds = static_cast<float2 *>(lds);
         const int first = wm + 4 * (lane >> 4);
         const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;   // words of this lane's rows that exist
+        if constexpr (EXACT) scale_sums(acc, st.power, powers.words + m0 + first, left);
         if (words - m0 < BM) {   // (the vocabulary's last tile alone)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
@@ -144,11 +171,12 @@ struct ScoreEpilogue {
 template <class T, int PLANES>
 struct GradEpilogue {
     T *d; int64_t stride, plane;
-    const float *lse, *dloss, *scale;    // scale: power of two that d is multiplied with, or null
+    const float *lse, *dloss, *scale;    // scale[0]: what dloss is multiplied with, or null
     Targets target;
     int64_t rows, words, word0, vocab;
+    Powers powers;                       // three planes
 
-    template <int TN> struct State { int64_t target[TN]; float top[TN], g[TN]; };
+    template <int TN> struct State { int64_t target[TN]; float top[TN], g[TN]; int power[PLANES == 3 ? TN : 1]; };
     template <int TN>
     __device__ __forceinline__ void prepare(State<TN> &s, int64_t n) const {
         const float up = scale ? *scale : 1.f;
@@ -158,6 +186,7 @@ struct GradEpilogue {
             s.target[j] = row ? target.at(n + j * 16) : -1;
             s.top[j] = row ? lse[n + j * 16] : 0.f;
             s.g[j] = row ? dloss[n + j * 16] * up : 0.f;
+            if constexpr (PLANES == 3) s.power[j] = row ? powers.rows[n + j * 16] : 0;
         }
     }
     template <int BM, int BN, int WM, int WN, int TM, int TN>
@@ -167,6 +196,7 @@ struct GradEpilogue {
         const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;
         const int out0 = wm + paired_row(lane), room = (int)(stride - m0 < BM ? stride - m0 : BM) - out0;
         const bool whole = words - m0 >= BM;                                 // all but the vocabulary's last tile
+        if constexpr (PLANES == 3) scale_sums(acc, st.power, powers.words + m0 + first, left);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + (lane & 15);
@@ -267,7 +297,7 @@ struct StoreEpilogue {
     template <int TN> __device__ __forceinline__ void prepare(State<TN> &, int64_t) const {}
     template <int BM, int BN, int WM, int WN, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
-        const float down = scale ? 1.f / *scale : 1.f;
+        const float down = scale ? scale[1] : 1.f;
         const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -322,19 +352,68 @@ __device__ __forceinline__ void planes_of(const Raw8<T> &r, u32x4 (&o)[sizeof(T)
     }
 }
 
-// Rows of src as aligned rows of 16-bit planes, zeros up to the planes' stride.  `mask`: rows without a target become zeros,
+// Rows of 16-bit elements as aligned rows, zeros up to their stride.  `mask`: rows without a target become zeros,
 // so that nothing in them, NaN included, reaches a product.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, void *dst,
-                                                   int64_t stride, int64_t plane, Targets mask) {
+__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride,
+                                                   Targets mask) {
     const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
     if (c >= stride) return;
     for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
-        u32x4 o[sizeof(T) == 4 ? 3 : 1];
+        u32x4 o[1];
         planes_of<T>(load_raw8(src + row * src_stride + c, mask.p && mask.at(row) < 0 ? 0 : cols - c), o);
+        *reinterpret_cast<u32x4 *>(dst + row * stride + c) = o[0];
+    }
+}
+
+// The same for binary32, a row per wavefront, with a second form for the logits: the row times the power of two that brings its largest
+// finite value to 2^14 .. 2^15, in two planes of binary16 (x = x1 + x2 to 2^-24 of it, and to 2^-40 of the row's largest); the
+// power that undoes it goes to `powers`.  Either form may be left out.
+__global__ __launch_bounds__(256) void pack32_kernel(const float *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride,
+                                                     int64_t plane, uint16_t *even, int *powers, Targets mask) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
+        const float *from = src + row * src_stride;
+        const int64_t have = mask.p && mask.at(row) < 0 ? 0 : cols;
+        float up = 1.f;
+        if (even) {
+            uint32_t top = 0;
+            for (int64_t c = lane * 8; c < stride; c += 512) {
+                const Raw8<f32> r = load_raw8(from + c, have - c);
 #pragma unroll
-        for (int q = 0; q < (int)(sizeof(o) / sizeof(o[0])); ++q)
-            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(dst) + q * plane + row * stride + c) = o[q];
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t b = r.v[i] & 0x7fffffffu;
+                    top = max(top, b < 0x7f800000u ? b : 0u);
+                }
+            }
+            top = row_max(top);
+            top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
+                      max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
+            int e = 14 - ((int)(top >> 23) - 127);         // (kept within the normal numbers)
+            e = top == 0 ? 0 : e > 126 ? 126 : e;
+            up = __uint_as_float((uint32_t)(e + 127) << 23);
+            if (lane == 0) powers[row] = -e;
+        }
+        for (int64_t c = lane * 8; c < stride; c += 512) {
+            const Raw8<f32> r = load_raw8(from + c, have - c);
+            if (dst) {
+                u32x4 o[3];
+                planes_of<f32>(r, o);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(dst + q * plane + row * stride + c) = o[q];
+            }
+            if (even) {
+                union { f16 t[8]; u32x4 u; } hi, lo;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = __uint_as_float(r.v[i]) * up;
+                    hi.t[i] = (f16)v;
+                    lo.t[i] = fabsf(v) < INFINITY ? (f16)(v - (float)hi.t[i]) : (f16)0.f;
+                }
+                *reinterpret_cast<u32x4 *>(even + row * stride + c) = hi.u;
+                *reinterpret_cast<u32x4 *>(even + plane + row * stride + c) = lo.u;
+            }
+        }
     }
 }
 
@@ -376,9 +455,12 @@ __global__ __launch_bounds__(1024) void score_join_kernel(const float2 *partial,
     }
 }
 
-// The power of two that brings the largest |dloss| to 2^14 .. 2^15: d of 16-bit floats, |d| <= |dloss|, then neither overflows nor
-// loses bits until it is 2^-29 of the largest.  1 where there is nothing to scale or the largest is not finite.
-__global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Targets target, int64_t rows, float *scale) {
+// d is rounded to the features' type as (p - [v = t]) dloss_n / top * to, where top is the largest |dloss|, and its products are scaled
+// back in binary32: scale[0] = to / top, scale[1] = top / to.  With one dloss for all rows (a mean) that factor is exactly `to`, a power of
+// two: neither the roundings of dloss itself nor, near a target, that of 1 - p then stand in every value (with dloss rounded along,
+// the weight's gradient was up to 1.5 times as far from the exact one).  to is 2^14 for binary16, of which |d| <= to neither overflows
+// nor loses bits until it is 2^-28 of it.  Both are 1 where the largest is 0 or not finite.
+__global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Targets target, int64_t rows, float to, float *scale) {
     __shared__ uint32_t lds[16];
     uint32_t top = 0;
     for (int64_t n = threadIdx.x; n < rows; n += 1024)
@@ -388,10 +470,10 @@ __global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Ta
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 16; ++i) top = max(top, lds[i]);
-        const int e = (int)(top >> 23);   // biased exponent; 2^(e-127) <= top < 2^(e-126)
-        int up = 127 + (141 - e);         // of the scale; kept within the normal numbers, as its inverse is
-        up = up < 1 ? 1 : up > 253 ? 253 : up;
-        *scale = top == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)up << 23);
+        const bool none = top == 0 || top >= 0x7f800000u;
+        const float g = fmaxf(__uint_as_float(top), 0x1p-100f);
+        scale[0] = none ? 1.f : to / g;
+        scale[1] = none ? 1.f : g / to;
     }
 }
 
@@ -401,7 +483,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
                                                   T *dx) {
     const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
     if (c >= cols) return;
-    const float down = scale ? 1.f / *scale : 1.f;
+    const float down = scale ? scale[1] : 1.f;
     for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
         f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         const float *from = sums + row * stride + c;   // (the stride is a multiple of 8)

@@ -235,7 +235,9 @@ namespace {
 
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewLds = 150 * 1024;
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of d, and of packed words, per piece
+// values of d, and of packed words, per piece: 256 MB of a 16-bit type, what the last-level cache holds; 768 MB of three planes (binary32
+// gains from fewer pieces: 2,048 rows of 512 columns, 60,000 words, TODO ms in one, TODO in three)
+constexpr int64_t kPieceValues = (int64_t)1 << 27;
 
 struct Xent {
     const void *x; int64_t x_stride;
@@ -266,8 +268,11 @@ int check_xent(const char *who, Xent &c) {
     return SABER_OK;
 }
 
-// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself.
-bool large_tiles(int64_t m, int64_t n, int64_t splits) { return parts_of(m, 256) * parts_of(n, 256) * splits >= kCus; }
+// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself, as two of the others
+// do that take about 5 / 8 of its time: whichever fills its rounds better.
+bool large_tiles(int64_t m, int64_t n) {
+    return 8 * parts_of(parts_of(m, 256) * parts_of(n, 256), kCus) <= 5 * parts_of(parts_of(m, 128) * parts_of(n, 128), 2 * kCus);
+}
 
 // Words of a piece, at most `most` (and 2^20: offsets within a tile are 32 bits), whole tiles.  Either all pieces are even, or all but
 // the last fill the CUs with whole rounds of tiles: of d (words x rows), and of the weight's gradient (words x columns), whichever
@@ -303,7 +308,7 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int64_t piece, parts, rows_pad, few_grid; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
@@ -311,48 +316,62 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
         const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), most = few_lds(c) > 64 * 1024 ? kCus : 4 * kCus;
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
-        f.piece = c.pack_w ? piece_words(c.vocab, kPieceBytes / (c.cols_pad * 2 * c.planes), c.rows, c.cols) : c.vocab;
+        f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / c.cols_pad, c.rows, c.cols) : c.vocab;
         f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
-        if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
-        if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * c.planes);
+        const int planes = c.planes == 3 ? 2 : 1;   // (the logits' form)
+        if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * planes);
+        if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * planes);
+        if (planes == 2) { f.x_powers = s.take<int>(c.rows); f.w_powers = s.take<int>(f.piece); }
     }
     f.partial = s.take<float2>(f.parts * f.rows_pad);
     f.at = s.take<float>(f.rows_pad);
     return f;
 }
 
-struct BackwardSpace { float *scale; uint16_t *x, *w, *d; float *sums; int64_t piece, stride; int splits; };
+struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *sums; int64_t piece, stride; int splits; bool dx_large; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
-    const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceBytes / (row * 2 * c.planes), most_w = kPieceBytes / (c.cols_pad * 2 * c.planes);
+    const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / row, most_w = kPieceValues / c.cols_pad;
     b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w, row, c.cols);
     const int64_t steps = parts_of(b.piece, kStep) * (c.planes == 3 ? 6 : 1);
-    // workgroups for every CU: the products over the vocabulary have few tiles, so their steps are shared out
+    // The features' gradient has few tiles and many steps, which are shared out until every CU has a workgroup: of large tiles, if
+    // each then still has 16 steps or more (eight of the smaller ones).
     const int64_t large = parts_of(c.cols_pad, 256) * parts_of(row, 256), small = parts_of(c.cols_pad, 128) * parts_of(row, 128);
-    int64_t splits = large >= 32 ? parts_of(kCus, large) : parts_of(2 * kCus, small);
-    if (splits > steps / 8) splits = steps / 8;
+    b.dx_large = parts_of(kCus, large) <= steps / 16;
+    int64_t splits = b.dx_large ? kCus / large : parts_of(2 * kCus, small);
+    if (!b.dx_large && splits > steps / 8) splits = steps / 8;
     if (splits < 1) splits = 1;
     b.splits = (int)splits;
-    b.scale = s.take<float>(1);
+    b.scale = s.take<float>(2);
     b.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
     if (c.pack_w) b.w = s.take<uint16_t>(b.piece * c.cols_pad * c.planes);
+    if (c.planes == 3) {   // the logits' form of both
+        b.x_even = s.take<uint16_t>(c.rows * c.cols_pad * 2);
+        b.w_even = s.take<uint16_t>(b.piece * c.cols_pad * 2);
+        b.x_powers = s.take<int>(c.rows);
+        b.w_powers = s.take<int>(b.piece);
+    }
     b.stride = up(b.piece, 64) | 64;
     b.d = s.take<uint16_t>(c.rows * b.stride * c.planes);
     b.sums = s.take<float>(b.splits * c.rows * c.cols_pad);
     return b;
 }
 
+// dst: the planes of the gradients' products (of 16-bit types the only form); even, powers: of the logits'
 template <class T>
-int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, int64_t plane, Targets mask, hipStream_t st) {
+int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, uint16_t *even, int *powers, int64_t plane, Targets mask, hipStream_t st) {
     const int64_t y = parts_of(rows, 4);
-    pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, plane, mask);
+    if constexpr (std::is_same<T, f32>::value)
+        pack32_kernel<<<(unsigned)(y < 16 * kCus ? y : 16 * kCus), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, plane, even, powers, mask);
+    else
+        pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, mask);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
 }
 
 template <class T, bool A_SLOW, bool B_SLOW, class E>
-int product(Operand a, Operand b, int64_t k, int planes, int splits, const E &e, hipStream_t st, bool large) {
-    Product p{a, b, (uint32_t)k, planes == 3 ? 6 : 1, 0, 0, splits};
+int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &e, hipStream_t st, bool large) {
+    Product p{a, b, (uint32_t)k, segments, 0, 0, splits};
     const int64_t tile = large ? 256 : 128;
     p.tiles_m = (int)parts_of(a.major, tile);
     p.tiles_n = (int)parts_of(b.major, tile);
@@ -364,8 +383,9 @@ int product(Operand a, Operand b, int64_t k, int planes, int splits, const E &e,
     return SABER_OK;
 }
 
-template <class T> struct MatrixType { using type = T; };
-template <> struct MatrixType<f32> { using type = bf16; };
+// of the operands: of the gradients' products, of the logits'
+template <class T> struct MatrixType { using type = T; using logits = T; };
+template <> struct MatrixType<f32> { using type = bf16; using logits = f16; };
 
 int check_targets(const char *who, const void *target, int target64) {
     return check_pointer(who, "target", target, target64 ? 8 : 4);
@@ -404,24 +424,26 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
     int64_t parts = 0;
     OPS_TRY(with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
-        using M = typename MatrixType<T>::type;
+        using M = typename MatrixType<T>::logits;
+        constexpr bool F32 = std::is_same<T, f32>::value;
         if (few(c)) {
             parts = f.parts;
             if (rows <= 16) return launch_few<T, 1>(c, f, t, st);
             if (rows <= 32) return launch_few<T, 2>(c, f, t, st);
             return launch_few<T, 4>(c, f, t, st);
         }
+        const Targets none{nullptr, 0};
         const int64_t plane_x = rows * c.cols_pad, plane_w = f.piece * c.cols_pad;
-        if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, f.x, plane_x, Targets{nullptr, 0}, st));
+        if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, F32 ? nullptr : f.x, F32 ? f.x : nullptr, f.x_powers, plane_x, none, st));
         const Operand ox = c.pack_x ? Operand{f.x, c.cols_pad, plane_x, rows} : Operand{x, x_stride, 0, rows};
-        const bool large = large_tiles(f.piece, rows, 1);
+        const bool large = large_tiles(f.piece, rows);
         for (int64_t v0 = 0; v0 < vocab; v0 += f.piece) {
             const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
-            if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, plane_w, Targets{nullptr, 0}, st));
+            if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, F32 ? nullptr : f.w, F32 ? f.w : nullptr, f.w_powers, plane_w, none, st));
             const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
-            const ScoreEpilogue<std::is_same<T, f32>::value> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts};
-            OPS_TRY((product<M, false, false>(ow, ox, cols, c.planes, 1, ep, st, large)));
+            const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, Powers{f.w_powers, f.x_powers}};
+            OPS_TRY((product<M, false, false>(ow, ox, cols, F32 ? 3 : 1, 1, ep, st, large)));
             parts += parts_of(words, large ? 256 : 128);
         }
         return SABER_OK;
@@ -456,13 +478,15 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
     return with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
         using M = typename MatrixType<T>::type;
-        constexpr int PLANES = std::is_same<T, f32>::value ? 3 : 1;
+        using L = typename MatrixType<T>::logits;
+        constexpr bool F32 = std::is_same<T, f32>::value;
+        constexpr int PLANES = F32 ? 3 : 1, SEGMENTS = F32 ? 6 : 1;
         const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.stride;
         const float *scale = nullptr;
         if (rows) {
-            OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, plane_x, t, st));
-            if (std::is_same<T, f16>::value) {
-                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, b.scale);
+            OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, b.x_even, b.x_powers, plane_x, t, st));
+            if (!F32) {   // (three planes keep all bits)
+                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, std::is_same<T, f16>::value ? 0x1p14f : 1.f, b.scale);
                 OPS_HIP(hipGetLastError());
                 scale = b.scale;
             }
@@ -472,21 +496,22 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
             T *dw = dweight ? static_cast<T *>(dweight) + v0 * cols : nullptr;
             if (rows) {
-                if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, plane_w, Targets{nullptr, 0}, st));
+                if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, b.w_even, b.w_powers, plane_w, Targets{nullptr, 0}, st));
                 const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
                 const Operand ox{b.x, c.cols_pad, plane_x, rows};
-                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab};
-                OPS_TRY((product<M, false, false>(ow, ox, cols, c.planes, 1, ep, st, large_tiles(words, rows, 1))));
+                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, Powers{b.w_powers, b.x_powers}};
+                const Operand lw = F32 ? Operand{b.w_even, c.cols_pad, plane_w, words} : ow, lx = F32 ? Operand{b.x_even, c.cols_pad, plane_x, rows} : ox;
+                OPS_TRY((product<L, false, false>(lw, lx, cols, F32 ? 3 : 1, 1, ep, st, large_tiles(words, rows))));
                 if (dx) {
                     const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
                     const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};
-                    OPS_TRY((product<M, true, false>(cw, od, words, c.planes, b.splits, sum, st, large_tiles(c.cols_pad, rows, b.splits))));
+                    OPS_TRY((product<M, true, false>(cw, od, words, SEGMENTS, b.splits, sum, st, b.dx_large)));
                 }
             }
             if (dweight) {   // (without rows: zeros)
                 const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.stride, plane_d, up(words, 8)};
                 const StoreEpilogue<T> store{dw, words, cols, scale};
-                OPS_TRY((product<M, true, true>(cx, cd, rows, c.planes, 1, store, st, large_tiles(cols, words, 1))));
+                OPS_TRY((product<M, true, true>(cx, cd, rows, SEGMENTS, 1, store, st, large_tiles(cols, words))));
             }
         }
         if (dx && rows) {
