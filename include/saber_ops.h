@@ -17,7 +17,7 @@
  *     rounded once, to nearest even.  The same inputs give the same bits.
  *   - Every function returns SABER_OK or a negative saber_status (saber.h) and never throws;
  *     saber_ops_last_error() has the message of the calling thread's last failure.
- *   - Limits: fewer than 2^31 rows and words, at most 2^20 columns (ERANGE).
+ *   - Limits: fewer than 2^31 rows and words, at most 2^20 columns; cross entropy: fewer than 2^26 rows (ERANGE).
  */
 #ifndef SABER_OPS_H
 #define SABER_OPS_H

@@ -275,9 +275,8 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial,
 
 // Rows too wide for registers: a workgroup of 1,024 goes over its row once per sum, from the caches after the first time.
 template <class T>
-__global__ __launch_bounds__(1024) void norm_forward_wide_kernel(NormForward a) {
-    __shared__ float lds[32];
-    const int64_t H = a.cols, row = blockIdx.x, nb = (H + kBlock - 1) / kBlock;
+__device__ __forceinline__ void norm_forward_wide_row(const NormForward &a, int64_t row, float *lds) {
+    const int64_t H = a.cols, nb = (H + kBlock - 1) / kBlock;
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
     const int64_t wide = (H + 8191) / 8192 * 8192;   // all lanes stay in the loop: they share a block's step
     float s = 0.f;
@@ -315,6 +314,11 @@ __global__ __launch_bounds__(1024) void norm_forward_wide_kernel(NormForward a) 
     }
     if (threadIdx.x == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
 }
+template <class T>
+__global__ __launch_bounds__(1024) void norm_forward_wide_kernel(NormForward a) {
+    __shared__ float lds[32];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) norm_forward_wide_row<T>(a, row, lds);
+}
 
 template <class T>
 __device__ __forceinline__ f32x8 load_hat(const NormBackward &a, int64_t row, int64_t c, float mean, float rstd) {
@@ -328,9 +332,8 @@ __device__ __forceinline__ f32x8 load_hat(const NormBackward &a, int64_t row, in
 }
 
 template <class T>
-__global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormBackward a) {
-    __shared__ float lds[32];
-    const int64_t H = a.cols, row = blockIdx.x;
+__device__ __forceinline__ void norm_backward_wide_row(const NormBackward &a, int64_t row, float *lds) {
+    const int64_t H = a.cols;
     const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s1 = 0.f, s2 = 0.f;
@@ -353,6 +356,11 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormBackward a
         for (int i = 0; i < 8; ++i) g[i] = rstd * (g[i] * w[i] - s1 - h[i] * s2);
         store8(static_cast<T *>(a.dx) + row * H + c, H - c, g);
     }
+}
+template <class T>
+__global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormBackward a) {
+    __shared__ float lds[32];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) norm_backward_wide_row<T>(a, row, lds);
 }
 
 // Partial sums for such rows: a workgroup takes 2,048 columns (grid.x) of every parts-th row (grid.y).

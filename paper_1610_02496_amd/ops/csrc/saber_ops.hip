@@ -26,6 +26,7 @@ int fail(int code, const char *fmt, ...) {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 20, kMaxWords = (int64_t)1 << 31;
 constexpr int kCus = 256;   // of gfx950: sizes of grids only
+constexpr int64_t kXentRows = (int64_t)1 << 26, kMaxTiles = (int64_t)1 << 24;   // (a launch has fewer than 2^32 threads)
 
 size_t size_of(int type) { return type == SABER_F32 ? 4 : 2; }
 bool is_type(int type) { return type == SABER_F32 || type == SABER_F16 || type == SABER_BF16; }
@@ -109,7 +110,7 @@ extern "C" int saber_layer_norm_forward(const void *x, int64_t x_stride, const v
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
-        if (cols > kNormCols) norm_forward_wide_kernel<T><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+        if (cols > kNormCols) norm_forward_wide_kernel<T><<<(unsigned)(rows < 64 * kCus ? rows : 64 * kCus), 1024, 0, st>>>(a);
         else {
             const int64_t groups = parts_of(rows, rows_per_group(cols));
             const unsigned grid = (unsigned)(groups < 8 * kCus ? groups : 8 * kCus);
@@ -167,7 +168,7 @@ extern "C" int saber_layer_norm_backward(const void *dy, int64_t dy_stride, cons
         using T = decltype(e);
         if (rows == 0) return SABER_OK;
         if (cols > kNormCols) {
-            if (dx) norm_backward_wide_kernel<T><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+            if (dx) norm_backward_wide_kernel<T><<<(unsigned)(rows < 64 * kCus ? rows : 64 * kCus), 1024, 0, st>>>(a);
             if (sums) norm_columns_wide_kernel<T><<<dim3((unsigned)parts_of(cols, 2048), (unsigned)parts), 256, 0, st>>>(a);
         } else
             OPS_TRY(with_norm_shape(cols, [&](auto tpr, auto nc) -> int {
@@ -255,6 +256,7 @@ bool direct(const void *p, int64_t stride, int64_t cols, int dtype) {
 
 int check_xent(const char *who, Xent &c) {
     OPS_TRY(check_rows(who, c.rows, c.cols, c.dtype));
+    if (c.rows >= kXentRows) return fail(SABER_ERANGE, "%s: %lld rows (limit 2^26 - 1)", who, (long long)c.rows);
     if (c.vocab < 1) return fail(SABER_EINVAL, "%s: a vocabulary of %lld words", who, (long long)c.vocab);
     if (c.vocab >= kMaxWords) return fail(SABER_ERANGE, "%s: a vocabulary of %lld words (limit 2^31 - 1)", who, (long long)c.vocab);
     OPS_TRY(check_stride(who, "x", c.x_stride, c.cols));
@@ -316,7 +318,9 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
         const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), most = few_lds(c) > 64 * 1024 ? kCus : 4 * kCus;
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
+        const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 128) * 128;   // words that one launch takes
         f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / c.cols_pad, c.rows, c.cols) : c.vocab;
+        if (f.piece > most) f.piece = most / 256 * 256;
         f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
         const int planes = c.planes == 3 ? 2 : 1;   // (the logits' form)
         if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * planes);
@@ -376,7 +380,7 @@ int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &
     p.tiles_m = (int)parts_of(a.major, tile);
     p.tiles_n = (int)parts_of(b.major, tile);
     const int64_t grid = (int64_t)p.tiles_m * p.tiles_n * splits;
-    if (grid >= (int64_t)1 << 31) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
+    if (grid >= kMaxTiles) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
     if (large) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
     else product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
     OPS_HIP(hipGetLastError());

@@ -423,3 +423,10 @@ def test_refusals_on_tensors():
         with pytest.raises(kind):
             call()
     assert np.isfinite(float(ops.linear_cross_entropy(x, w, t)))   # and goes on working
+
+
+def test_example_trains_a_head_on_the_topics():
+    """The example's whole run: topics of the sampler, training, scores of documents that were left out."""
+    from examples import topic_head
+    losses, held, unigram, one = topic_head.main(["--docs", "200", "--vocab", "1000", "--topics", "32", "--width", "128", "--steps", "40"])
+    assert losses[-1] < losses[0] - 1.0 and held < unigram and np.isfinite(one)
