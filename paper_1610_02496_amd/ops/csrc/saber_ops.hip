@@ -321,7 +321,7 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
         const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 128) * 128;   // words that one launch takes
         f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / c.cols_pad, c.rows, c.cols) : c.vocab;
         if (f.piece > most) f.piece = most / 256 * 256;
-        f.parts = parts_of(f.piece, 128) * parts_of(c.vocab, f.piece);   // with the smaller tiles
+        f.parts = c.vocab / f.piece * parts_of(f.piece, 128) + parts_of(c.vocab % f.piece, 128);   // with the smaller tiles
         const int planes = c.planes == 3 ? 2 : 1;   // (the logits' form)
         if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * planes);
         if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * planes);
