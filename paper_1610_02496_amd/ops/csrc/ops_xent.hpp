@@ -477,28 +477,38 @@ __global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Ta
     }
 }
 
-// dx = sum of the splits' partial sums, in a fixed order
+// dx = sum of the splits' partial sums, in a fixed order: every wavefront takes a quarter of the splits of 512 columns of a row, eight
+// on their way at a time, and the quarters meet in LDS
 template <class T>
 __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits, int64_t rows, int64_t stride, int64_t cols, const float *scale,
                                                   T *dx) {
-    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
-    if (c >= cols) return;
+    __shared__ f32x8 lds[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 8;
     const float down = scale ? scale[1] : 1.f;
-    for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
+    const int k0 = splits * wave / 4, k1 = splits * (wave + 1) / 4;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
         f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const float *from = sums + row * stride + c;   // (the stride is a multiple of 8)
-        int k = 0;
-        for (; k + 4 <= splits; k += 4) {              // four on their way at a time
-            f32x8 u[4];
+        if (c < cols) {
+            const float *from = sums + row * stride + c;   // (the stride is a multiple of 8)
+            int k = k0;
+            for (; k + 8 <= k1; k += 8) {
+                f32x8 u[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = load8(from + (int64_t)(k + i) * rows * stride, 8);
+                for (int i = 0; i < 8; ++i) u[i] = load8(from + (int64_t)(k + i) * rows * stride, 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v += u[i];
+                for (int i = 0; i < 8; ++i) v += u[i];
+            }
+#pragma unroll 4
+            for (; k < k1; ++k) v += load8(from + (int64_t)k * rows * stride, 8);
         }
-        for (; k < splits; ++k) v += load8(from + (int64_t)k * rows * stride, 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= down;
-        store8(dx + row * cols + c, cols - c, v);
+        lds[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0 && c < cols) {
+            for (int i = 1; i < 4; ++i) v += lds[i][lane];
+            store8(dx + row * cols + c, cols - c, v * down);
+        }
+        __syncthreads();
     }
 }
 

@@ -519,8 +519,7 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
             }
         }
         if (dx && rows) {
-            const int64_t y = parts_of(rows, 4);
-            sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, scale, static_cast<T *>(dx));
+            sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(rows < 16384 ? rows : 16384)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, scale, static_cast<T *>(dx));
             OPS_HIP(hipGetLastError());
         }
         return SABER_OK;
