@@ -30,7 +30,6 @@ __device__ __forceinline__ Raw8<T> load_raw8(const T *p, int64_t n) {
     Raw8<T> r;
 #pragma unroll
     for (int i = 0; i < kDwords; ++i) r.v[i] = 0;
-    if (n <= 0) return r;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) {
@@ -153,7 +152,6 @@ __device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {
 __device__ __forceinline__ Bytes8 load_raw_q(const int8_t *p, int64_t n) {
     if (n >= 8) return *reinterpret_cast<const Bytes8 *>(p);
     Bytes8 q = {{0, 0}};
-    if (n <= 0) return q;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) q.v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
