@@ -24,11 +24,34 @@ BLOCK = 128   # columns that share a step of a checkpoint
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _int64 = ctypes.c_int64
+_F32 = torch.float32
+
+_L = load_library()
+_norm_forward, _norm_backward, _norm_space = (_L.saber_layer_norm_forward, _L.saber_layer_norm_backward,
+                                              _L.saber_layer_norm_backward_workspace)
+_save8, _restore8 = _L.saber_checkpoint8_save, _L.saber_checkpoint8_restore
+_xent_forward, _xent_backward = _L.saber_linear_xent_forward, _L.saber_linear_xent_backward
+
+# without the objects that torch.cuda.current_stream() makes on every call (2 us of a call of 12)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _launch(call, device, *args):
+    """The call on the current stream of the tensors' device."""
+    index = device.index
+    if _current_device() == index:
+        rc = call(*args, _current_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, _current_stream(index))
+    if rc != SABER_OK:
+        _check(rc)
 
 
 def _check(rc):
     if rc != SABER_OK:
-        raise SaberError(rc, load_library().saber_ops_last_error().decode("utf-8", "replace"))
+        raise SaberError(rc, _L.saber_ops_last_error().decode("utf-8", "replace"))
 
 
 def _type(name, t):
@@ -38,70 +61,42 @@ def _type(name, t):
     return code
 
 
-def _on(name, t, device):
-    if t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-
-
-def _device(t, name):
+def _device(t, name, like=None):
+    """The device of a tensor in device memory: that of `like` where there is one."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a tensor" % name)
     if not t.is_cuda:
         raise ValueError("%s must be in device memory, not on %s" % (name, t.device))
+    if like is not None and t.device != like:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, like))
     return t.device
 
 
 def _rows(t, name):
-    """(rows, columns, elements between rows) of a tensor seen as a matrix of its last dimension, without a copy where the
-    layout allows it; the tensor itself, or a contiguous copy."""
-    if t.dim() == 2:
-        rows, cols = t.shape
-        if t.stride(1) == 1 or cols == 1:
-            stride = t.stride(0)
-            if stride >= cols:
-                return t, rows, cols, stride
-            if rows <= 1:
-                return t, rows, cols, cols
-        t = t.contiguous()
-        return t, rows, cols, cols
-    if t.dim() == 0:
+    """(matrix, rows, columns, elements between rows) of a tensor seen as a matrix of its last dimension, without a copy where
+    the layout allows it; the matrix is the tensor itself, or a contiguous copy."""
+    shape = t.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        stride, one = t.stride()
+        if (one == 1 or cols == 1) and (stride >= cols or rows <= 1):
+            return t, rows, cols, stride if stride >= cols else cols
+        return t.contiguous(), rows, cols, cols
+    if not shape:
         raise ValueError("%s has no columns" % name)
-    cols = t.shape[-1]
-    t = t.contiguous()
-    return t, t.numel() // cols if cols else 0, cols, cols
-
-
-class _Launch:
-    """The raw stream to launch on, with the tensors' device current."""
-
-    __slots__ = ("index", "guard")
-
-    def __init__(self, device):
-        self.index = device.index
-        self.guard = None
-
-    def __enter__(self):
-        if _current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-        return _current_stream(self.index)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-
-# without the objects that torch.cuda.current_stream() makes on every call (2 us of a call of 12)
-_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    cols = shape[-1]
+    return t.contiguous(), t.numel() // cols if cols else 0, cols, cols
 
 
 def _vector(t, name, cols, like, of):
-    _device(t, name)
-    _on(name, t, like)
+    _device(t, name, like)
     if t.shape != (cols,):
         raise ValueError("%s must hold %d values, one per column of %s" % (name, cols, of))
     return t if t.is_contiguous() else t.contiguous()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 # ---- checkpoints in 8 bits -------------------------------------------------------------------------------------------
@@ -118,17 +113,14 @@ class Checkpoint8:
     def restore(self, dtype=None):
         """The activation, in its own type or another floating type."""
         q = self.q
-        x = torch.empty(q.shape, dtype=dtype or self.dtype, device=q.device)
+        x = torch.empty_like(q, dtype=dtype or self.dtype)
         cols = q.shape[-1]
-        with _Launch(q.device) as stream:
-            _check(load_library().saber_checkpoint8_restore(q.data_ptr(), self.scale.data_ptr(), q.numel() // cols if cols else 0, cols,
-                                                            _type("dtype", x), x.data_ptr(), stream))
+        _launch(_restore8, q.device, q.data_ptr(), self.scale.data_ptr(), q.numel() // cols if cols else 0, cols, _type("dtype", x), x.data_ptr())
         return x
 
 
 def _empty_checkpoint(x, rows, cols):
-    return Checkpoint8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
-                       torch.empty((rows, (cols + BLOCK - 1) // BLOCK), dtype=torch.float32, device=x.device), x.dtype)
+    return Checkpoint8(x.new_empty(x.shape, dtype=torch.int8), x.new_empty((rows, (cols + BLOCK - 1) // BLOCK), dtype=_F32), x.dtype)
 
 
 def checkpoint8(x) -> Checkpoint8:
@@ -137,8 +129,7 @@ def checkpoint8(x) -> Checkpoint8:
     code = _type("x", x)
     m, rows, cols, stride = _rows(x, "x")
     c = _empty_checkpoint(x, rows, cols)
-    with _Launch(device) as stream:
-        _check(load_library().saber_checkpoint8_save(m.data_ptr(), stride, rows, cols, code, c.q.data_ptr(), c.scale.data_ptr(), stream))
+    _launch(_save8, device, m.data_ptr(), stride, rows, cols, code, c.q.data_ptr(), c.scale.data_ptr())
     return c
 
 
@@ -159,68 +150,60 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
     own or that of ``x``).  With ``checkpoint`` the input is held in 8 bits for the backward pass, written in the same
     pass over ``x``; ``x`` itself is not kept."""
     device = _device(x, "x")
-    code = _type("x", x)
+    code = wcode = _type("x", x)
     m, rows, cols, stride = _rows(x, "x")
-    wcode = code
     if weight is not None:
         weight = _vector(weight, "weight", cols, device, "x")
         wcode = _type("weight", weight)
     if bias is not None:
         bias = _vector(bias, "bias", cols, device, "x")
-        bcode = _type("bias", bias)
-        if weight is not None and bcode != wcode:
+        if weight is None:
+            wcode = _type("bias", bias)
+        elif bias.dtype != weight.dtype:
             raise TypeError("weight and bias must have one type, not %s and %s" % (weight.dtype, bias.dtype))
-        wcode = bcode
-    y = torch.empty(x.shape, dtype=x.dtype, device=device)
-    mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=device)
-    c = _empty_checkpoint(x, rows, cols) if checkpoint else None
-    with _Launch(device) as stream:
-        _check(load_library().saber_layer_norm_forward(
-            m.data_ptr(), stride, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), rows, cols,
-            code, wcode, eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), None if c is None else c.q.data_ptr(),
-            None if c is None else c.scale.data_ptr(), stream))
+    y = torch.empty_like(m)   # (contiguous: m is a matrix of whole rows)
+    mean, rstd = x.new_empty((2, rows), dtype=_F32).unbind()
+    c, q, scale = None, None, None
+    if checkpoint:
+        c = _empty_checkpoint(x, rows, cols)
+        q, scale = c.q.data_ptr(), c.scale.data_ptr()
+    _launch(_norm_forward, device, m.data_ptr(), stride, _ptr(weight), _ptr(bias), rows, cols, code, wcode, eps, y.data_ptr(), mean.data_ptr(),
+            rstd.data_ptr(), q, scale)
     return y, NormSaved(None if checkpoint else m, c, weight, bias, mean, rstd)
 
 
 def layer_norm_backward(dy, saved, need_x=True, need_weight=True, need_bias=True):
     """``(dx, dweight, dbias)`` of a layer norm for the gradient ``dy`` of its output; None where not needed or where the
     norm has no weight or bias."""
-    device = _device(dy, "dy")
-    source = saved.x if saved.checkpoint is None else saved.checkpoint.q
-    dtype = saved.x.dtype if saved.checkpoint is None else saved.checkpoint.dtype
+    c = saved.checkpoint
+    source, dtype = (saved.x, saved.x.dtype) if c is None else (c.q, c.dtype)
+    device = _device(dy, "dy", source.device)
     if dy.dtype != dtype:
         raise TypeError("dy must be %s like the norm's input, not %s" % (dtype, dy.dtype))
-    _on("dy", dy, source.device)
-    code = _TYPES[dtype]
+    code = wcode = _TYPES[dtype]
     m, rows, cols, stride = _rows(dy, "dy")
     if cols != source.shape[-1] or rows != saved.mean.shape[0]:
         raise ValueError("dy must have the shape of the norm's input")
     weight, bias = saved.weight, saved.bias
-    wcode = code if weight is None and bias is None else _TYPES[(bias if weight is None else weight).dtype]
-    dx = torch.empty(dy.shape, dtype=dtype, device=device) if need_x else None
+    if weight is not None or bias is not None:
+        wcode = _TYPES[(bias if weight is None else weight).dtype]
+    dx = torch.empty_like(m) if need_x else None
     dweight = torch.empty_like(weight) if need_weight and weight is not None else None
     dbias = torch.empty_like(bias) if need_bias and bias is not None else None
-    L = load_library()
     space, nbytes = None, 0
     if dweight is not None or dbias is not None:
-        nbytes = _norm_space(L, rows, cols)
-        space = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    c = saved.checkpoint
-    x, x_stride = (None, 0) if c is not None else (saved.x.data_ptr(), _rows(saved.x, "x")[3])
-    with _Launch(device) as stream:
-        _check(L.saber_layer_norm_backward(
-            m.data_ptr(), stride, x, x_stride, None if c is None else c.q.data_ptr(), None if c is None else c.scale.data_ptr(),
-            saved.mean.data_ptr(), saved.rstd.data_ptr(), None if weight is None else weight.data_ptr(), rows, cols, code, wcode,
-            None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
-            None if dbias is None else dbias.data_ptr(), None if space is None else space.data_ptr(), nbytes, stream))
+        n = _int64()
+        _check(_norm_space(rows, cols, ctypes.addressof(n)))
+        nbytes = n.value
+        space = dy.new_empty(nbytes, dtype=torch.uint8)
+    x, x_stride, q, scale = None, 0, None, None
+    if c is None:
+        x, x_stride = source.data_ptr(), _rows(source, "x")[3]
+    else:
+        q, scale = source.data_ptr(), c.scale.data_ptr()
+    _launch(_norm_backward, device, m.data_ptr(), stride, x, x_stride, q, scale, saved.mean.data_ptr(), saved.rstd.data_ptr(), _ptr(weight), rows, cols,
+            code, wcode, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(space), nbytes)
     return dx, dweight, dbias
-
-
-def _norm_space(L, rows, cols):
-    n = _int64()
-    _check(L.saber_layer_norm_backward_workspace(rows, cols, ctypes.addressof(n)))
-    return n.value
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -254,64 +237,55 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
 def _head(x, weight, target):
     device = _device(x, "x")
     code = _type("x", x)
-    _device(weight, "weight")
-    _on("weight", weight, device)
+    _device(weight, "weight", device)
     if weight.dtype != x.dtype:
         raise TypeError("weight must be %s like x, not %s" % (x.dtype, weight.dtype))
     if weight.dim() != 2 or weight.shape[1] != x.shape[-1]:
         raise ValueError("weight must be [words, %d] for features of that width" % x.shape[-1])
-    _device(target, "target")
-    _on("target", target, device)
-    if target.dtype != torch.int64 and target.dtype != torch.int32:
+    _device(target, "target", device)
+    wide = target.dtype == torch.int64
+    if not wide and target.dtype != torch.int32:
         raise TypeError("target must be int32 or int64, not %s" % target.dtype)
     if target.shape != x.shape[:-1]:
         raise ValueError("target must hold one word per row of x")
     m, rows, cols, stride = _rows(x, "x")
     w, vocab, _, w_stride = _rows(weight, "weight")
-    return device, code, m, rows, cols, stride, w, vocab, w_stride, target if target.is_contiguous() else target.contiguous()
+    t = target if target.is_contiguous() else target.contiguous()
+    # (m, w and t are held here until the call: they may be copies)
+    return device, (m, w, t), (m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), wide), (rows, vocab, cols, code)
 
 
-def _space(call, args, device):
-    """Work space of a pass: how much, and the memory."""
+def _with_space(call, device, x, args):
+    """The call with a work space of the size that it asks for."""
     n = _int64()
-    _check(call(*args, None, ctypes.addressof(n), None))
-    return n, torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
+    at = ctypes.addressof(n)
+    _check(call(*args, None, at, None))
+    space = x.new_empty(n.value or 1, dtype=torch.uint8)
+    _launch(call, device, *args, space.data_ptr(), at)
 
 
 def linear_cross_entropy_forward(x, weight, target):
     """``(loss, lse)`` per row of ``x``: minus log likelihood of the row's target word under softmax(x weight^T), and the
     logarithm of the softmax' normaliser; float32, in the shape of ``target``.  The logits are not held.  A negative target
     leaves its row out (loss 0); one beyond the vocabulary gives NaN."""
-    device, code, m, rows, cols, stride, w, vocab, w_stride, t = _head(x, weight, target)
-    loss = torch.empty(target.shape, dtype=torch.float32, device=device)
-    lse = torch.empty(target.shape, dtype=torch.float32, device=device)
-    call = load_library().saber_linear_xent_forward
-    args = (m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), t.dtype == torch.int64, rows, vocab, cols, code, loss.data_ptr(),
-            lse.data_ptr())
-    with _Launch(device) as stream:
-        n, space = _space(call, args, device)
-        _check(call(*args, space.data_ptr(), ctypes.addressof(n), stream))
+    device, held, inputs, sizes = _head(x, weight, target)
+    loss, lse = x.new_empty((2,) + target.shape, dtype=_F32).unbind()
+    _with_space(_xent_forward, device, x, inputs + sizes + (loss.data_ptr(), lse.data_ptr()))
     return loss, lse
 
 
 def linear_cross_entropy_backward(dloss, x, weight, target, lse, need_x=True, need_weight=True):
     """``(dx, dweight)`` for the gradient ``dloss`` (float32) of every row's loss; None where not needed.  ``lse`` is what the
     forward pass gave."""
-    device, code, m, rows, cols, stride, w, vocab, w_stride, t = _head(x, weight, target)
+    device, held, inputs, sizes = _head(x, weight, target)
     for name, v in (("dloss", dloss), ("lse", lse)):
-        _device(v, name)
-        _on(name, v, device)
-        if v.dtype != torch.float32 or v.shape != target.shape:
+        _device(v, name, device)
+        if v.dtype != _F32 or v.shape != target.shape:
             raise ValueError("%s must be float32, one value per row of x" % name)
     dloss, lse = dloss.contiguous(), lse.contiguous()
-    dx = torch.empty(x.shape, dtype=x.dtype, device=device) if need_x else None
-    dweight = torch.empty((vocab, cols), dtype=x.dtype, device=device) if need_weight else None
-    call = load_library().saber_linear_xent_backward
-    args = (dloss.data_ptr(), m.data_ptr(), stride, w.data_ptr(), w_stride, t.data_ptr(), t.dtype == torch.int64, lse.data_ptr(), rows,
-            vocab, cols, code, None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr())
-    with _Launch(device) as stream:
-        n, space = _space(call, args, device)
-        _check(call(*args, space.data_ptr(), ctypes.addressof(n), stream))
+    dx = torch.empty_like(held[0]) if need_x else None
+    dweight = torch.empty_like(held[1]) if need_weight else None
+    _with_space(_xent_backward, device, x, (dloss.data_ptr(),) + inputs + (lse.data_ptr(),) + sizes + (_ptr(dx), _ptr(dweight)))
     return dx, dweight
 
 
