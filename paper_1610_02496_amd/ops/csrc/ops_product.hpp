@@ -1,12 +1,12 @@
 // Matrix products of the head on the matrix cores: D[m][n] = sum over k of A[m][k] B[n][k], with either operand stored with k
 // fastest or with k slowest, and an epilogue that consumes the tile from registers.
 //
-// A workgroup computes a BM x BN tile in steps of 64 along k.  Operands go from memory to LDS directly (16 bytes a lane), one step
-// ahead of the arithmetic, into two buffers.  LDS is written in order of the lanes; what a lane fetches is permuted instead, so that
-// the reads of a fragment meet different banks:
+// A workgroup of four wavefronts computes a BM x BN tile in steps of 64 along k.  Operands go from memory to LDS directly (16 bytes a
+// lane), up to two steps ahead of the arithmetic.  LDS is written in order of the lanes; what a lane fetches is permuted instead, so
+// that the reads of a fragment meet different banks:
 //   k fastest: a row of 64 k is 8 pieces of 16 bytes; piece p of row r lies at p ^ (r & 7); a lane reads its 8 values of k at once.
-//   k slowest: a row holds BM (BN) columns in pieces of 16 bytes; piece p of row k lies at p ^ 2 f(k), f(k) = (k & 3) | (k & 8) >> 1;
-//              a lane's 8 values of k come through two transposing reads of 4 rows x 16 columns each.
+//   k slowest: a row holds U = 128 (64) columns in pieces of 16 bytes; piece p of row k lies at p ^ 2 f(k), f(k) = (k & 3) | (k & 8) >> 1
+//              (k & 3); a lane's 8 values of k come through two transposing reads of 4 rows x 16 columns each.
 // Rows and columns outside the operands are read as zeros (the bounds of the buffer descriptors), so no tile reads out of range.
 //
 // Operands of binary32 come as planes, and the products of planes that matter are added as further steps along k ("segments"):
@@ -69,12 +69,13 @@ __device__ __forceinline__ void settled(f32x4 (&c)[M][N]) {
 #pragma unroll
     for (int i = 0; i < M; ++i)
 #pragma unroll
-        for (int j = 0; j < N; j += 4) asm volatile("s_nop 7" : "+a"(c[i][j]), "+a"(c[i][j + 1]), "+a"(c[i][j + 2]), "+a"(c[i][j + 3]));
+        for (int j = 0; j < N; j += 2) asm volatile("s_nop 7" : "+a"(c[i][j]), "+a"(c[i][j + 1]));
 }
 
 using LdsBytes = __attribute__((address_space(3))) char;
 
-__device__ __forceinline__ int slow_swizzle(int k) { return ((k & 3) | ((k & 8) >> 1)) << 1; }
+template <int U>
+__device__ __forceinline__ int slow_swizzle(int k) { return ((k & 3) | (U == 128 ? (k & 8) >> 1 : 0)) << 1; }
 
 // 16 bytes per lane from the buffer to LDS, lane after lane from `lds` on, past the registers.  Nothing waits for it but a wait for
 // the vector memory counter; in assembly, because the compiler puts such a wait in front of every later read of LDS.  The load has no
@@ -91,23 +92,22 @@ __device__ __forceinline__ u32x4 buffer_of(const char *p, uint32_t bytes) {
                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
-// LDS is a ring of units: 128 rows of m (n) by 64 k, in the layout above; 16 KB.
-constexpr int kUnit = 128, kUnitBytes = kUnit * kStep * 2;
-
+// LDS is a ring of units: U = 128 (64) rows of m (n) by 64 k, in the layout above; 16 (8) KB.
 // How a wave fetches its share of one operand's tile of W columns (or rows) of m, unit by unit.
-template <bool SLOW, int W, int WAVES>
+template <bool SLOW, int W, int U, int WAVES>
 struct Loader {
-    static constexpr int kEach = kUnitBytes / 1024 / WAVES;      // requests of a wave per unit, 1 KB each
-    static constexpr int kAll = kEach * (W / kUnit);             // and per step
-    static constexpr int kRows = SLOW ? 4 : 8;                   // stored rows that one request covers
-    static_assert(kEach == 4, "four waves");
+    static constexpr int kEach = U * kStep * 2 / 1024 / WAVES;   // requests of a wave per unit, 1 KB each
+    static constexpr int kAll = kEach * (W / U);                 // and per step
+    static constexpr int kPieces = SLOW ? U / 8 : 8;             // of 16 bytes, in a stored row
+    static constexpr int kRows = 64 / kPieces;                   // stored rows that one request covers
+    static_assert(WAVES == 4 && (U == 128 || U == 64), "the permutation's dependence on the request");
     const char *base;        // first element of the tile, plane 0
     uint32_t stride_bytes;
     int64_t plane_bytes;
     uint32_t extent;         // k fastest: bytes from the tile's first row to its last one's start; k slowest: bytes of a row
     uint32_t voff;           // of the wave's first request
     int piece_k;             // k fastest: first k of the lane's piece; k slowest: its piece
-    int lane_k, wave_k;      // k slowest: the stored row of the lane's first piece, within 4, and of the wave's first
+    int lane_k, wave_k;      // k slowest: the stored row of the lane's piece within a request, and of the wave's first request
 
     __device__ __forceinline__ void init(const Operand &o, int64_t origin, int wave, int lane) {
         stride_bytes = (uint32_t)o.stride * 2;
@@ -115,9 +115,9 @@ struct Loader {
         if constexpr (SLOW) {
             base = static_cast<const char *>(o.p) + origin * 2;
             extent = (uint32_t)((o.major - origin < W ? o.major - origin : W) * 2);
-            voff = (wave * kEach * kRows + (lane >> 4)) * stride_bytes;
-            piece_k = lane & 15;
-            lane_k = lane >> 4;
+            voff = (wave * kEach * kRows + lane / kPieces) * stride_bytes;
+            piece_k = lane % kPieces;
+            lane_k = lane / kPieces;
             wave_k = wave * kEach * kRows;
         } else {
             base = static_cast<const char *>(o.p) + origin * (int64_t)stride_bytes;
@@ -147,8 +147,8 @@ struct Loader {
         rsrc = buffer_of(p, any ? bytes : 0);                    // past the last step: zeros that nobody uses
         off[0] = off[1] = at;
         if constexpr (SLOW) {                                    // the permutation is one for the first two requests, one for the others
-            off[0] += (uint32_t)(piece_k ^ slow_swizzle(lane_k + wave_k)) * 16;
-            off[1] += (uint32_t)(piece_k ^ slow_swizzle(lane_k + wave_k + 2 * kRows)) * 16;
+            off[0] += (uint32_t)(piece_k ^ slow_swizzle<U>(lane_k + wave_k)) * 16;
+            off[1] += (uint32_t)(piece_k ^ slow_swizzle<U>(lane_k + wave_k + 2 * kRows)) * 16;
         }
     }
     // the next step of a segment that has one after it which is whole
@@ -163,13 +163,13 @@ struct Loader {
     // request j of the step; lds: the wave's place in the unit that it belongs to
     __device__ __forceinline__ void one(LdsBytes *lds, int j) const {
         const int u = j / kEach, i = j % kEach;
-        load_to_lds(rsrc, lds + i * 1024, off[SLOW ? i >> 1 : 0], i * kRows * stride_bytes + (SLOW ? u * kUnit * 2 : u * kUnit * stride_bytes));
+        load_to_lds(rsrc, lds + i * 1024, off[SLOW ? i >> 1 : 0], i * kRows * stride_bytes + (SLOW ? u * U * 2 : u * U * stride_bytes));
     }
 };
 
 // Fragments of 16 rows of m by 32 values of k: lane l holds row l % 16, k 8 (l / 16) .. + 7.  The addresses of a lane differ between
 // fragments by constants, up to the permutation: a register per distinct one, the rest are the instructions' own offsets.
-template <bool SLOW, int N>
+template <bool SLOW, int U, int N>
 struct Reader {
     uint32_t at[SLOW ? N : 2];
     __device__ __forceinline__ void init(int row, int lane) {   // row: of the unit
@@ -177,7 +177,7 @@ struct Reader {
             // lane l of 16 addresses row k + l / 4 of four, columns 4 (l % 4) .. + 3; it receives column l of the four rows
             const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), col = row + 4 * (lane & 3);
 #pragma unroll
-            for (int i = 0; i < N; ++i) at[i] = k * kUnit * 2 + (((col + 16 * i) * 2) ^ (slow_swizzle(k) * 16));
+            for (int i = 0; i < N; ++i) at[i] = k * U * 2 + (((col + 16 * i) * 2) ^ (slow_swizzle<U>(k) * 16));
         } else {
             at[0] = (row + (lane & 15)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
             at[1] = at[0] ^ 64;
@@ -188,8 +188,8 @@ struct Reader {
         if constexpr (SLOW) {   // (k + 4 and k + 32 are permuted like k)
             using P = __attribute__((address_space(3))) s16x4 *;
             union { s16x4 h[2]; u32x4 v; } u;
-            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + kk * kUnit * 2));
-            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + (kk + 4) * kUnit * 2));
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + kk * U * 2));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at[i] + (kk + 4) * U * 2));
             return u.v;
         } else
             return *(const __attribute__((address_space(3))) u32x4 *)(lds + at[kk / 32] + i * 16 * 128);
@@ -200,7 +200,8 @@ template <class T, bool A_SLOW, bool B_SLOW, int BM, int BN, int WM, int WN, cla
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilogue e) {
 #if defined(__HIP_DEVICE_COMPILE__)   // (the host pass knows neither the matrix instructions nor their types)
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int UA = BM / kUnit, UB = BN / kUnit, UNITS = UA + UB, RING = UNITS * 5 / 2;   // units of a step, and in LDS
+    constexpr int U = BM < 128 ? BM : 128, kUnitBytes = U * kStep * 2;
+    constexpr int UA = BM / U, UB = BN / U, UNITS = UA + UB, RING = UNITS * 5 / 2;           // units of a step, and in LDS
     static_assert(UA == UB, "the order of requests");
     __shared__ __attribute__((aligned(1024))) char smem[RING * kUnitBytes];
     LdsBytes *const lds = (LdsBytes *)smem;
@@ -222,15 +223,15 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
     const int tm = in_group / width, tn = group * 8 + in_group % width;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
 
-    Loader<A_SLOW, BM, WAVES> la;
-    Loader<B_SLOW, BN, WAVES> lb;
+    Loader<A_SLOW, BM, U, WAVES> la;
+    Loader<B_SLOW, BN, U, WAVES> lb;
     la.init(p.a, m0, wave, lane);
     lb.init(p.b, n0, wave, lane);
     const int wm = (wave / WN) * TM * 16, wn = (wave % WN) * TN * 16;
-    Reader<A_SLOW, TM> ra;
-    Reader<B_SLOW, TN> rb;
-    ra.init(wm % kUnit, lane);
-    rb.init(wn % kUnit, lane);
+    Reader<A_SLOW, U, TM> ra;
+    Reader<B_SLOW, U, TN> rb;
+    ra.init(wm % U, lane);
+    rb.init(wn % U, lane);
 
     const int per_seg = (int)((p.k + kStep - 1) / kStep), steps = per_seg * p.segments;
     const int first = (int)((int64_t)steps * split / p.splits), last = (int)((int64_t)steps * (split + 1) / p.splits);
@@ -249,11 +250,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
     // requests at just the pace of the products, and a wave that has to wait for it is one that multiplies nothing.
     // Before group FREE everyone has read all of step s.  The ring has room for two and a half steps, so B of step s + 2 then goes where
     // A of step s was, and A of step s + 3 where B of step s was.  Before group NEED step s + 1 has arrived.
-    constexpr int LA = Loader<A_SLOW, BM, WAVES>::kAll, LB = Loader<B_SLOW, BN, WAVES>::kAll, EACH = Loader<A_SLOW, BM, WAVES>::kEach;
+    constexpr int LA = Loader<A_SLOW, BM, U, WAVES>::kAll, LB = Loader<B_SLOW, BN, U, WAVES>::kAll, EACH = Loader<A_SLOW, BM, U, WAVES>::kEach;
     constexpr int GROUPS = 2 * TM, FREE = TM / 2 + 1, NEED = TM + TM / 2;
     static_assert(LA + LB == GROUPS, "one request per group");
     constexpr int READ1 = (TM + TN + FREE - 2) / (FREE - 1);                 // reads per group: of k 32 .. 63, in groups 0 .. FREE - 2
     constexpr int READ0 = (TM + TN + GROUPS - NEED - 1) / (GROUPS - NEED);   // of the next step's k 0 .. 31, from group NEED on
+    constexpr int MOVE = TN > 3 ? TN - 3 : 0;                                // the product after which the next step is gone to
     constexpr int AHEAD = GROUPS - FREE - LB;                                // requests for A of step s + 2 before step s begins
     u32x4 fa[2][TM], fb[2][TN];
     // where a step's data is asked for: the next step of its segment, or, rarely, another segment, a step that ends in mid-air, or none
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
     LdsBytes *to_a = lds, *to_b = lds + UA * kUnitBytes;                     // of the step that is asked for
     auto request_a = [&](int j) { la.one((UA > 1 && j >= EACH ? after(to_a, 1) : to_a) + own, j); };
     auto request_b = [&](int j) { lb.one((UB > 1 && j >= EACH ? after(to_b, 1) : to_b) + own, j); };
-    LdsBytes *from_a = lds + wm / kUnit * kUnitBytes, *from_b = lds + (UA + wn / kUnit) * kUnitBytes;   // of the step that is read
+    LdsBytes *from_a = lds + wm / U * kUnitBytes, *from_b = lds + (UA + wn / U) * kUnitBytes;   // of the step that is read
     auto read = [&](int set, int j, int kk) {
         if (j < TN) fb[set][j] = rb.get(from_b, j, kk);
         else if (j < TN + TM) fa[set][j - TN] = ra.get(from_a, j - TN, kk);
@@ -334,8 +336,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
 #pragma unroll
                     for (int r = j; r < READ0; r += TN) read(0, (g - NEED) * READ0 + r, 0);   // (after the last step: zeros, never used)
                 }
-                if constexpr (j == TN - 3 && g == FREE - 1) { next_b(); to_b = after(to_b, UNITS); }
-                if constexpr (j == TN - 3 && g == FREE + LB - 1) { next_a(); to_a = after(to_a, UNITS); }
+                if constexpr (j == MOVE && g == FREE - 1) { next_b(); to_b = after(to_b, UNITS); }
+                if constexpr (j == MOVE && g == FREE + LB - 1) { next_a(); to_a = after(to_a, UNITS); }
                 if constexpr (j == TN - 1) {
                     if constexpr (g < FREE) request_a(AHEAD + g);
                     else if constexpr (g < FREE + LB) request_b(g - FREE);

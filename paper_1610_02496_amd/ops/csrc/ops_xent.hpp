@@ -618,18 +618,18 @@ __global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, i
         if (!done) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            float top = -INFINITY;
+            float top = m[j];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (v0 + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
                 if (v0 + r >= vocab) acc[j][r] = -INFINITY;
                 top = fmaxf(top, acc[j][r]);
             }
+            if (__builtin_amdgcn_ballot_w64(top > m[j])) s[j] *= m[j] == top ? 1.f : expf(m[j] - top);   // ever more rarely
+            m[j] = top;
             const Exp<F32> power(top > -INFINITY ? top : 0.f);
-            float sum = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += power(acc[j][r]);
-            join(m[j], s[j], top, sum);
+            for (int r = 0; r < 4; ++r) s[j] += power(acc[j][r]);
             acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }

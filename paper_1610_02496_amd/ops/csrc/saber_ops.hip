@@ -237,7 +237,8 @@ namespace {
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewLds = 150 * 1024;
 // values of d, and of packed words, per piece: 256 MB of a 16-bit type, what the last-level cache holds; 768 MB of three planes (binary32
-// gains from fewer pieces: 2,048 rows of 512 columns, 60,000 words, TODO ms in one, TODO in three)
+// gains from fewer pieces: the gradients of 2,048 rows of 512 columns and 60,000 words, d and the weight's product take 1.21 ms in one,
+// 1.49 ms in three)
 constexpr int64_t kPieceValues = (int64_t)1 << 27;
 
 struct Xent {
@@ -270,15 +271,25 @@ int check_xent(const char *who, Xent &c) {
     return SABER_OK;
 }
 
-// A tile of 256 x 256 has twice the arithmetic per byte from LDS of one of 128 x 128, but takes a CU for itself, as two of the others
-// do that take about 5 / 8 of its time: whichever fills its rounds better.
-bool large_tiles(int64_t m, int64_t n) {
-    return 8 * parts_of(parts_of(m, 256) * parts_of(n, 256), kCus) <= 5 * parts_of(parts_of(m, 128) * parts_of(n, 128), 2 * kCus);
+// The tile of a product of `steps` steps of 64 along k.  256 x 256 has twice the arithmetic per byte from LDS of 128 x 128 and four times
+// that of 64 x 64, but takes a CU for itself; two of the second share one, four of the third, and then one's loads and stores go on beside
+// the other's products.  Which ends first, in units of 0.1 us: rounds of workgroups times what a step and what a workgroup's two ends cost, and
+// the first loads and last stores, which nothing hides.  Measured in us with 256, 128 and 64 in turn (bf16 but for the last; 250 x 5000
+// in f32 has 12 steps), of products m x n by steps: 4096 x 32,768 by 16: 342, 362, -; 32,768 x 1024 by 64: 235, 287, -;
+// 200 x 60,000 by 8: 33.7, 25.7, 35.4; 60,000 x 512 by 4: 37.6, 35.2, 49.6; 500 x 10,000 by 5: 28.3, 13.3, 14.8; 32 x 2000 by 8: 26.0,
+// 11.5, 7.6; 250 x 5000 by 12: 41.4, 15.2, 10.9.
+int tile_of(int64_t m, int64_t n, int64_t steps) {
+    auto tiles = [&](int64_t t) { return parts_of(m, t) * parts_of(n, t); };
+    const int64_t large = tiles(256), middle = tiles(128), small = tiles(64);
+    const int64_t t256 = parts_of(large, kCus) * (18 * steps + 100) + 100;
+    const int64_t t128 = middle <= kCus ? 8 * steps + 55 : parts_of(middle, 2 * kCus) * (11 * steps + 45) + 20;
+    const int64_t t64 = small <= kCus ? 4 * steps + 35 : small <= 2 * kCus ? 6 * steps + 35 : parts_of(small, 4 * kCus) * (10 * steps + 20) + 35;
+    return t64 < t128 && t64 < t256 ? 64 : t128 < t256 ? 128 : 256;
 }
 
 // Words of a piece, at most `most` (and 2^20: offsets within a tile are 32 bits), whole tiles.  Either all pieces are even, or all but
 // the last fill the CUs with whole rounds of tiles: of d (words x rows), and of the weight's gradient (words x columns), whichever
-// takes fewer rounds in all.  (4,096 rows of 1,024 columns, 100,000 words: 36 rounds even, 32 the other way, 3.4 -> TODO ms.)
+// takes fewer rounds in all.  (4,096 rows of 1,024 columns, 100,000 words, both passes: 36 rounds and 3.46 ms even, 32 and 3.30 ms the other way.)
 int64_t piece_words(int64_t vocab, int64_t most, int64_t rows, int64_t cols) {
     if (most > (int64_t)1 << 20) most = (int64_t)1 << 20;
     most = most / 256 * 256;
@@ -310,18 +321,19 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; int tile; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
     if (few(c)) {
-        const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), most = few_lds(c) > 64 * 1024 ? kCus : 4 * kCus;
+        const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), each = 160 * 1024 / (few_lds(c) + 1024), most = kCus * (each > 4 ? 4 : each < 1 ? 1 : each);
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
-        const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 128) * 128;   // words that one launch takes
+        const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 64) * 64;   // words that one launch takes
         f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / c.cols_pad, c.rows, c.cols) : c.vocab;
         if (f.piece > most) f.piece = most / 256 * 256;
-        f.parts = c.vocab / f.piece * parts_of(f.piece, 128) + parts_of(c.vocab % f.piece, 128);   // with the smaller tiles
+        f.tile = tile_of(f.piece, c.rows, parts_of(c.cols, kStep) * (c.planes == 3 ? 3 : 1));
+        f.parts = c.vocab / f.piece * parts_of(f.piece, f.tile) + parts_of(c.vocab % f.piece, f.tile);
         const int planes = c.planes == 3 ? 2 : 1;   // (the logits' form)
         if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * planes);
         if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * planes);
@@ -332,18 +344,22 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
     return f;
 }
 
-struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *sums; int64_t piece, stride; int splits; bool dx_large; };
+struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *sums; int64_t piece, stride; int splits, dx_tile; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
     const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / row, most_w = kPieceValues / c.cols_pad;
     b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w, row, c.cols);
     const int64_t steps = parts_of(b.piece, kStep) * (c.planes == 3 ? 6 : 1);
-    // The features' gradient has few tiles and many steps, which are shared out until every CU has a workgroup: of large tiles, if
-    // each then still has 16 steps or more (eight of the smaller ones).
-    const int64_t large = parts_of(c.cols_pad, 256) * parts_of(row, 256), small = parts_of(c.cols_pad, 128) * parts_of(row, 128);
-    b.dx_large = parts_of(kCus, large) <= steps / 16;
-    int64_t splits = b.dx_large ? kCus / large : parts_of(2 * kCus, small);
-    if (!b.dx_large && splits > steps / 8) splits = steps / 8;
+    // The features' gradient has few tiles and many steps, which are shared out until every CU has a workgroup: of the largest tiles
+    // of which each still has 16 steps or more.
+    b.dx_tile = 64;
+    for (int tile : {256, 128}) {
+        const int64_t tiles = parts_of(c.cols_pad, tile) * parts_of(row, tile);
+        if (b.dx_tile == 64 && parts_of(kCus, tiles) <= steps / 16) b.dx_tile = tile;
+    }
+    const int64_t tiles = parts_of(c.cols_pad, b.dx_tile) * parts_of(row, b.dx_tile);
+    int64_t splits = kCus * (b.dx_tile == 256 ? 1 : 2) / tiles;
+    if (splits > steps / 8) splits = steps / 8;
     if (splits < 1) splits = 1;
     b.splits = (int)splits;
     b.scale = s.take<float>(2);
@@ -374,15 +390,15 @@ int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *ds
 }
 
 template <class T, bool A_SLOW, bool B_SLOW, class E>
-int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &e, hipStream_t st, bool large) {
+int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &e, hipStream_t st, int tile) {
     Product p{a, b, (uint32_t)k, segments, 0, 0, splits};
-    const int64_t tile = large ? 256 : 128;
     p.tiles_m = (int)parts_of(a.major, tile);
     p.tiles_n = (int)parts_of(b.major, tile);
     const int64_t grid = (int64_t)p.tiles_m * p.tiles_n * splits;
     if (grid >= kMaxTiles) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
-    if (large) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
-    else product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
+    if (tile == 256) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
+    else if (tile == 128) product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
+    else product_kernel<T, A_SLOW, B_SLOW, 64, 64, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
 }
@@ -440,15 +456,14 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
         const int64_t plane_x = rows * c.cols_pad, plane_w = f.piece * c.cols_pad;
         if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, F32 ? nullptr : f.x, F32 ? f.x : nullptr, f.x_powers, plane_x, none, st));
         const Operand ox = c.pack_x ? Operand{f.x, c.cols_pad, plane_x, rows} : Operand{x, x_stride, 0, rows};
-        const bool large = large_tiles(f.piece, rows);
         for (int64_t v0 = 0; v0 < vocab; v0 += f.piece) {
             const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
             if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, F32 ? nullptr : f.w, F32 ? f.w : nullptr, f.w_powers, plane_w, none, st));
             const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
             const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, Powers{f.w_powers, f.x_powers}};
-            OPS_TRY((product<M, false, false>(ow, ox, cols, F32 ? 3 : 1, 1, ep, st, large)));
-            parts += parts_of(words, large ? 256 : 128);
+            OPS_TRY((product<M, false, false>(ow, ox, cols, F32 ? 3 : 1, 1, ep, st, f.tile)));
+            parts += parts_of(words, f.tile);
         }
         return SABER_OK;
     }));
@@ -505,17 +520,17 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
                 const Operand ox{b.x, c.cols_pad, plane_x, rows};
                 const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, Powers{b.w_powers, b.x_powers}};
                 const Operand lw = F32 ? Operand{b.w_even, c.cols_pad, plane_w, words} : ow, lx = F32 ? Operand{b.x_even, c.cols_pad, plane_x, rows} : ox;
-                OPS_TRY((product<L, false, false>(lw, lx, cols, F32 ? 3 : 1, 1, ep, st, large_tiles(words, rows))));
+                OPS_TRY((product<L, false, false>(lw, lx, cols, F32 ? 3 : 1, 1, ep, st, tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1)))));
                 if (dx) {
                     const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
                     const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};
-                    OPS_TRY((product<M, true, false>(cw, od, words, SEGMENTS, b.splits, sum, st, b.dx_large)));
+                    OPS_TRY((product<M, true, false>(cw, od, words, SEGMENTS, b.splits, sum, st, b.dx_tile)));
                 }
             }
             if (dweight) {   // (without rows: zeros)
                 const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.stride, plane_d, up(words, 8)};
                 const StoreEpilogue<T> store{dw, words, cols, scale};
-                OPS_TRY((product<M, true, true>(cx, cd, rows, SEGMENTS, 1, store, st, large_tiles(cols, words))));
+                OPS_TRY((product<M, true, true>(cx, cd, rows, SEGMENTS, 1, store, st, tile_of(cols, words, parts_of(rows, kStep) * SEGMENTS))));
             }
         }
         if (dx && rows) {
