@@ -246,6 +246,38 @@ def test_linear_cross_entropy_both_passes(rows, vocab, cols, dtype, pad, wide_ta
     assert only[0] is None and torch.equal(only[1], dw)
 
 
+# sizes whose products take the larger tiles (the ones above take the smallest): of 128 x 128 in all products, and of 256 x 256
+@pytest.mark.parametrize("rows,vocab,cols,dtype,pad", [
+    (500, 9000, 900, BF16, 0), (500, 9000, 900, F16, 3), (500, 9000, 300, F32, 0),
+    (1500, 21500, 1500, BF16, 4), (1500, 21500, 1500, F16, 0), (300, 22001, 500, F32, 0)])
+def test_linear_cross_entropy_of_many_words_and_rows(rows, vocab, cols, dtype, pad):
+    print("cross entropy", rows, vocab, cols, dtype, pad, flush=True)
+    x = dev(make(1, rows, cols + pad, dtype=dtype))[:, :cols]
+    w = dev(make(2, vocab, cols + pad, dtype=dtype, scale=1.5 / cols ** 0.5))[:, :cols]
+    t = dev(torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(3)))
+    t[rows // 2:rows // 2 + rows // 8] = -1
+    g = dev(make(4, rows).abs() + 0.1)
+    loss, lse = pk.ops.linear_cross_entropy_forward(x, w, t)
+    x64, w64, i, has, to = x.double(), w.double(), torch.arange(rows, device="cuda"), t >= 0, t.clamp(min=0)
+    logits = x64 @ w64.T
+    lse64 = torch.logsumexp(logits, 1)
+    off = (cols + 8) * E * (x64.abs() @ w64.abs().T).amax(1) + (2 ** -20 if dtype != F32 else 2 ** -22) * (1 + logits.abs().amax(1))
+    within(lse, lse64, off, "lse")
+    within(loss, torch.where(has, lse64 - logits[i, to], 0.0), 2 * off, "loss")
+    dx, dw = pk.ops.linear_cross_entropy_backward(g, x, w, t, lse)
+    d64 = (logits - lse64[:, None]).exp()
+    d64[i, to] -= 1
+    d64 *= torch.where(has, g.double(), 0.0)[:, None]
+    hold = {F32: 2.0 ** -22, F16: 2.0 ** -11, BF16: 2.0 ** -8}[dtype]
+    p = d64.abs() + 1e-30
+    p_abs = p.clone()
+    p_abs[i, to] += torch.where(has, g.double(), 0.0)
+    d_err = hold * p * 1.01 + p_abs * (4 * off[:, None] + 2 ** -20) + float(g.max()) * 2.0 ** -37
+    dx64, dw64 = d64 @ w64, d64.T @ x64
+    within(dx, dx64, ROUND[dtype] * dx64.abs() * 1.01 + TINY[dtype] + d_err @ w64.abs() + (vocab + 8) * E * (p @ w64.abs()), "dx")
+    within(dw, dw64, ROUND[dtype] * dw64.abs() * 1.01 + TINY[dtype] + d_err.T @ x64.abs() + (rows + 8) * E * (p.T @ x64.abs()), "dweight")
+
+
 def test_cross_entropy_in_several_pieces():
     """Enough rows that the vocabulary is cut: 20,000 rows leave 6,656 words a piece."""
     rows, vocab, cols = 20_000, 14_001, 40
