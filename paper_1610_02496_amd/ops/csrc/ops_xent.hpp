@@ -528,22 +528,26 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 
 // Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time, any
 // alignment, a batch ahead of its use; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its
-// words; a workgroup leaves one partial result per row.
+// words; a workgroup leaves one partial result per row.  With few words 2^share_log waves (1, 2, 4, 8) take a tile's columns in turn, so that
+// more of the weights are on their way at once; the first of them adds up what they found.
 constexpr int kFewWaves = 8;
+template <class T> constexpr int kFewBatch = sizeof(T) == 4 ? 4 : 8;   // fragments of 32 columns that a wavefront asks for at a time
 
 template <class T, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, int64_t x_stride, const T *w, int64_t w_stride, Targets target,
-                                                                   int64_t rows, int64_t vocab, int64_t cols, float2 *partial,
+                                                                   int64_t rows, int64_t vocab, int64_t cols, int share_log, float2 *partial,
                                                                    int64_t rows_pad, float *at) {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int PLANES = F32 ? 3 : 1, BATCH = F32 ? 4 : 8;
+    constexpr int PLANES = F32 ? 3 : 1, BATCH = kFewBatch<T>;
     using M = typename std::conditional<F32, bf16, T>::type;
     extern __shared__ __attribute__((aligned(16))) char few_lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
     const int pad = (int)((cols + 31) / 32 * 32), row_bytes = pad * 2 + 16, plane_bytes = (int)rows * row_bytes;
     const int64_t tiles = (vocab + 15) / 16;
-    int64_t tile = (int64_t)blockIdx.x * kFewWaves + wave;
-    int k = 0;                           // first column of the batch to come
+    const int share = 1 << share_log, k_first = (wave & (share - 1)) * 32 * BATCH, k_step = share * 32 * BATCH;
+    const int64_t next_tile = (int64_t)gridDim.x * kFewWaves >> share_log, first_tile = ((int64_t)blockIdx.x * kFewWaves + wave) >> share_log;
+    int64_t tile = k_first < pad ? first_tile : tiles;
+    int k = k_first;                     // first column of the batch to come
     Raw8<T> raw[BATCH];
     auto ask = [&] {
         const int64_t v = tile * 16 + (lane & 15);
@@ -588,15 +592,33 @@ __global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, i
         mine[j] = few_lds + (int)(n < rows ? n : rows - 1) * row_bytes + grp * 16;
         acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    auto fold = [&](int64_t v0) {   // 16 words' logits into the sums
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float top = m[j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (v0 + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
+                if (v0 + r >= vocab) acc[j][r] = -INFINITY;
+                top = fmaxf(top, acc[j][r]);
+            }
+            if (__builtin_amdgcn_ballot_w64(top > m[j])) s[j] *= m[j] == top ? 1.f : expf(m[j] - top);   // ever more rarely
+            m[j] = top;
+            const Exp<F32> power(top > -INFINITY ? top : 0.f);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[j] += power(acc[j][r]);
+            acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
     while (tile < tiles) {
         const int64_t v0 = tile * 16 + 4 * grp;
         const int k_now = k;
         Raw8<T> now[BATCH];
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) now[u] = raw[u];
-        k += 32 * BATCH;
+        k += k_step;
         const bool done = k >= pad;
-        if (done) { k = 0; tile += (int64_t)gridDim.x * kFewWaves; }
+        if (done) { k = k_first; tile += next_tile; }
         if (tile < tiles) ask();
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
@@ -615,25 +637,22 @@ __global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, i
                 }
             }
         }
-        if (!done) continue;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float top = m[j];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (v0 + r == t[j] && t[j] < vocab) at[j * 16 + (lane & 15)] = acc[j][r];
-                if (v0 + r >= vocab) acc[j][r] = -INFINITY;
-                top = fmaxf(top, acc[j][r]);
-            }
-            if (__builtin_amdgcn_ballot_w64(top > m[j])) s[j] *= m[j] == top ? 1.f : expf(m[j] - top);   // ever more rarely
-            m[j] = top;
-            const Exp<F32> power(top > -INFINITY ? top : 0.f);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[j] += power(acc[j][r]);
-            acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
+        if (done && share == 1) fold(v0);
     }
     __syncthreads();   // the features have been read: LDS is free
+    if (share > 1) {
+        f32x4 *sums = reinterpret_cast<f32x4 *>(few_lds);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[(j * kFewWaves + wave) * 64 + lane] = acc[j];
+        __syncthreads();
+        if ((wave & (share - 1)) == 0) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                for (int i = 1; i < share; ++i) acc[j] += sums[(j * kFewWaves + wave + i) * 64 + lane];
+            fold(first_tile * 16 + 4 * grp);
+        }
+        __syncthreads();
+    }
     float2 *lds = reinterpret_cast<float2 *>(few_lds);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {

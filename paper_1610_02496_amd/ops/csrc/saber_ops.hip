@@ -321,12 +321,17 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; int tile; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; int tile, share_log; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
     if (few(c)) {
-        const int64_t groups = parts_of(parts_of(c.vocab, 16), kFewWaves), each = 160 * 1024 / (few_lds(c) + 1024), most = kCus * (each > 4 ? 4 : each < 1 ? 1 : each);
+        const int64_t tiles = parts_of(c.vocab, 16), each = 160 * 1024 / (few_lds(c) + 1024), most = kCus * (each > 4 ? 4 : each < 1 ? 1 : each);
+        const int64_t batch = 32 * (c.planes == 3 ? kFewBatch<f32> : kFewBatch<bf16>);
+        // few words: wavefronts share a tile's columns, as long as that leaves no CU with two workgroups (3 rows of 1912 in f32, 1000 words:
+        // 58.9, 39.8, 28.1, 23.2 us with 1, 2, 4, 8 of them, both kernels; 16,400 words, where two would have to share a CU, 69.9 and 82.2)
+        for (f.share_log = 0; 1 << f.share_log < kFewWaves && parts_of(tiles << (f.share_log + 1), kFewWaves) <= kCus && batch << f.share_log < c.cols;) ++f.share_log;
+        const int64_t groups = parts_of(tiles << f.share_log, kFewWaves);
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
         const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 64) * 64;   // words that one launch takes
@@ -413,10 +418,10 @@ int check_targets(const char *who, const void *target, int target64) {
 
 template <class T, int NT>
 int launch_few(const Xent &c, const ForwardSpace &f, Targets t, hipStream_t st) {
-    const int64_t least = kFewWaves * NT * 128, lds = few_lds(c) > least ? few_lds(c) : least;   // the wavefronts' results at the end
+    const int64_t least = kFewWaves * NT * (f.share_log ? 1024 : 128), lds = few_lds(c) > least ? few_lds(c) : least;   // the wavefronts' results at the end
     const auto kernel = score_few_kernel<T, NT>;
     if (lds > 64 * 1024) OPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<(unsigned)f.few_grid, kFewWaves * 64, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.partial, f.rows_pad, f.at);
+    kernel<<<(unsigned)f.few_grid, kFewWaves * 64, (size_t)lds, st>>>(static_cast<const T *>(c.x), c.x_stride, static_cast<const T *>(c.w), c.w_stride, t, c.rows, c.vocab, c.cols, f.share_log, f.partial, f.rows_pad, f.at);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
 }
