@@ -368,32 +368,32 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_str
 
 // The same for binary32, a row per wavefront, with a second form for the logits: the row times the power of two that brings its largest
 // finite value to 2^14 .. 2^15, in two planes of binary16 (x = x1 + x2 to 2^-24 of it, and to 2^-40 of the row's largest); the
-// power that undoes it goes to `powers`.  Either form may be left out.
-__global__ __launch_bounds__(256) void pack32_kernel(const float *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride,
-                                                     int64_t plane, uint16_t *even, int *powers, Targets mask) {
+// power that undoes it goes to `powers`.  The planes may be left out.  One launch packs features and projection, one after the other.
+struct Rows32 { const float *src; int64_t src_stride, rows; uint16_t *dst; int64_t plane; uint16_t *even; int *powers; Targets mask; };
+__global__ __launch_bounds__(256) void pack32_kernel(Rows32 x, Rows32 w, int64_t cols, int64_t stride) {
     const int lane = threadIdx.x & 63;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
-        const float *from = src + row * src_stride;
-        const int64_t have = mask.p && mask.at(row) < 0 ? 0 : cols;
-        float up = 1.f;
-        if (even) {
-            uint32_t top = 0;
-            for (int64_t c = lane * 8; c < stride; c += 512) {
-                const Raw8<f32> r = load_raw8(from + c, have - c);
+    for (int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); at < x.rows + w.rows; at += (int64_t)gridDim.x * 4) {
+        const bool first = at < x.rows;
+        const int64_t row = first ? at : at - x.rows, plane = first ? x.plane : w.plane;
+        uint16_t *const dst = first ? x.dst : w.dst, *const even = first ? x.even : w.even;
+        const float *const from = first ? x.src + row * x.src_stride : w.src + row * w.src_stride;
+        const int64_t have = first && x.mask.p && x.mask.at(row) < 0 ? 0 : cols;
+        uint32_t top = 0;
+        for (int64_t c = lane * 8; c < stride; c += 512) {
+            const Raw8<f32> r = load_raw8(from + c, have - c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t b = r.v[i] & 0x7fffffffu;
-                    top = max(top, b < 0x7f800000u ? b : 0u);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t b = r.v[i] & 0x7fffffffu;
+                top = max(top, b < 0x7f800000u ? b : 0u);
             }
-            top = row_max(top);
-            top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
-                      max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
-            int e = 14 - ((int)(top >> 23) - 127);         // (kept within the normal numbers)
-            e = top == 0 ? 0 : e > 126 ? 126 : e;
-            up = __uint_as_float((uint32_t)(e + 127) << 23);
-            if (lane == 0) powers[row] = -e;
         }
+        top = row_max(top);
+        top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
+                  max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
+        int e = 14 - ((int)(top >> 23) - 127);         // (kept within the normal numbers)
+        e = top == 0 ? 0 : e > 126 ? 126 : e;
+        const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+        if (lane == 0) (first ? x.powers : w.powers)[row] = -e;
         for (int64_t c = lane * 8; c < stride; c += 512) {
             const Raw8<f32> r = load_raw8(from + c, have - c);
             if (dst) {
@@ -402,17 +402,15 @@ __global__ __launch_bounds__(256) void pack32_kernel(const float *src, int64_t s
 #pragma unroll
                 for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(dst + q * plane + row * stride + c) = o[q];
             }
-            if (even) {
-                union { f16 t[8]; u32x4 u; } hi, lo;
+            union { f16 t[8]; u32x4 u; } hi, lo;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float v = __uint_as_float(r.v[i]) * up;
-                    hi.t[i] = (f16)v;
-                    lo.t[i] = fabsf(v) < INFINITY ? (f16)(v - (float)hi.t[i]) : (f16)0.f;
-                }
-                *reinterpret_cast<u32x4 *>(even + row * stride + c) = hi.u;
-                *reinterpret_cast<u32x4 *>(even + plane + row * stride + c) = lo.u;
+            for (int i = 0; i < 8; ++i) {
+                const float v = __uint_as_float(r.v[i]) * up;
+                hi.t[i] = (f16)v;
+                lo.t[i] = fabsf(v) < INFINITY ? (f16)(v - (float)hi.t[i]) : (f16)0.f;
             }
+            *reinterpret_cast<u32x4 *>(even + row * stride + c) = hi.u;
+            *reinterpret_cast<u32x4 *>(even + plane + row * stride + c) = lo.u;
         }
     }
 }

@@ -382,14 +382,16 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
     return b;
 }
 
-// dst: the planes of the gradients' products (of 16-bit types the only form); even, powers: of the logits'
 template <class T>
-int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, uint16_t *even, int *powers, int64_t plane, Targets mask, hipStream_t st) {
+int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, Targets mask, hipStream_t st) {
     const int64_t y = parts_of(rows, 4);
-    if constexpr (std::is_same<T, f32>::value)
-        pack32_kernel<<<(unsigned)(y < 16 * kCus ? y : 16 * kCus), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, plane, even, powers, mask);
-    else
-        pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, mask);
+    pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, mask);
+    OPS_HIP(hipGetLastError());
+    return SABER_OK;
+}
+int pack32(const Rows32 &x, const Rows32 &w, const Xent &c, hipStream_t st) {
+    const int64_t groups = parts_of(x.rows + w.rows, 4);
+    pack32_kernel<<<(unsigned)(groups < 16 * kCus ? groups : 16 * kCus), 256, 0, st>>>(x, w, c.cols, c.cols_pad);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
 }
@@ -459,12 +461,16 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
         }
         const Targets none{nullptr, 0};
         const int64_t plane_x = rows * c.cols_pad, plane_w = f.piece * c.cols_pad;
-        if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, F32 ? nullptr : f.x, F32 ? f.x : nullptr, f.x_powers, plane_x, none, st));
+        if constexpr (!F32)
+            if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, f.x, none, st));
         const Operand ox = c.pack_x ? Operand{f.x, c.cols_pad, plane_x, rows} : Operand{x, x_stride, 0, rows};
         for (int64_t v0 = 0; v0 < vocab; v0 += f.piece) {
             const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
-            if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, F32 ? nullptr : f.w, F32 ? f.w : nullptr, f.w_powers, plane_w, none, st));
+            if constexpr (F32)
+                OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, nullptr, plane_x, f.x, f.x_powers, none},
+                               Rows32{w0, w_stride, words, nullptr, plane_w, f.w, f.w_powers, none}, c, st));
+            else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, none, st));
             const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
             const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, Powers{f.w_powers, f.x_powers}};
             OPS_TRY((product<M, false, false>(ow, ox, cols, F32 ? 3 : 1, 1, ep, st, f.tile)));
@@ -508,8 +514,8 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
         const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.stride;
         const float *scale = nullptr;
         if (rows) {
-            OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, b.x_even, b.x_powers, plane_x, t, st));
-            if (!F32) {   // (three planes keep all bits)
+            if constexpr (!F32) {   // (three planes keep all bits)
+                OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, t, st));
                 grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, std::is_same<T, f16>::value ? 0x1p14f : 1.f, b.scale);
                 OPS_HIP(hipGetLastError());
                 scale = b.scale;
@@ -520,7 +526,10 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
             T *dw = dweight ? static_cast<T *>(dweight) + v0 * cols : nullptr;
             if (rows) {
-                if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, b.w_even, b.w_powers, plane_w, Targets{nullptr, 0}, st));
+                if constexpr (F32)
+                    OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, t},
+                                   Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, Targets{nullptr, 0}}, c, st));
+                else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, Targets{nullptr, 0}, st));
                 const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
                 const Operand ox{b.x, c.cols_pad, plane_x, rows};
                 const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, Powers{b.w_powers, b.x_powers}};
