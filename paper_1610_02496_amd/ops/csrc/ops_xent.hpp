@@ -527,7 +527,8 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 // Up to 16 NT rows: W is read once from memory straight into the matrix cores' operand registers, 16 words by 32 columns at a time, any
 // alignment, a batch ahead of its use; the rows' features stay in LDS.  Every wave keeps a running maximum and sum for its
 // words; a workgroup leaves one partial result per row.  With few words 2^share_log waves (1, 2, 4, 8) take a tile's columns in turn, so that
-// more of the weights are on their way at once; the first of them adds up what they found.
+// more of the weights are on their way at once; the first of them adds up what they found.  Bound by memory: one row of 1024 in bf16 and
+// 100,000 words (205 MB) 42 us, 4.9 TB/s; 61 rows of 777 in f16 and 30,011 words (47 MB, no row aligned) 27 us, the loads' latency and number.
 constexpr int kFewWaves = 8;
 template <class T> constexpr int kFewBatch = sizeof(T) == 4 ? 4 : 8;   // fragments of 32 columns that a wavefront asks for at a time
 

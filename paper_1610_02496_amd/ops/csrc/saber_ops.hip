@@ -63,8 +63,9 @@ int check_pointer(const char *who, const char *what, const void *p, size_t align
 // ---- layer norm --------------------------------------------------------------------------------------------------------------
 
 // Rows of up to 1,024 columns belong to a wavefront, up to 4,096 to a workgroup of 256, up to 8,192 to one of 512: a lane has 16
-// elements of a row at most, so that the row after can be on its way (the backward pass with 32 a lane: 250 registers, a
-// wavefront per SIMD).  Wider ones are read again for every sum.
+// elements of a row at most, so that the row after can be on its way.  Measured in us, forward and backward: 16,384 x 1024 in bf16 with
+// the checkpoint, a wavefront 24 and 21, a workgroup 32 and 28; 65,536 x 2048 in f16, a workgroup 98 and 157, a wavefront (32 elements a
+// lane) 92 and 163, more in all with the partial sums.  Wider ones are read again for every sum.
 constexpr int64_t kNormCols = 8192;
 
 template <class F>
@@ -78,7 +79,7 @@ int with_norm_shape(int64_t cols, F &&f) {
     return f(GG{}, C2{});
 }
 int64_t rows_per_group(int64_t cols) { return cols <= 1024 ? 4 : 1; }
-// workgroups of the backward pass: each leaves a partial row of both sums
+// workgroups of the backward pass, as many as the CUs hold at a time: each leaves a partial row of both sums
 int64_t norm_parts(int64_t rows, int64_t cols) {
     if (cols > kNormCols) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
     const int64_t groups = parts_of(rows > 0 ? rows : 1, rows_per_group(cols)), most = (cols <= 1024 ? 3 : cols <= 4096 ? 4 : 2) * kCus;
@@ -234,6 +235,11 @@ extern "C" int saber_checkpoint8_restore(const int8_t *q, const float *scale, in
 
 namespace {
 
+// Up to 64 rows whose features fit LDS go through the kernel for few rows.  It reads the projection as it lies where the products would
+// have it packed first (us of few rows and of products: 61 rows of 777 in f16, 30,011 words, 31 and 39; 1 row of 2048 in f32, 100,000
+// words, 263 and 654), and shares out long rows of few words (9 rows in bf16: 2048 columns of 1000 words 15.8 and 23.0, 1024 of 30,000
+// 25.4 and 28.4).  Where a 16-bit projection lies well and is large the two are alike, within a sixth (1024 of 100,000 82.6 and 83.4, 2048
+// of 100,000 149 and 129).
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewLds = 150 * 1024;
 // values of d, and of packed words, per piece: 256 MB of a 16-bit type, what the last-level cache holds; 768 MB of three planes (binary32
