@@ -109,6 +109,13 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
     return v;
 }
 
+// the same over the whole wavefront
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = row_max(v);
+    return max(max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16)),
+               max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
+}
+
 // One lane's chunk of a block of 128 columns, in 8 bits: step c = max|x| / 127 of the block, whole numbers round(x / c), ties to
 // even.  A block of zeros has step 0.  A NaN or an infinity makes the step not finite: the block is restored as NaN.
 // All 16 lanes of the block call this together.

@@ -16,8 +16,9 @@
 //
 // Operands of binary32 come as planes, and the products of planes that matter are added as further steps along k ("segments"):
 //   three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each), six segments, any range of values;
-//   two planes of binary16, x = x1 + x2 to 2^-24, three segments, for operands whose rows were brought to one magnitude.
-// What is left out is below 2^-23 of the product of two magnitudes.
+//   two planes of binary16, x = x1 + x2 to 2^-23, three segments, for operands whose rows were brought to one magnitude and hold little
+//   that is far below it; what is left out is up to 2^-22 of the product of two magnitudes.  Tiles of other rows are left to another
+//   kernel.
 #pragma once
 #include <type_traits>
 #include <utility>
@@ -201,8 +202,31 @@ struct Reader {
     }
 };
 
-template <class T, bool A_SLOW, bool B_SLOW, int BM, int BN, int WM, int WN, class Epilogue>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilogue e) {
+// Workgroups go round the eight XCDs; each XCD gets a run of neighbouring tiles, eight of n by all of m, so that what its
+// workgroups read at a time meets in its L2.
+__device__ __forceinline__ void tile_of_workgroup(const Product &p, uint32_t id, int &split, int &tm, int &tn) {
+    const uint32_t plane_tiles = (uint32_t)p.tiles_m * p.tiles_n, tiles = plane_tiles * p.splits;
+    {
+        const uint32_t each = tiles / 8, more = tiles % 8, x = id % 8;
+        id = x * each + (x < more ? x : more) + id / 8;
+    }
+    split = (int)(id / plane_tiles);
+    id -= split * plane_tiles;
+    const int group = (int)(id / (p.tiles_m * 8u));
+    const int width = p.tiles_n - group * 8 < 8 ? p.tiles_n - group * 8 : 8;
+    const int in_group = (int)(id - group * (p.tiles_m * 8u));
+    tm = in_group / width;
+    tn = group * 8 + in_group % width;
+}
+
+// the tiles that a product leaves to another kernel
+struct None {
+    template <int BM, int BN>
+    __device__ __forceinline__ bool has(int64_t, int64_t, int64_t, int64_t, int) const { return false; }
+};
+
+template <class T, bool A_SLOW, bool B_SLOW, int BM, int BN, int WM, int WN, class Epilogue, class LeftOut>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilogue e, LeftOut left_out) {
 #if defined(__HIP_DEVICE_COMPILE__)   // (the host pass knows neither the matrix instructions nor their types)
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int U = BM < 128 ? BM : 128, kUnitBytes = U * kStep * 2;
@@ -212,21 +236,10 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Epilog
     LdsBytes *const lds = (LdsBytes *)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    // Workgroups go round the eight XCDs; each XCD gets a run of neighbouring tiles, eight of n by all of m, so that what its
-    // workgroups read at a time meets in its L2.
-    const uint32_t plane_tiles = (uint32_t)p.tiles_m * p.tiles_n, tiles = plane_tiles * p.splits;
-    uint32_t id = blockIdx.x;
-    {
-        const uint32_t each = tiles / 8, more = tiles % 8, x = id % 8;
-        id = x * each + (x < more ? x : more) + id / 8;
-    }
-    const int split = (int)(id / plane_tiles);
-    id -= split * plane_tiles;
-    const int group = (int)(id / (p.tiles_m * 8u));
-    const int width = p.tiles_n - group * 8 < 8 ? p.tiles_n - group * 8 : 8;
-    const int in_group = (int)(id - group * (p.tiles_m * 8u));
-    const int tm = in_group / width, tn = group * 8 + in_group % width;
+    int split, tm, tn;
+    tile_of_workgroup(p, blockIdx.x, split, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    if (left_out.template has<BM, BN>(m0, n0, p.a.major, p.b.major, lane)) return;
 
     Loader<A_SLOW, BM, U, WAVES> la;
     Loader<B_SLOW, BN, U, WAVES> lb;

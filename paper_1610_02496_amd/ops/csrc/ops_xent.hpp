@@ -77,6 +77,108 @@ __device__ __forceinline__ float groups_sum(float v) {
 // Rows of binary32 are multiplied after they were brought to one magnitude: the sums' powers of two, of the words and of the rows.
 struct Powers { const int *words, *rows; };
 
+__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+
+// The logits' tiles of binary32 whose rows the two planes do not hold.  A value is held to 2^-23 of itself, but no better than to 2^-25
+// after the row's power of two (the steps of binary16 end there), so a logit is off by up to 2^-25 (2^px sum|W| + 2^pw sum|x|) more than
+// by its products' roundings: up to 2^-22 is left as it is, next to the rounding of a binary32 sum.  Rows whose values are all of one
+// magnitude, as a norm gives them, stay a thousand times below that.  Beyond (a count of 10^6 next to features of 1; rows that hold an
+// infinity or NaN, whose sum stands as infinite) the tile is computed from the operands themselves by products in binary32, right for all
+// values, infinities included.  2,048 rows of 512 and 60,000 words, forward: 0.50 ms with planes, 1.43 ms where every tile is such a
+// one (130 TFLOP/s in binary32).
+struct Direct32 {
+    const float *a; int64_t a_stride;    // words
+    const float *b; int64_t b_stride;    // rows
+    const float *a_sums, *b_sums;        // of magnitudes, per row; infinite where they are not finite
+    Powers powers;
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool has(int64_t m0, int64_t n0, int64_t words, int64_t rows, int lane) const {
+        uint32_t a_power = 0, b_power = 0, a_sum = 0, b_sum = 0;   // (sums as bits: magnitudes keep their order)
+#pragma unroll
+        for (int i = 0; i < BM; i += 64)
+            if (m0 + i + lane < words) {
+                a_power = max(a_power, (uint32_t)(powers.words[m0 + i + lane] + 512));
+                a_sum = max(a_sum, __float_as_uint(a_sums[m0 + i + lane]));
+            }
+#pragma unroll
+        for (int i = 0; i < BN; i += 64)
+            if (n0 + i + lane < rows) {
+                b_power = max(b_power, (uint32_t)(powers.rows[n0 + i + lane] + 512));
+                b_sum = max(b_sum, __float_as_uint(b_sums[n0 + i + lane]));
+            }
+        a_power = wave_max(a_power); b_power = wave_max(b_power); a_sum = wave_max(a_sum); b_sum = wave_max(b_sum);
+        const float off = ldexpf(__uint_as_float(a_sum), (int)b_power - 512) + ldexpf(__uint_as_float(b_sum), (int)a_power - 512);
+        return !(off <= 8.f);
+    }
+
+    // Four values of k per lane group and turn, straight from memory, into sums of words from m on and of rows from n on.  A lane past the
+    // last one takes the last one's values, which the epilogue does not use.
+    template <int TM, int TN>
+    __device__ __forceinline__ void run(f32x4 (&acc)[TM][TN], int64_t m, int64_t n, int64_t words, int64_t rows, int64_t cols, int lane) const {
+        const float *pa[TM], *pb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) pa[i] = a + last(m + i * 16 + (lane & 15), words) * a_stride + 4 * (lane >> 4);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) pb[j] = b + last(n + j * 16 + (lane & 15), rows) * b_stride + 4 * (lane >> 4);
+#pragma unroll 1
+        for (int64_t k = 0; k < cols; k += 16) {
+            const int64_t left = k + 16 <= cols ? 4 : cols - k - 4 * (lane >> 4);
+            f32x4 fa[TM], fb[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[i] = load4(pa[i] + k, left);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = load4(pb[j] + k, left);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma4(fa[i][r], fb[j][r], acc[i][j]);
+        }
+    }
+
+private:
+    static __device__ __forceinline__ int64_t last(int64_t at, int64_t of) { return at < of ? at : of - 1; }
+    // the first n of four elements, zeros for the others
+    static __device__ __forceinline__ f32x4 load4(const float *p, int64_t n) {
+        struct __attribute__((packed, aligned(4))) Four { f32x4 v; };
+        if (n >= 4) return reinterpret_cast<const Four *>(p)->v;
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : 0.f;
+        return v;
+    }
+};
+
+// Those tiles, in the numbering of the product that leaves them out; the others' workgroups end at once.
+template <int BM, int BN, int WM, int WN, class Epilogue>
+__global__ __launch_bounds__(WM * WN * 64) void direct32_kernel(Product p, Epilogue e, Direct32 tiles) {
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    __shared__ float2 lds[WM * BN];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int split, tm, tn;
+    tile_of_workgroup(p, blockIdx.x, split, tm, tn);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    if (!tiles.template has<BM, BN>(m0, n0, p.a.major, p.b.major, lane)) return;
+    const int wm = (wave / WN) * TM * 16, wn = (wave % WN) * TN * 16;
+    typename Epilogue::template State<TN> state;
+    e.prepare(state, n0 + wn + (lane & 15));
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    tiles.run(acc, m0 + wm, n0 + wn, p.a.major, p.b.major, p.k, lane);
+    e.template finish<BM, BN, WM, WN, false>(acc, state, m0, n0, wm, wn, lane, wave, split, tm, (void *)lds);
+}
+
 // A column's target relative to the tile, clipped to -1 and what a tile cannot hold.
 __device__ __forceinline__ int within_tile(int64_t target, int64_t first_word) {
     const int64_t t = target - first_word;
@@ -114,13 +216,13 @@ struct ScoreEpilogue {
             if constexpr (EXACT) s.power[j] = n + j * 16 < rows ? powers.rows[n + j * 16] : 0;
         }
     }
-    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    template <int BM, int BN, int WM, int WN, bool SCALED = true, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int wave,
                                            int, int tm, void *lds) const {
         float2 *join_lds = static_cast<float2 *>(lds);
         const int first = wm + 4 * (lane >> 4);
         const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;   // words of this lane's rows that exist
-        if constexpr (EXACT) scale_sums(acc, st.power, powers.words + m0 + first, left);
+        if constexpr (EXACT && SCALED) scale_sums(acc, st.power, powers.words + m0 + first, left);
         if (words - m0 < BM) {   // (the vocabulary's last tile alone)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
@@ -189,14 +291,14 @@ struct GradEpilogue {
             if constexpr (PLANES == 3) s.power[j] = row ? powers.rows[n + j * 16] : 0;
         }
     }
-    template <int BM, int BN, int WM, int WN, int TM, int TN>
+    template <int BM, int BN, int WM, int WN, bool SCALED = true, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &st, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int,
                                            void *) const {
         const int first = wm + 4 * (lane >> 4);
         const int left = (int)(words - m0 < BM ? words - m0 : BM) - first;
         const int out0 = wm + paired_row(lane), room = (int)(stride - m0 < BM ? stride - m0 : BM) - out0;
         const bool whole = words - m0 >= BM;                                 // all but the vocabulary's last tile
-        if constexpr (PLANES == 3) scale_sums(acc, st.power, powers.words + m0 + first, left);
+        if constexpr (PLANES == 3 && SCALED) scale_sums(acc, st.power, powers.words + m0 + first, left);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn + j * 16 + (lane & 15);
@@ -367,9 +469,10 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_str
 }
 
 // The same for binary32, a row per wavefront, with a second form for the logits: the row times the power of two that brings its largest
-// finite value to 2^14 .. 2^15, in two planes of binary16 (x = x1 + x2 to 2^-24 of it, and to 2^-40 of the row's largest); the
-// power that undoes it goes to `powers`.  The planes may be left out.  One launch packs features and projection, one after the other.
-struct Rows32 { const float *src; int64_t src_stride, rows; uint16_t *dst; int64_t plane; uint16_t *even; int *powers; Targets mask; };
+// finite value to 2^14 .. 2^15, in two planes of binary16 (x = x1 + x2 to 2^-23 of it, or to 2^-40 of the row's largest where that is
+// more); the power that undoes it goes to `powers`, the sum of magnitudes to `sums`, from which a tile sees whether that is enough.  The
+// planes may be left out.  One launch packs features and projection, one after the other.
+struct Rows32 { const float *src; int64_t src_stride, rows; uint16_t *dst; int64_t plane; uint16_t *even; int *powers; float *sums; Targets mask; };
 __global__ __launch_bounds__(256) void pack32_kernel(Rows32 x, Rows32 w, int64_t cols, int64_t stride) {
     const int lane = threadIdx.x & 63;
     for (int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); at < x.rows + w.rows; at += (int64_t)gridDim.x * 4) {
@@ -379,21 +482,25 @@ __global__ __launch_bounds__(256) void pack32_kernel(Rows32 x, Rows32 w, int64_t
         const float *const from = first ? x.src + row * x.src_stride : w.src + row * w.src_stride;
         const int64_t have = first && x.mask.p && x.mask.at(row) < 0 ? 0 : cols;
         uint32_t top = 0;
+        float sum = 0.f;
         for (int64_t c = lane * 8; c < stride; c += 512) {
             const Raw8<f32> r = load_raw8(from + c, have - c);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t b = r.v[i] & 0x7fffffffu;
                 top = max(top, b < 0x7f800000u ? b : 0u);
+                sum += __uint_as_float(b);
             }
         }
-        top = row_max(top);
-        top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
-                  max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
-        int e = 14 - ((int)(top >> 23) - 127);         // (kept within the normal numbers)
-        e = top == 0 ? 0 : e > 126 ? 126 : e;
+        top = wave_max(top);
+        sum = wave_sum(sum);
+        int e = 14 - ((int)(top >> 23) - 127);         // (kept within the normal numbers; a row of zeros has the smallest power)
+        e = e > 126 ? 126 : e;
         const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-        if (lane == 0) (first ? x.powers : w.powers)[row] = -e;
+        if (lane == 0) {
+            (first ? x.powers : w.powers)[row] = -e;
+            (first ? x.sums : w.sums)[row] = sum < INFINITY ? sum : INFINITY;   // (of a NaN as well)
+        }
         for (int64_t c = lane * 8; c < stride; c += 512) {
             const Raw8<f32> r = load_raw8(from + c, have - c);
             if (dst) {

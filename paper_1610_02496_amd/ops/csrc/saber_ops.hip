@@ -327,7 +327,7 @@ struct Carve {   // a work space handed out piece by piece; base null: only coun
     }
 };
 
-struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; int64_t piece, parts, rows_pad, few_grid; int tile, share_log; };
+struct ForwardSpace { float2 *partial; float *at; uint16_t *x, *w; int *x_powers, *w_powers; float *x_sums, *w_sums; int64_t piece, parts, rows_pad, few_grid; int tile, share_log; };
 ForwardSpace forward_space(const Xent &c, Carve &s) {
     ForwardSpace f{};
     f.rows_pad = up(c.rows, 16);
@@ -348,14 +348,19 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
         const int planes = c.planes == 3 ? 2 : 1;   // (the logits' form)
         if (c.pack_x) f.x = s.take<uint16_t>(c.rows * c.cols_pad * planes);
         if (c.pack_w) f.w = s.take<uint16_t>(f.piece * c.cols_pad * planes);
-        if (planes == 2) { f.x_powers = s.take<int>(c.rows); f.w_powers = s.take<int>(f.piece); }
+        if (planes == 2) {
+            f.x_powers = s.take<int>(c.rows);
+            f.w_powers = s.take<int>(f.piece);
+            f.x_sums = s.take<float>(c.rows);
+            f.w_sums = s.take<float>(f.piece);
+        }
     }
     f.partial = s.take<float2>(f.parts * f.rows_pad);
     f.at = s.take<float>(f.rows_pad);
     return f;
 }
 
-struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *sums; int64_t piece, stride; int splits, dx_tile; };
+struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *x_sums, *w_sums, *sums; int64_t piece, stride; int splits, dx_tile; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
     const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / row, most_w = kPieceValues / c.cols_pad;
@@ -381,6 +386,8 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
         b.w_even = s.take<uint16_t>(b.piece * c.cols_pad * 2);
         b.x_powers = s.take<int>(c.rows);
         b.w_powers = s.take<int>(b.piece);
+        b.x_sums = s.take<float>(c.rows);
+        b.w_sums = s.take<float>(b.piece);
     }
     b.stride = up(b.piece, 64) | 64;
     b.d = s.take<uint16_t>(c.rows * b.stride * c.planes);
@@ -402,17 +409,23 @@ int pack32(const Rows32 &x, const Rows32 &w, const Xent &c, hipStream_t st) {
     return SABER_OK;
 }
 
-template <class T, bool A_SLOW, bool B_SLOW, class E>
-int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &e, hipStream_t st, int tile) {
+template <class T, bool A_SLOW, bool B_SLOW, class E, class LeftOut = None>
+int product(Operand a, Operand b, int64_t k, int segments, int splits, const E &e, hipStream_t st, int tile, const LeftOut &left_out = LeftOut{}) {
     Product p{a, b, (uint32_t)k, segments, 0, 0, splits};
     p.tiles_m = (int)parts_of(a.major, tile);
     p.tiles_n = (int)parts_of(b.major, tile);
     const int64_t grid = (int64_t)p.tiles_m * p.tiles_n * splits;
     if (grid >= kMaxTiles) return fail(SABER_ERANGE, "a product of %lld tiles", (long long)grid);
-    if (tile == 256) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
-    else if (tile == 128) product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
-    else product_kernel<T, A_SLOW, B_SLOW, 64, 64, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e);
+    if (tile == 256) product_kernel<T, A_SLOW, B_SLOW, 256, 256, 2, 2, E, LeftOut><<<(unsigned)grid, 256, 0, st>>>(p, e, left_out);
+    else if (tile == 128) product_kernel<T, A_SLOW, B_SLOW, 128, 128, 2, 2, E, LeftOut><<<(unsigned)grid, 256, 0, st>>>(p, e, left_out);
+    else product_kernel<T, A_SLOW, B_SLOW, 64, 64, 2, 2, E, LeftOut><<<(unsigned)grid, 256, 0, st>>>(p, e, left_out);
     OPS_HIP(hipGetLastError());
+    if constexpr (std::is_same<LeftOut, Direct32>::value) {
+        if (tile == 256) direct32_kernel<256, 256, 4, 2, E><<<(unsigned)grid, 512, 0, st>>>(p, e, left_out);
+        else if (tile == 128) direct32_kernel<128, 128, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e, left_out);
+        else direct32_kernel<64, 64, 2, 2, E><<<(unsigned)grid, 256, 0, st>>>(p, e, left_out);
+        OPS_HIP(hipGetLastError());
+    }
     return SABER_OK;
 }
 
@@ -474,12 +487,17 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
             const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
             if constexpr (F32)
-                OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, nullptr, plane_x, f.x, f.x_powers, none},
-                               Rows32{w0, w_stride, words, nullptr, plane_w, f.w, f.w_powers, none}, c, st));
+                OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, nullptr, plane_x, f.x, f.x_powers, f.x_sums, none},
+                               Rows32{w0, w_stride, words, nullptr, plane_w, f.w, f.w_powers, f.w_sums, none}, c, st));
             else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, none, st));
             const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
-            const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, Powers{f.w_powers, f.x_powers}};
-            OPS_TRY((product<M, false, false>(ow, ox, cols, F32 ? 3 : 1, 1, ep, st, f.tile)));
+            const Powers powers{f.w_powers, f.x_powers};
+            const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, powers};
+            if constexpr (F32) {
+                const Direct32 direct{w0, w_stride, static_cast<const T *>(x), x_stride, f.w_sums, f.x_sums, powers};
+                OPS_TRY((product<M, false, false>(ow, ox, cols, 3, 1, ep, st, f.tile, direct)));
+            } else
+                OPS_TRY((product<M, false, false>(ow, ox, cols, 1, 1, ep, st, f.tile)));
             parts += parts_of(words, f.tile);
         }
         return SABER_OK;
@@ -533,14 +551,20 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
             T *dw = dweight ? static_cast<T *>(dweight) + v0 * cols : nullptr;
             if (rows) {
                 if constexpr (F32)
-                    OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, t},
-                                   Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, Targets{nullptr, 0}}, c, st));
+                    OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, b.x_sums, t},
+                                   Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, b.w_sums, Targets{nullptr, 0}}, c, st));
                 else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, Targets{nullptr, 0}, st));
                 const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
                 const Operand ox{b.x, c.cols_pad, plane_x, rows};
-                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, Powers{b.w_powers, b.x_powers}};
-                const Operand lw = F32 ? Operand{b.w_even, c.cols_pad, plane_w, words} : ow, lx = F32 ? Operand{b.x_even, c.cols_pad, plane_x, rows} : ox;
-                OPS_TRY((product<L, false, false>(lw, lx, cols, F32 ? 3 : 1, 1, ep, st, tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1)))));
+                const Powers powers{b.w_powers, b.x_powers};
+                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, powers};
+                const int tile = tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1));
+                if constexpr (F32) {
+                    const Operand lw{b.w_even, c.cols_pad, plane_w, words}, lx{b.x_even, c.cols_pad, plane_x, rows};
+                    const Direct32 direct{w0, w_stride, static_cast<const T *>(x), x_stride, b.w_sums, b.x_sums, powers};
+                    OPS_TRY((product<L, false, false>(lw, lx, cols, 3, 1, ep, st, tile, direct)));
+                } else
+                    OPS_TRY((product<L, false, false>(ow, ox, cols, 1, 1, ep, st, tile)));
                 if (dx) {
                     const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
                     const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};

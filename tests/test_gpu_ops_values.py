@@ -1,0 +1,134 @@
+"""The head's operators on the GPU over the values that a program may bring: rows of mixed magnitudes, infinities, gradients of very
+different size, sizes at which every loop takes a second turn.  Against plain implementations in 64 bits."""
+import pytest
+import torch
+
+import paper_1610_02496_amd as pk
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+ROUND = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}
+E = 2.0 ** -24
+
+
+def normal(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def words(seed, rows, vocab):
+    return torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(seed))
+
+
+def within(got, want, bound, what):
+    got, want = got.double().cpu(), want.double().cpu()
+    bound = (bound if isinstance(bound, torch.Tensor) else torch.tensor(float(bound))).double().cpu()
+    assert got.shape == want.shape, what
+    off = (got - want).abs()
+    bad = ~(off <= bound)
+    assert not bool(bad.any()), "%s: %d of %d values, worst %.3g against a bound of %.3g" % (
+        what, int(bad.sum()), bad.numel(), float(off[bad].max()), float(bound.expand_as(off)[bad].min()))
+
+
+def xent64(x, w, t, g):
+    """On the operands' device, which is where sizes are large."""
+    x, w = x.double(), w.double()
+    logits = torch.mm(x, w.t())
+    lse = torch.logsumexp(logits, 1)
+    i, has, to = torch.arange(len(t), device=x.device), t >= 0, t.clamp(min=0)
+    loss = torch.where(has, lse - logits[i, to], 0.0)
+    d = (logits - lse[:, None]).exp()
+    d[i, to] -= 1
+    d *= torch.where(has, g.double(), 0.0)[:, None]
+    return loss, lse, d, logits
+
+
+def rounding(x, w, logits):
+    """What a logit in binary32 may be off: the roundings of its sum walk at random, so that four standard deviations of
+    sqrt(columns) steps of 2^-24 of the sum of magnitudes hold, and the exponentials add 2^-22 of the logit's size."""
+    mag = torch.mm(x.double().abs(), w.double().abs().t())
+    return 4 * (x.shape[1] + 8) ** 0.5 * E * mag.amax(1) + 2 ** -22 * (1 + logits.abs().amax(1))
+
+
+def both_passes32(x, w, t, g):
+    """Forward and backward pass in binary32 on the GPU against 64 bits."""
+    x, w, t, g = x.to("cuda", F32), w.to("cuda", F32), t.cuda(), g.to("cuda", F32)
+    loss, lse = pk.ops.linear_cross_entropy_forward(x, w, t)
+    loss64, lse64, d, logits = xent64(x, w, t, g)
+    off = rounding(x, w, logits)
+    within(lse, lse64, off, "lse")
+    within(loss, loss64, 2 * off, "loss")
+    dx, dw = pk.ops.linear_cross_entropy_backward(g, x, w, t, lse)
+    p = d.abs()
+    p[torch.arange(len(t), device="cuda"), t.clamp(min=0)] += torch.where(t >= 0, g.double(), 0.0)
+    d_err = p * (4 * off[:, None] + 2 ** -20)
+    x64, w64 = x.double(), w.double()
+    for got, d64, err, other, what in ((dx, d, d_err, w64, "dx"), (dw, d.t().contiguous(), d_err.t().contiguous(), x64, "dweight")):
+        want, sums = torch.mm(d64, other), torch.mm(d64.abs(), other.abs())
+        within(got, want, torch.mm(err, other.abs()) + 4 * (d64.shape[1] + 8) ** 0.5 * E * sums + E * want.abs() + 1e-37, what)
+
+
+MIXED = {
+    "one magnitude": lambda x, w: None,
+    "a large column without weight": lambda x, w: (x[:, 3].mul_(1e8), w[:, 3].zero_()),
+    "a large column of small weight": lambda x, w: (x[:, 3].mul_(1e8), w[:, 3].mul_(1e-8)),
+    "a very large column without weight": lambda x, w: (x[:, 3].mul_(1e10), w[:, 3].zero_()),
+    "an unused column that hides all others": lambda x, w: (x[:, 3].fill_(1e30), w[:, 3].zero_()),
+    "a large column of the weights": lambda x, w: (w[:, 5].mul_(1e9), x[:, 5].mul_(1e-9)),
+    "two columns against each other, 2^16": lambda x, w: (x[:, 3].mul_(2.0 ** 16), w[:, 3].mul_(2.0 ** -16), x[:, 4].mul_(2.0 ** -16), w[:, 4].mul_(2.0 ** 16)),
+    "two columns against each other, 2^20": lambda x, w: (x[:, 3].mul_(2.0 ** 20), w[:, 3].mul_(2.0 ** -20), x[:, 4].mul_(2.0 ** -20), w[:, 4].mul_(2.0 ** 20)),
+    "sparse rows, 2^30": lambda x, w: (x[:, 2:].mul_(normal(9, *x[:, 2:].shape) > 2), x[:, 0].fill_(1), x[:, 1].mul_(2.0 ** -30),
+                                       w.mul_(torch.arange(w.shape[1]) < 2), w[:, 1].mul_(2.0 ** 30)),
+    "single rows of counts": lambda x, w: (x[::7, 3].mul_(3e6), w[:, 3].mul_(1e-7)),
+}
+
+
+@pytest.mark.parametrize("rows,vocab,cols", [(20, 1000, 512), (90, 700, 513), (300, 9000, 512), (300, 22001, 500)])
+@pytest.mark.parametrize("what", MIXED)
+def test_binary32_rows_of_mixed_magnitudes(what, rows, vocab, cols):
+    print("mixed magnitudes:", what, rows, vocab, cols, flush=True)
+    x, w = normal(1, rows, cols), normal(2, vocab, cols) * (4.0 / cols ** 0.5)
+    MIXED[what](x, w)
+    t = words(3, rows, vocab)
+    t[rows // 2] = -1
+    both_passes32(x, w, t, normal(4, rows).abs() + 0.1)
+
+
+def test_binary32_tiles_of_either_kind_side_by_side():
+    """Only some words and some rows are of mixed magnitudes: tiles beside and below each other are of either kind."""
+    rows, vocab, cols = 700, 5000, 200
+    x, w = normal(1, rows, cols), normal(2, vocab, cols) * (3.0 / cols ** 0.5)
+    x[100:130, 7] *= 1e9
+    w[2100:2300, 8] *= 1e9
+    x[:, 8] *= 1e-9
+    w[:, 7] *= 1e-9
+    both_passes32(x, w, words(3, rows, vocab), normal(4, rows).abs() + 0.1)
+
+
+@pytest.mark.parametrize("rows", [90, 300])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_words_of_infinite_weight(rows, dtype):
+    """A word whose logit is minus infinity takes no part: the others' loss and gradients are those of a vocabulary without it."""
+    vocab, cols = 900, 96
+    x, w = normal(1, rows, cols).to("cuda", dtype), (normal(2, vocab, cols) * 0.3).to("cuda", dtype)
+    x[:, 5] = x[:, 5].abs() + 0.125
+    x[:, 6:9] = 1.0                       # (a value of few bits: nothing of it is left for a second plane)
+    masked = torch.tensor([0, 17, 255, 256, 899], device="cuda")
+    w[masked, 5] = float("-inf")
+    w[masked, 6] = float("-inf")
+    kept = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    kept[masked] = False
+    t = words(3, rows, vocab - 5)
+    t[2] = -1
+    at = torch.arange(vocab, device="cuda")[kept][t.clamp(min=0).cuda()]
+    at[2] = -1
+    g = torch.ones(rows, device="cuda")
+    loss, lse = pk.ops.linear_cross_entropy_forward(x, w, at)
+    loss64, lse64, d, logits = xent64(x, w[kept], t.cuda(), g)
+    off = rounding(x, w[kept], logits) + 2 ** -20
+    within(lse, lse64, off, "lse")
+    within(loss, loss64, 2 * off, "loss")
+    _, dw = pk.ops.linear_cross_entropy_backward(g, x, w, at, lse, need_x=False)
+    assert bool(torch.isfinite(dw).all()) and float(dw[masked].abs().sum()) == 0
+    want = torch.mm(d.t().contiguous(), x.double())
+    assert float((dw[kept].double() - want).norm() / want.norm()) < {F32: 2.0 ** -18, F16: 2.0 ** -10, BF16: 2.0 ** -7}[dtype]
