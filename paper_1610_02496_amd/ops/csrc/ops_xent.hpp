@@ -429,14 +429,20 @@ struct StoreEpilogue {
 // ---- small kernels ---------------------------------------------------------------------------------------------------------
 
 // The bits of eight values as operands of the matrix cores: one of 16 bits, or three of bfloat16 whose sum is the value of 32
-// (cut off, so that it is exact; an infinity or NaN stays whole in the first).
-template <class T>
+// (cut off, so that it is exact; an infinity or NaN stays whole in the first).  SIGNED: the second and third plane of a value that leaves
+// nothing for them hold its sign and 2^-126 in place of zero, so that times an infinity each plane gives the same infinity, none NaN
+// (to a sum of products this adds 2^-125 of the other operand's at most).
+template <class T, bool SIGNED = false>
 __device__ __forceinline__ void planes_of(const Raw8<T> &r, u32x4 (&o)[sizeof(T) == 4 ? 3 : 1]) {
     if constexpr (sizeof(T) == 2) o[0] = u32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
     else {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.v[i]);
+        float least[SIGNED ? 8 : 1];
+        if constexpr (SIGNED)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) least[i] = copysignf(fminf(fabsf(v[i]), 0x1p-126f), v[i]);
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             uint32_t h[8];
@@ -447,6 +453,7 @@ __device__ __forceinline__ void planes_of(const Raw8<T> &r, u32x4 (&o)[sizeof(T)
                 // a NaN whose upper half would read as an infinity keeps a bit of it
                 h[i] = odd && (all & 0x7fffffu) ? b | 0x400000u : b;
                 v[i] = odd ? 0.f : v[i] - __uint_as_float(b);
+                if constexpr (SIGNED) v[i] = fabsf(v[i]) < 0x1p-126f ? least[i] : v[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[q][i] = __builtin_amdgcn_perm(h[2 * i + 1], h[2 * i], 0x07060302);
@@ -678,7 +685,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void score_few_kernel(const T *x, i
             for (int i = 0; i < BATCH; ++i) {
                 const int m = n + i * (kFewWaves / 2);
                 u32x4 o[PLANES];
-                planes_of<T>(f[i], o);
+                planes_of<T, true>(f[i], o);
                 if (m < rows)
 #pragma unroll
                     for (int q = 0; q < PLANES; ++q) *reinterpret_cast<u32x4 *>(few_lds + q * plane_bytes + m * row_bytes + c * 2) = o[q];

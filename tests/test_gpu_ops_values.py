@@ -105,7 +105,7 @@ def test_binary32_tiles_of_either_kind_side_by_side():
     both_passes32(x, w, words(3, rows, vocab), normal(4, rows).abs() + 0.1)
 
 
-@pytest.mark.parametrize("rows", [90, 300])
+@pytest.mark.parametrize("rows", [3, 40, 90, 300])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_words_of_infinite_weight(rows, dtype):
     """A word whose logit is minus infinity takes no part: the others' loss and gradients are those of a vocabulary without it."""
