@@ -269,11 +269,29 @@ struct ScoreEpilogue {
     }
 };
 
+// d of 16 bits is brought to one magnitude row by row, so that a row's products are as good whatever its dloss is next to the others':
+// with `top` the largest |dloss| and dloss_n = m 2^j top, 1 <= |m| < 2, it is held as (p - [v = t]) m to.  What is missing stands outside of
+// the products: dx_n is multiplied by 2^j top / to in binary32, and the product of the weight's gradient takes x_n 2^j in place of x_n (a
+// power of two).  With one dloss for all rows (a mean) m is 1: neither the rounding of dloss itself nor, near a target, that of 1 - p then
+// stands in every value (with dloss rounded along, the weight's gradient was up to 1.5 times as far from the exact one).
+// to is 2^14 for binary16, of which |d| < 2 to neither overflows nor loses bits until it is 2^-28 of it; x then is multiplied by a power
+// of two 2^u as well, which brings its largest value to 2^14 .. 2^15, so that x_n 2^j keeps its bits down to about 2^-28 of the largest.
+template <class T> constexpr float kGradTo = std::is_same<T, f16>::value ? 0x1p14f : 1.f;
+struct GradScale { float top, down; int up; };   // down: top / to / 2^u; up: u
+// (m, j) of a dloss; one that is not finite stands for itself
+__device__ __forceinline__ float split_dloss(float dloss, float top, int &j) {
+    const float q = dloss / top;
+    const bool odd = !(fabsf(q) < INFINITY) || q == 0.f;
+    j = odd ? 0 : __builtin_amdgcn_frexp_expf(q) - 1;
+    return odd ? q : 2.f * __builtin_amdgcn_frexp_mantf(q);
+}
+
 // d of the piece, [row][words of the piece], PLANES planes of 16 bits; words past the vocabulary are zeros
 template <class T, int PLANES>
 struct GradEpilogue {
     T *d; int64_t stride, plane;
-    const float *lse, *dloss, *scale;    // scale[0]: what dloss is multiplied with, or null
+    const float *lse, *dloss;
+    const GradScale *scale;              // one plane
     Targets target;
     int64_t rows, words, word0, vocab;
     Powers powers;                       // three planes
@@ -281,13 +299,18 @@ struct GradEpilogue {
     template <int TN> struct State { int64_t target[TN]; float top[TN], g[TN]; int power[PLANES == 3 ? TN : 1]; };
     template <int TN>
     __device__ __forceinline__ void prepare(State<TN> &s, int64_t n) const {
-        const float up = scale ? *scale : 1.f;
+        float top = 1.f;
+        if constexpr (PLANES == 1) top = scale->top;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const bool row = n + j * 16 < rows;
             s.target[j] = row ? target.at(n + j * 16) : -1;
             s.top[j] = row ? lse[n + j * 16] : 0.f;
-            s.g[j] = row ? dloss[n + j * 16] * up : 0.f;
+            s.g[j] = row ? dloss[n + j * 16] : 0.f;
+            if constexpr (PLANES == 1) {
+                int power;
+                s.g[j] = split_dloss(s.g[j], top, power) * kGradTo<T>;
+            }
             if constexpr (PLANES == 3) s.power[j] = row ? powers.rows[n + j * 16] : 0;
         }
     }
@@ -393,13 +416,13 @@ struct SumEpilogue {
 template <class T>
 struct StoreEpilogue {
     T *out; int64_t rows, cols;
-    const float *scale;
+    const GradScale *scale;              // of d, or null
 
     template <int TN> struct State {};
     template <int TN> __device__ __forceinline__ void prepare(State<TN> &, int64_t) const {}
     template <int BM, int BN, int WM, int WN, int TM, int TN>
     __device__ __forceinline__ void finish(f32x4 (&acc)[TM][TN], const State<TN> &, int64_t m0, int64_t n0, int wm, int wn, int lane, int, int, int, void *) const {
-        const float down = scale ? scale[1] : 1.f;
+        const float down = scale ? scale->down : 1.f;
         const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -461,17 +484,34 @@ __device__ __forceinline__ void planes_of(const Raw8<T> &r, u32x4 (&o)[sizeof(T)
     }
 }
 
-// Rows of 16-bit elements as aligned rows, zeros up to their stride.  `mask`: rows without a target become zeros,
-// so that nothing in them, NaN included, reaches a product.
+// Rows of 16-bit elements as aligned rows, zeros up to their stride.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride,
-                                                   Targets mask) {
+__global__ __launch_bounds__(256) void pack_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride) {
     const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
     if (c >= stride) return;
     for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
         u32x4 o[1];
-        planes_of<T>(load_raw8(src + row * src_stride + c, mask.p && mask.at(row) < 0 ? 0 : cols - c), o);
+        planes_of<T>(load_raw8(src + row * src_stride + c, cols - c), o);
         *reinterpret_cast<u32x4 *>(dst + row * stride + c) = o[0];
+    }
+}
+
+// Features for the product of the weight's gradient: the same, times 2^(j + u).  Rows without a target become zeros, so that nothing in
+// them, NaN included, reaches a product.
+template <class T>
+__global__ __launch_bounds__(256) void pack_scaled_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t stride,
+                                                          Targets target, const float *dloss, const GradScale *scale) {
+    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+    if (c >= stride) return;
+    const float top = scale->top;
+    const int up = scale->up;
+    for (int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.y * 4) {
+        f32x8 v = load8(src + row * src_stride + c, target.at(row) < 0 ? 0 : cols - c);
+        int j;
+        split_dloss(dloss[row], top, j);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], j + up);
+        store8(reinterpret_cast<T *>(dst) + row * stride + c, 8, v);
     }
 }
 
@@ -567,37 +607,61 @@ __global__ __launch_bounds__(1024) void score_join_kernel(const float2 *partial,
     }
 }
 
-// d is rounded to the features' type as (p - [v = t]) dloss_n / top * to, where top is the largest |dloss|, and its products are scaled
-// back in binary32: scale[0] = to / top, scale[1] = top / to.  With one dloss for all rows (a mean) that factor is exactly `to`, a power of
-// two: neither the roundings of dloss itself nor, near a target, that of 1 - p then stand in every value (with dloss rounded along,
-// the weight's gradient was up to 1.5 times as far from the exact one).  to is 2^14 for binary16, of which |d| <= to neither overflows
-// nor loses bits until it is 2^-28 of it.  Both are 1 where the largest is 0 or not finite.
-__global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Targets target, int64_t rows, float to, float *scale) {
-    __shared__ uint32_t lds[16];
+// largest finite magnitude of the rows with a target, one per workgroup
+template <class T>
+__global__ __launch_bounds__(256) void magnitude_kernel(const T *src, int64_t src_stride, int64_t rows, int64_t cols, Targets target, uint32_t *most) {
+    __shared__ uint32_t lds[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t top = 0;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < rows; row += (int64_t)gridDim.x * 4) {
+        if (target.at(row) < 0) continue;
+        for (int64_t c = lane * 8; c < cols; c += 512) {
+            const f32x8 v = load8(src + row * src_stride + c, cols - c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+                top = max(top, b < 0x7f800000u ? b : 0u);
+            }
+        }
+    }
+    top = wave_max(top);
+    if (lane == 0) lds[wave] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) most[blockIdx.x] = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+}
+
+// what d is relative to: the largest finite |dloss| of the rows with a target (1 if there is none but zeros), and of `parts` magnitudes of
+// features the largest (none: u = 0)
+__global__ __launch_bounds__(1024) void grad_scale_kernel(const float *dloss, Targets target, int64_t rows, float to, const uint32_t *most, int parts,
+                                                          GradScale *scale) {
+    __shared__ uint32_t lds[2][16];
+    uint32_t top = 0, size = 0;
     for (int64_t n = threadIdx.x; n < rows; n += 1024)
-        if (target.at(n) >= 0) top = max(top, __float_as_uint(dloss[n]) & 0x7fffffffu);
-    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+        if (target.at(n) >= 0) {
+            const uint32_t b = __float_as_uint(dloss[n]) & 0x7fffffffu;
+            top = max(top, b < 0x7f800000u ? b : 0u);
+        }
+    for (int i = threadIdx.x; i < parts; i += 1024) size = max(size, most[i]);
+    top = wave_max(top);
+    size = wave_max(size);
+    if ((threadIdx.x & 63) == 0) { lds[0][threadIdx.x >> 6] = top; lds[1][threadIdx.x >> 6] = size; }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) top = max(top, lds[i]);
-        const bool none = top == 0 || top >= 0x7f800000u;
-        const float g = fmaxf(__uint_as_float(top), 0x1p-100f);
-        scale[0] = none ? 1.f : to / g;
-        scale[1] = none ? 1.f : g / to;
+        for (int i = 1; i < 16; ++i) { top = max(top, lds[0][i]); size = max(size, lds[1][i]); }
+        const float g = top ? __uint_as_float(top) : 1.f;
+        const int up = size ? 14 - ((int)(size >> 23) - 127) : 0;   // (binary16 has no magnitude below 2^-24)
+        *scale = GradScale{g, __builtin_amdgcn_ldexpf(g / to, -up), up};
     }
 }
 
-// dx = sum of the splits' partial sums, in a fixed order: every wavefront takes a quarter of the splits of 512 columns of a row, eight
+// dx = sum of the splits' partial sums times what d is relative to, in a fixed order; zeros for a row without a target: every wavefront takes a quarter of the splits of 512 columns of a row, eight
 // on their way at a time, and the quarters meet in LDS
 template <class T>
-__global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits, int64_t rows, int64_t stride, int64_t cols, const float *scale,
-                                                  T *dx) {
+__global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits, int64_t rows, int64_t stride, int64_t cols, Targets target,
+                                                  const float *dloss, const GradScale *scale, T *dx) {
     __shared__ f32x8 lds[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 8;
-    const float down = scale ? scale[1] : 1.f;
     const int k0 = splits * wave / 4, k1 = splits * (wave + 1) / 4;
     for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
         f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -618,7 +682,15 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
         __syncthreads();
         if (wave == 0 && c < cols) {
             for (int i = 1; i < 4; ++i) v += lds[i][lane];
-            store8(dx + row * cols + c, cols - c, v * down);
+            float down = 1.f;
+            if constexpr (sizeof(T) == 2) {
+                int j;
+                split_dloss(dloss[row], scale->top, j);
+                down = __builtin_amdgcn_ldexpf(scale->top / kGradTo<T>, j);
+            }
+            if (target.at(row) < 0) v = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            else v *= down;
+            store8(dx + row * cols + c, cols - c, v);
         }
         __syncthreads();
     }

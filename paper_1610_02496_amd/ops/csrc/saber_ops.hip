@@ -360,7 +360,7 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
     return f;
 }
 
-struct BackwardSpace { float *scale; uint16_t *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *x_sums, *w_sums, *sums; int64_t piece, stride; int splits, dx_tile; };
+struct BackwardSpace { GradScale *scale; uint32_t *most; int most_parts; uint16_t *x_plain, *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *x_sums, *w_sums, *sums; int64_t piece, stride; int splits, dx_tile; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
     const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / row, most_w = kPieceValues / c.cols_pad;
@@ -378,7 +378,12 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
     if (splits > steps / 8) splits = steps / 8;
     if (splits < 1) splits = 1;
     b.splits = (int)splits;
-    b.scale = s.take<float>(2);
+    b.scale = s.take<GradScale>(1);
+    if (c.dtype == SABER_F16) {
+        b.most_parts = (int)(parts_of(row, 4) < kCus ? parts_of(row, 4) : kCus);
+        b.most = s.take<uint32_t>(b.most_parts);
+    }
+    if (c.planes == 1 && c.pack_x) b.x_plain = s.take<uint16_t>(c.rows * c.cols_pad);
     b.x = s.take<uint16_t>(c.rows * c.cols_pad * c.planes);
     if (c.pack_w) b.w = s.take<uint16_t>(b.piece * c.cols_pad * c.planes);
     if (c.planes == 3) {   // the logits' form of both
@@ -395,10 +400,13 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
     return b;
 }
 
-template <class T>
-int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, Targets mask, hipStream_t st) {
+dim3 pack_grid(int64_t rows, const Xent &c) {
     const int64_t y = parts_of(rows, 4);
-    pack_kernel<T><<<dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768)), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad, mask);
+    return dim3((unsigned)parts_of(c.cols_pad, 512), (unsigned)(y < 32768 ? y : 32768));
+}
+template <class T>
+int pack(const T *src, int64_t stride, int64_t rows, const Xent &c, uint16_t *dst, hipStream_t st) {
+    pack_kernel<T><<<pack_grid(rows, c), 256, 0, st>>>(src, stride, rows, c.cols, dst, c.cols_pad);
     OPS_HIP(hipGetLastError());
     return SABER_OK;
 }
@@ -481,7 +489,7 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
         const Targets none{nullptr, 0};
         const int64_t plane_x = rows * c.cols_pad, plane_w = f.piece * c.cols_pad;
         if constexpr (!F32)
-            if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, f.x, none, st));
+            if (c.pack_x) OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, f.x, st));
         const Operand ox = c.pack_x ? Operand{f.x, c.cols_pad, plane_x, rows} : Operand{x, x_stride, 0, rows};
         for (int64_t v0 = 0; v0 < vocab; v0 += f.piece) {
             const int64_t words = vocab - v0 < f.piece ? vocab - v0 : f.piece;
@@ -489,7 +497,7 @@ extern "C" int saber_linear_xent_forward(const void *x, int64_t x_stride, const 
             if constexpr (F32)
                 OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, nullptr, plane_x, f.x, f.x_powers, f.x_sums, none},
                                Rows32{w0, w_stride, words, nullptr, plane_w, f.w, f.w_powers, f.w_sums, none}, c, st));
-            else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, none, st));
+            else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, f.w, st));
             const Operand ow = c.pack_w ? Operand{f.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
             const Powers powers{f.w_powers, f.x_powers};
             const ScoreEpilogue<F32> ep{f.partial, f.rows_pad, f.at, t, rows, words, v0, (int)parts, powers};
@@ -536,15 +544,20 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
         constexpr bool F32 = std::is_same<T, f32>::value;
         constexpr int PLANES = F32 ? 3 : 1, SEGMENTS = F32 ? 6 : 1;
         const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.stride;
-        const float *scale = nullptr;
-        if (rows) {
-            if constexpr (!F32) {   // (three planes keep all bits)
-                OPS_TRY(pack(static_cast<const T *>(x), x_stride, rows, c, b.x, t, st));
-                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, std::is_same<T, f16>::value ? 0x1p14f : 1.f, b.scale);
+        const GradScale *scale = F32 ? nullptr : b.scale;   // (three planes keep all bits)
+        if constexpr (!F32)
+            if (rows) {
+                const T *from = static_cast<const T *>(x);
+                if constexpr (std::is_same<T, f16>::value) {
+                    magnitude_kernel<T><<<b.most_parts, 256, 0, st>>>(from, x_stride, rows, cols, t, b.most);
+                    OPS_HIP(hipGetLastError());
+                }
+                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, kGradTo<T>, b.most, b.most_parts, b.scale);
                 OPS_HIP(hipGetLastError());
-                scale = b.scale;
+                pack_scaled_kernel<T><<<pack_grid(rows, c), 256, 0, st>>>(from, x_stride, rows, cols, b.x, c.cols_pad, t, dloss, scale);
+                OPS_HIP(hipGetLastError());
+                if (c.pack_x) OPS_TRY(pack(from, x_stride, rows, c, b.x_plain, st));
             }
-        }
         for (int64_t v0 = 0; v0 < vocab; v0 += b.piece) {
             const int64_t words = vocab - v0 < b.piece ? vocab - v0 : b.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
@@ -553,9 +566,9 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
                 if constexpr (F32)
                     OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, b.x_sums, t},
                                    Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, b.w_sums, Targets{nullptr, 0}}, c, st));
-                else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, Targets{nullptr, 0}, st));
+                else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, st));
                 const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
-                const Operand ox{b.x, c.cols_pad, plane_x, rows};
+                const Operand ox = c.pack_x ? Operand{b.x_plain, c.cols_pad, 0, rows} : Operand{x, x_stride, 0, rows};
                 const Powers powers{b.w_powers, b.x_powers};
                 const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, powers};
                 const int tile = tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1));
@@ -578,7 +591,7 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
             }
         }
         if (dx && rows) {
-            sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(rows < 16384 ? rows : 16384)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, scale, static_cast<T *>(dx));
+            sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(rows < 16384 ? rows : 16384)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, t, dloss, scale, static_cast<T *>(dx));
             OPS_HIP(hipGetLastError());
         }
         return SABER_OK;

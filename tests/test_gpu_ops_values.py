@@ -132,3 +132,58 @@ def test_words_of_infinite_weight(rows, dtype):
     assert bool(torch.isfinite(dw).all()) and float(dw[masked].abs().sum()) == 0
     want = torch.mm(d.t().contiguous(), x.double())
     assert float((dw[kept].double() - want).norm() / want.norm()) < {F32: 2.0 ** -18, F16: 2.0 ** -10, BF16: 2.0 ** -7}[dtype]
+
+
+def spread(dtype, rows=200, vocab=9000, cols=128):
+    """A batch whose dloss spans 2^26: sizes at which binary16 holds dx and dweight themselves, and a projection with a common part, so that
+    the softmax' many small probabilities make up much of dx."""
+    x, w = (normal(1, rows, cols) * 0.3).to("cuda", dtype), (normal(2, vocab, cols) * 0.3 + 0.5).to("cuda", dtype)
+    t = words(3, rows, vocab)
+    t[5] = -1
+    g = (1 + normal(4, rows).abs().clamp(max=0.9)) * 2.0 ** (12 - torch.arange(rows) % 27).double()
+    return x, w, t.cuda(), g.to("cuda", F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_rows_of_small_gradient_keep_their_precision(dtype):
+    x, w, t, g = spread(dtype)
+    rows, cols = x.shape
+    loss, lse = pk.ops.linear_cross_entropy_forward(x, w, t)
+    dx, dw = pk.ops.linear_cross_entropy_backward(g, x, w, t, lse)
+    _, _, d, logits = xent64(x, w, t, g)
+    x64, w64, has = x.double(), w.double(), t >= 0
+    hold = {F32: 2.0 ** -22, F16: 2.0 ** -11, BF16: 2.0 ** -8}[dtype]
+    size = torch.where(has, g.double(), 0.0)
+    p = d.abs()
+    p[torch.arange(rows, device="cuda"), t.clamp(min=0)] += size
+    # d is rounded relative to its row's dloss; binary16's steps end at 2^-24 after 2^14
+    d_err = hold * d.abs() + p * (4 * rounding(x, w, logits)[:, None] + 2 ** -20) + size[:, None] * 2.0 ** -38
+    tiny = 2.0 ** -25 if dtype is F16 else 1e-37
+    want = torch.mm(d, w64)
+    within(dx, want, ROUND[dtype] * want.abs() * 1.01 + tiny + torch.mm(d_err, w64.abs()) + (len(w) + 8) * E * torch.mm(p, w64.abs()), "dx")
+    want = torch.mm(d.t().contiguous(), x64)
+    # the features of a row of small dloss are brought to it: 2^-39 of the largest feature times the largest dloss, in binary16
+    moved = (p / size.clamp(min=1e-300)[:, None]).sum(0)[:, None] * float(g.max()) * float(x64.abs().max()) * 2.0 ** -38
+    within(dw, want, ROUND[dtype] * want.abs() * 1.01 + tiny + torch.mm(d_err.t().contiguous(), x64.abs()) + (rows + 8) * E * torch.mm(p.t().contiguous(), x64.abs()) + moved, "dweight")
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_a_gradient_that_is_not_finite_stays_in_its_row(dtype, value):
+    x, w, t, g = spread(dtype, vocab=3000)
+    g[17] = value
+    lse = pk.ops.linear_cross_entropy_forward(x, w, t)[1]
+    dx = pk.ops.linear_cross_entropy_backward(g, x, w, t, lse, need_weight=False)[0]
+    assert not bool(torch.isfinite(dx[17]).any())
+    left, t2, g2 = torch.arange(200) != 17, t.clone(), g.clone()
+    t2[17], g2[17] = -1, 0.0
+    want = pk.ops.linear_cross_entropy_backward(g2, x, w, t2, lse, need_weight=False)[0]
+    assert torch.equal(dx[left], want[left])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_no_gradient_at_all(dtype):
+    x, w, t, _ = spread(dtype, rows=70, vocab=300)
+    lse = pk.ops.linear_cross_entropy_forward(x, w, t)[1]
+    dx, dw = pk.ops.linear_cross_entropy_backward(torch.zeros(70, device="cuda"), x, w, t, lse)
+    assert float(dx.abs().sum()) == 0 and float(dw.abs().sum()) == 0
