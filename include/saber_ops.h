@@ -97,7 +97,7 @@ int saber_linear_xent_forward(const void *x, int64_t x_stride, const void *weigh
  *   lse as the forward pass gave it; dx [rows][cols], dweight [vocab][cols] of dtype, either may be NULL
  * Between the products d is held in the type of x, for one piece of the vocabulary at a time (a work space of bounded
  * size); binary32 keeps its 24 bits.  Rows left out have zeros in dx and add nothing to dweight, whatever x and lse
- * hold there.  workspace as above.  Errors: EINVAL, ERANGE, EDEVICE.
+ * hold there; no rows give zeros for dweight.  workspace as above.  Errors: EINVAL, ERANGE, EDEVICE.
  */
 int saber_linear_xent_backward(const float *dloss, const void *x, int64_t x_stride, const void *weight, int64_t w_stride,
                                const void *target, int target64, const float *lse, int64_t rows, int64_t vocab,

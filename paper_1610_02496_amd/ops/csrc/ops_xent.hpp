@@ -696,6 +696,12 @@ __global__ __launch_bounds__(256) void sum_kernel(const float *sums, int splits,
     }
 }
 
+template <class T>
+__global__ __launch_bounds__(256) void zeros_kernel(T *p, int64_t n) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048)
+        store8(p + i, n - i, f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
+}
+
 // ---- few rows --------------------------------------------------------------------------------------------------------------
 
 template <class T>

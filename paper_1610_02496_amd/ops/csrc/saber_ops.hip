@@ -544,53 +544,56 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
         constexpr bool F32 = std::is_same<T, f32>::value;
         constexpr int PLANES = F32 ? 3 : 1, SEGMENTS = F32 ? 6 : 1;
         const int64_t plane_x = rows * c.cols_pad, plane_w = b.piece * c.cols_pad, plane_d = rows * b.stride;
+        if (rows == 0) {   // (a gradient of nothing: zeros)
+            const int64_t n = vocab * cols, groups = parts_of(n, 2048);
+            zeros_kernel<T><<<(unsigned)(groups < 16 * kCus ? groups : 16 * kCus), 256, 0, st>>>(static_cast<T *>(dweight), n);
+            OPS_HIP(hipGetLastError());
+            return SABER_OK;
+        }
         const GradScale *scale = F32 ? nullptr : b.scale;   // (three planes keep all bits)
-        if constexpr (!F32)
-            if (rows) {
-                const T *from = static_cast<const T *>(x);
-                if constexpr (std::is_same<T, f16>::value) {
-                    magnitude_kernel<T><<<b.most_parts, 256, 0, st>>>(from, x_stride, rows, cols, t, b.most);
-                    OPS_HIP(hipGetLastError());
-                }
-                grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, kGradTo<T>, b.most, b.most_parts, b.scale);
+        if constexpr (!F32) {
+            const T *from = static_cast<const T *>(x);
+            if constexpr (std::is_same<T, f16>::value) {
+                magnitude_kernel<T><<<b.most_parts, 256, 0, st>>>(from, x_stride, rows, cols, t, b.most);
                 OPS_HIP(hipGetLastError());
-                pack_scaled_kernel<T><<<pack_grid(rows, c), 256, 0, st>>>(from, x_stride, rows, cols, b.x, c.cols_pad, t, dloss, scale);
-                OPS_HIP(hipGetLastError());
-                if (c.pack_x) OPS_TRY(pack(from, x_stride, rows, c, b.x_plain, st));
             }
+            grad_scale_kernel<<<1, 1024, 0, st>>>(dloss, t, rows, kGradTo<T>, b.most, b.most_parts, b.scale);
+            OPS_HIP(hipGetLastError());
+            pack_scaled_kernel<T><<<pack_grid(rows, c), 256, 0, st>>>(from, x_stride, rows, cols, b.x, c.cols_pad, t, dloss, scale);
+            OPS_HIP(hipGetLastError());
+            if (c.pack_x) OPS_TRY(pack(from, x_stride, rows, c, b.x_plain, st));
+        }
         for (int64_t v0 = 0; v0 < vocab; v0 += b.piece) {
             const int64_t words = vocab - v0 < b.piece ? vocab - v0 : b.piece;
             const T *w0 = static_cast<const T *>(weight) + v0 * w_stride;
             T *dw = dweight ? static_cast<T *>(dweight) + v0 * cols : nullptr;
-            if (rows) {
-                if constexpr (F32)
-                    OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, b.x_sums, t},
-                                   Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, b.w_sums, Targets{nullptr, 0}}, c, st));
-                else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, st));
-                const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
-                const Operand ox = c.pack_x ? Operand{b.x_plain, c.cols_pad, 0, rows} : Operand{x, x_stride, 0, rows};
-                const Powers powers{b.w_powers, b.x_powers};
-                const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, powers};
-                const int tile = tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1));
-                if constexpr (F32) {
-                    const Operand lw{b.w_even, c.cols_pad, plane_w, words}, lx{b.x_even, c.cols_pad, plane_x, rows};
-                    const Direct32 direct{w0, w_stride, static_cast<const T *>(x), x_stride, b.w_sums, b.x_sums, powers};
-                    OPS_TRY((product<L, false, false>(lw, lx, cols, 3, 1, ep, st, tile, direct)));
-                } else
-                    OPS_TRY((product<L, false, false>(ow, ox, cols, 1, 1, ep, st, tile)));
-                if (dx) {
-                    const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
-                    const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};
-                    OPS_TRY((product<M, true, false>(cw, od, words, SEGMENTS, b.splits, sum, st, b.dx_tile)));
-                }
+            if constexpr (F32)
+                OPS_TRY(pack32(Rows32{static_cast<const T *>(x), x_stride, v0 ? 0 : rows, b.x, plane_x, b.x_even, b.x_powers, b.x_sums, t},
+                               Rows32{w0, w_stride, words, b.w, plane_w, b.w_even, b.w_powers, b.w_sums, Targets{nullptr, 0}}, c, st));
+            else if (c.pack_w) OPS_TRY(pack(w0, w_stride, words, c, b.w, st));
+            const Operand ow = c.pack_w ? Operand{b.w, c.cols_pad, plane_w, words} : Operand{w0, w_stride, 0, words};
+            const Operand ox = c.pack_x ? Operand{b.x_plain, c.cols_pad, 0, rows} : Operand{x, x_stride, 0, rows};
+            const Powers powers{b.w_powers, b.x_powers};
+            const GradEpilogue<M, PLANES> ep{reinterpret_cast<M *>(b.d), b.stride, plane_d, lse, dloss, scale, t, rows, words, v0, vocab, powers};
+            const int tile = tile_of(words, rows, parts_of(cols, kStep) * (F32 ? 3 : 1));
+            if constexpr (F32) {
+                const Operand lw{b.w_even, c.cols_pad, plane_w, words}, lx{b.x_even, c.cols_pad, plane_x, rows};
+                const Direct32 direct{w0, w_stride, static_cast<const T *>(x), x_stride, b.w_sums, b.x_sums, powers};
+                OPS_TRY((product<L, false, false>(lw, lx, cols, 3, 1, ep, st, tile, direct)));
+            } else
+                OPS_TRY((product<L, false, false>(ow, ox, cols, 1, 1, ep, st, tile)));
+            if (dx) {
+                const SumEpilogue sum{b.sums, c.cols_pad, rows, c.cols_pad, v0 > 0};
+                const Operand cw{ow.p, ow.stride, ow.plane, c.cols_pad}, od{b.d, b.stride, plane_d, rows};
+                OPS_TRY((product<M, true, false>(cw, od, words, SEGMENTS, b.splits, sum, st, b.dx_tile)));
             }
-            if (dweight) {   // (without rows: zeros)
+            if (dweight) {
                 const Operand cx{b.x, c.cols_pad, plane_x, c.cols_pad}, cd{b.d, b.stride, plane_d, up(words, 8)};
                 const StoreEpilogue<T> store{dw, words, cols, scale};
                 OPS_TRY((product<M, true, true>(cx, cd, rows, SEGMENTS, 1, store, st, tile_of(cols, words, parts_of(rows, kStep) * SEGMENTS))));
             }
         }
-        if (dx && rows) {
+        if (dx) {
             sum_kernel<T><<<dim3((unsigned)parts_of(cols, 512), (unsigned)(rows < 16384 ? rows : 16384)), 256, 0, st>>>(b.sums, b.splits, rows, c.cols_pad, cols, t, dloss, scale, static_cast<T *>(dx));
             OPS_HIP(hipGetLastError());
         }

@@ -187,3 +187,16 @@ def test_no_gradient_at_all(dtype):
     lse = pk.ops.linear_cross_entropy_forward(x, w, t)[1]
     dx, dw = pk.ops.linear_cross_entropy_backward(torch.zeros(70, device="cuda"), x, w, t, lse)
     assert float(dx.abs().sum()) == 0 and float(dw.abs().sum()) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab,cols", [(1, 1), (777, 33), (9000, 520)])
+def test_cross_entropy_of_no_rows(dtype, vocab, cols):
+    x, w, t = torch.empty(0, cols, device="cuda", dtype=dtype), normal(2, vocab, cols).to("cuda", dtype), torch.empty(0, dtype=torch.int64, device="cuda")
+    loss, lse = pk.ops.linear_cross_entropy_forward(x, w, t)
+    dx, dw = pk.ops.linear_cross_entropy_backward(torch.empty(0, device="cuda"), x, w, t, lse)
+    assert loss.shape == lse.shape == (0,) and dx.shape == (0, cols) and dw.shape == (vocab, cols) and bool((dw == 0).all())
+    w.requires_grad_()
+    loss = pk.ops.linear_cross_entropy(x, w, t)
+    loss.backward()
+    assert float(loss) == 0 and bool((w.grad == 0).all())
