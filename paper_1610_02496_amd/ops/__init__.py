@@ -269,7 +269,8 @@ def linear_cross_entropy_forward(x, weight, target):
     logarithm of the softmax' normaliser; float32, in the shape of ``target``.  The logits are not held.  A negative target
     leaves its row out (loss 0); one beyond the vocabulary gives NaN."""
     device, held, inputs, sizes = _head(x, weight, target)
-    loss, lse = x.new_empty((2,) + target.shape, dtype=_F32).unbind()
+    # (two tensors of their own, not views of one: a program may change its loss in place)
+    loss, lse = x.new_empty(target.shape, dtype=_F32), x.new_empty(target.shape, dtype=_F32)
     _with_space(_xent_forward, device, x, inputs + sizes + (loss.data_ptr(), lse.data_ptr()))
     return loss, lse
 

@@ -200,3 +200,20 @@ def test_cross_entropy_of_no_rows(dtype, vocab, cols):
     loss = pk.ops.linear_cross_entropy(x, w, t)
     loss.backward()
     assert float(loss) == 0 and bool((w.grad == 0).all())
+
+
+def test_a_loss_may_be_changed_in_place():
+    x, w, t = normal(1, 90, 64).to("cuda", BF16), normal(2, 700, 64).mul(0.2).to("cuda", BF16), words(3, 90, 700).cuda()
+    weight, left_out = torch.rand(90, device="cuda"), torch.arange(90, device="cuda") % 9 == 7
+    grads = []
+    for in_place in (False, True):
+        xs, ws = x.clone().requires_grad_(), w.clone().requires_grad_()
+        loss = pk.ops.linear_cross_entropy(xs, ws, t, "none")
+        if in_place:
+            loss.mul_(weight)
+            loss[left_out] = 0
+        else:
+            loss = torch.where(left_out, 0.0, loss * weight)
+        loss.sum().backward()
+        grads.append((xs.grad, ws.grad))
+    assert torch.equal(grads[0][0], grads[1][0]) and torch.equal(grads[0][1], grads[1][1])
