@@ -78,7 +78,8 @@ int saber_checkpoint8_restore(const int8_t *q, const float *scale, int64_t rows,
 
 /*
  * Softmax cross entropy of x weight^T: lse_n = log sum_v exp(x_n . W_v), loss_n = lse_n - x_n . W_target(n).  The logits
- * are never held.
+ * are never held: the work space is packed operands where they are needed (of the weight at most 256 MB at a time) and
+ * a maximum and a sum per row and tile of words.
  *   x [rows][cols], weight [vocab][cols] of dtype; target [rows]: int32, or int64 if target64
  *   A negative target leaves the row out: its loss is 0 (lse is still the row's).  One of vocab or more gives NaN.
  *   loss, lse [rows]
@@ -95,8 +96,9 @@ int saber_linear_xent_forward(const void *x, int64_t x_stride, const void *weigh
  * Gradients for dloss [rows]: with d_nv = dloss_n (exp(x_n . W_v - lse_n) - [v = target(n)])
  *   dx_n = sum_v d_nv W_v,  dweight_v = sum_n d_nv x_n
  *   lse as the forward pass gave it; dx [rows][cols], dweight [vocab][cols] of dtype, either may be NULL
- * Between the products d is held in the type of x, for one piece of the vocabulary at a time (a work space of bounded
- * size); binary32 keeps its 24 bits.  Rows left out have zeros in dx and add nothing to dweight, whatever x and lse
+ * Between the products d is held in the type of x, for one piece of the vocabulary at a time; binary32 keeps its 24
+ * bits.  The work space does not grow with the vocabulary: d of a piece takes 256 MB at most and so do its packed words
+ * (256 words make a piece whatever the sizes), beside copies of the features and partial sums of dx.  Rows left out have zeros in dx and add nothing to dweight, whatever x and lse
  * hold there; no rows give zeros for dweight.  workspace as above.  Errors: EINVAL, ERANGE, EDEVICE.
  */
 int saber_linear_xent_backward(const float *dloss, const void *x, int64_t x_stride, const void *weight, int64_t w_stride,

@@ -242,9 +242,9 @@ namespace {
 // of 100,000 149 and 129).
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewLds = 150 * 1024;
-// values of d, and of packed words, per piece: 256 MB of a 16-bit type, what the last-level cache holds; 768 MB of three planes (binary32
-// gains from fewer pieces: the gradients of 2,048 rows of 512 columns and 60,000 words, d and the weight's product take 1.21 ms in one,
-// 1.49 ms in three)
+// 16-bit values of d, and of packed words, per piece: 256 MB of each, what the last-level cache holds.  A value of binary32 is three of d,
+// two of the logits' words, five of the gradients' words.  (In binary32 fewer pieces are faster, a training step of 2,048 rows of 512
+// columns and 60,000 words 2.42 ms in one and 2.67 in four, but d of all words is larger than the logits.)
 constexpr int64_t kPieceValues = (int64_t)1 << 27;
 
 struct Xent {
@@ -295,7 +295,8 @@ int tile_of(int64_t m, int64_t n, int64_t steps) {
 
 // Words of a piece, at most `most` (and 2^20: offsets within a tile are 32 bits), whole tiles.  Either all pieces are even, or all but
 // the last fill the CUs with whole rounds of tiles: of d (words x rows), and of the weight's gradient (words x columns), whichever
-// takes fewer rounds in all.  (4,096 rows of 1,024 columns, 100,000 words, both passes: 36 rounds and 3.46 ms even, 32 and 3.30 ms the other way.)
+// takes fewer rounds in all, the latter if they are alike.  (4,096 rows of 1,024 columns, 100,000 words, both passes: 36 rounds and 3.46 ms
+// even, 32 and 3.30 ms the other way; 2,048 of 512 in binary32, 60,000 words: 12 rounds either way, 2.73 and 2.67 ms.)
 int64_t piece_words(int64_t vocab, int64_t most, int64_t rows, int64_t cols) {
     if (most > (int64_t)1 << 20) most = (int64_t)1 << 20;
     most = most / 256 * 256;
@@ -312,7 +313,7 @@ int64_t piece_words(int64_t vocab, int64_t most, int64_t rows, int64_t cols) {
     };
     const int64_t even = up(parts_of(vocab, parts_of(vocab, most)), 256);
     const int64_t round = row_tiles <= kCus ? kCus / row_tiles * 256 : 256, filled = most / round * round;
-    return filled > 0 && rounds(filled) < rounds(even) ? filled : even;
+    return filled > 0 && rounds(filled) <= rounds(even) ? filled : even;
 }
 
 int64_t few_lds(const Xent &c) { return c.rows * (up(c.cols, 32) * 2 + 16) * c.planes; }
@@ -341,7 +342,7 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
         f.few_grid = f.parts = groups < most ? groups : most;
     } else {
         const int64_t most = (kMaxTiles - 1) / parts_of(c.rows > 0 ? c.rows : 1, 64) * 64;   // words that one launch takes
-        f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / c.cols_pad, c.rows, c.cols) : c.vocab;
+        f.piece = c.pack_w ? piece_words(c.vocab, kPieceValues / (c.planes == 3 ? 2 : 1) / c.cols_pad, c.rows, c.cols) : c.vocab;
         if (f.piece > most) f.piece = most / 256 * 256;
         f.tile = tile_of(f.piece, c.rows, parts_of(c.cols, kStep) * (c.planes == 3 ? 3 : 1));
         f.parts = c.vocab / f.piece * parts_of(f.piece, f.tile) + parts_of(c.vocab % f.piece, f.tile);
@@ -363,7 +364,7 @@ ForwardSpace forward_space(const Xent &c, Carve &s) {
 struct BackwardSpace { GradScale *scale; uint32_t *most; int most_parts; uint16_t *x_plain, *x, *w, *d, *x_even, *w_even; int *x_powers, *w_powers; float *x_sums, *w_sums, *sums; int64_t piece, stride; int splits, dx_tile; };
 BackwardSpace backward_space(const Xent &c, Carve &s) {
     BackwardSpace b{};
-    const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / row, most_w = kPieceValues / c.cols_pad;
+    const int64_t row = c.rows > 0 ? c.rows : 1, most_d = kPieceValues / c.planes / row, most_w = kPieceValues / (c.planes == 3 ? 5 : 1) / c.cols_pad;
     b.piece = piece_words(c.vocab, most_d < most_w ? most_d : most_w, row, c.cols);
     const int64_t steps = parts_of(b.piece, kStep) * (c.planes == 3 ? 6 : 1);
     // The features' gradient has few tiles and many steps, which are shared out until every CU has a workgroup: of the largest tiles

@@ -1,4 +1,9 @@
 """Edges of the operators' range on the host side, without a GPU: empty batches, the largest sizes, what work space they ask for."""
+import ctypes
+
+import pytest
+
+import paper_1610_02496_amd as pk
 from tests import fake_hip
 
 
@@ -21,3 +26,30 @@ def test_no_product_of_an_empty_batch(tmp_path):
                     assert launches("zeros_kernel")[0] == zeros + 1
     assert launches("product_kernel")[0] == 0
     """)
+
+
+def need(backward, rows, vocab, cols, dtype, stride=None):
+    n = ctypes.c_int64()
+    L, P, s = pk.load_library(), 1 << 20, stride or cols
+    if backward:
+        rc = L.saber_linear_xent_backward(P, P, s, P, s, P, 1, P, rows, vocab, cols, dtype, P, P, None, ctypes.addressof(n), None)
+    else:
+        rc = L.saber_linear_xent_forward(P, s, P, s, P, 1, rows, vocab, cols, dtype, P, P, None, ctypes.addressof(n), None)
+    assert rc == 0, L.saber_ops_last_error()
+    return n.value
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("rows,vocab,cols", [(64, 141_000, 1000), (2048, 60_000, 512), (300, 200_000, 2048), (8192, 141_000, 1000), (4096, 1 << 24, 777), (65, 1 << 28, 64)])
+def test_work_space_of_every_type_is_bounded(rows, vocab, cols, dtype):
+    """d of a piece and its packed words take 256 MB each at most; besides there are copies of the features (ten bytes a value at most)
+    and partial sums of dx (of as many tiles as the CUs hold), forward a maximum and a sum per row and 64 words at most."""
+    features, pad = rows * -(-cols // 8) * 8, 1 << 20
+    assert need(True, rows, vocab, cols, dtype) <= 2 * (1 << 28) + 10 * features + max(4 * features, 1 << 27) + 8 * min(vocab, 1 << 20) + pad
+    assert need(False, rows, vocab, cols, dtype) <= (1 << 28) + 4 * features + (rows + 16) * 8 * (vocab // 64 + 1) + 8 * min(vocab, 1 << 20) + pad
+
+
+def test_binary32_work_space_is_smaller_than_large_logits():
+    for rows, vocab, cols in ((2048, 60_000, 512), (4096, 100_000, 1024), (8192, 141_000, 1000)):
+        for backward in (False, True):
+            assert need(backward, rows, vocab, cols, 0) < 4 * rows * vocab
