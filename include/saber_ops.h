@@ -17,7 +17,8 @@
  *     rounded once, to nearest even.  The same inputs give the same bits.
  *   - Every function returns SABER_OK or a negative saber_status (saber.h) and never throws;
  *     saber_ops_last_error() has the message of the calling thread's last failure.
- *   - Limits: fewer than 2^31 rows and words, at most 2^20 columns; cross entropy: fewer than 2^26 rows (ERANGE).
+ *   - Limits: fewer than 2^31 rows and words, at most 2^20 columns; cross entropy: at most 2^26 - 16 rows, and
+ *     fewer than 2^40 values of the features in its backward pass (ERANGE).
  */
 #ifndef SABER_OPS_H
 #define SABER_OPS_H

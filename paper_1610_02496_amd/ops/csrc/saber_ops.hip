@@ -26,7 +26,7 @@ int fail(int code, const char *fmt, ...) {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 20, kMaxWords = (int64_t)1 << 31;
 constexpr int kCus = 256;   // of gfx950: sizes of grids only
-constexpr int64_t kXentRows = (int64_t)1 << 26, kMaxTiles = (int64_t)1 << 24;   // (a launch has fewer than 2^32 threads)
+constexpr int64_t kXentRows = ((int64_t)1 << 26) - 16, kMaxTiles = (int64_t)1 << 24;   // (a launch has fewer than 2^32 threads)
 
 size_t size_of(int type) { return type == SABER_F32 ? 4 : 2; }
 bool is_type(int type) { return type == SABER_F32 || type == SABER_F16 || type == SABER_BF16; }
@@ -263,7 +263,7 @@ bool direct(const void *p, int64_t stride, int64_t cols, int dtype) {
 
 int check_xent(const char *who, Xent &c) {
     OPS_TRY(check_rows(who, c.rows, c.cols, c.dtype));
-    if (c.rows >= kXentRows) return fail(SABER_ERANGE, "%s: %lld rows (limit 2^26 - 1)", who, (long long)c.rows);
+    if (c.rows > kXentRows) return fail(SABER_ERANGE, "%s: %lld rows (limit 2^26 - 16)", who, (long long)c.rows);
     if (c.vocab < 1) return fail(SABER_EINVAL, "%s: a vocabulary of %lld words", who, (long long)c.vocab);
     if (c.vocab >= kMaxWords) return fail(SABER_ERANGE, "%s: a vocabulary of %lld words (limit 2^31 - 1)", who, (long long)c.vocab);
     OPS_TRY(check_stride(who, "x", c.x_stride, c.cols));
@@ -374,6 +374,7 @@ BackwardSpace backward_space(const Xent &c, Carve &s) {
         const int64_t tiles = parts_of(c.cols_pad, tile) * parts_of(row, tile);
         if (b.dx_tile == 64 && parts_of(kCus, tiles) <= steps / 16) b.dx_tile = tile;
     }
+    while (b.dx_tile < 256 && parts_of(c.cols_pad, b.dx_tile) * parts_of(row, b.dx_tile) >= kMaxTiles) b.dx_tile *= 2;
     const int64_t tiles = parts_of(c.cols_pad, b.dx_tile) * parts_of(row, b.dx_tile);
     int64_t splits = kCus * (b.dx_tile == 256 ? 1 : 2) / tiles;
     if (splits > steps / 8) splits = steps / 8;
@@ -525,6 +526,8 @@ extern "C" int saber_linear_xent_backward(const float *dloss, const void *x, int
     if (!workspace_bytes) return fail(SABER_EINVAL, "%s: workspace_bytes is null", who);
     Carve s{static_cast<char *>(workspace)};
     const BackwardSpace b = backward_space(c, s);
+    if (parts_of(c.cols_pad, b.dx_tile) * parts_of(rows, b.dx_tile) * b.splits >= kMaxTiles)   // (features of 2^40 values)
+        return fail(SABER_ERANGE, "%s: %lld rows of %lld columns", who, (long long)rows, (long long)cols);
     if (!workspace) { *workspace_bytes = s.at; return SABER_OK; }
     if (!aligned(workspace, 256)) return fail(SABER_EINVAL, "%s: the work space is not aligned to 256 bytes", who);
     if (*workspace_bytes < s.at) return fail(SABER_EINVAL, "%s: work space of %lld bytes, %lld are needed", who, (long long)*workspace_bytes, (long long)s.at);

@@ -53,3 +53,32 @@ def test_binary32_work_space_is_smaller_than_large_logits():
     for rows, vocab, cols in ((2048, 60_000, 512), (4096, 100_000, 1024), (8192, 141_000, 1000)):
         for backward in (False, True):
             assert need(backward, rows, vocab, cols, 0) < 4 * rows * vocab
+
+
+def test_the_largest_batches_are_refused_up_front_or_launched_whole(tmp_path):
+    """Either every launch of a call stays within the runtime's limits (fewer than 2^32 threads), or nothing is launched at all."""
+    lib = fake_hip.build(tmp_path)
+    fake_hip.run(lib, """
+    L = pk.load_library()
+    space = np.zeros(1 << 16, dtype=np.uint8)
+    P = (space.ctypes.data + 255) // 256 * 256
+    n = ctypes.c_int64()
+    refused = 0
+    for rows in ((1 << 26) - 17, (1 << 26) - 16, (1 << 26) - 15, (1 << 26) - 1, 1 << 26, 1 << 25):
+        for vocab, cols in ((1, 1), (300, 64), (70000, 1024), (300, 9000), (20, 1 << 18)):
+            for dtype in (0, 1, 2):
+                for backward in (0, 1):
+                    args = ([P] if backward else []) + [P, cols, P, cols, P, 0] + ([P] if backward else []) + [rows, vocab, cols, dtype, P, P]
+                    call = L.saber_linear_xent_backward if backward else L.saber_linear_xent_forward
+                    before = launches("kernel")[0]
+                    rc = call(*args, None, ctypes.addressof(n), None)
+                    if rc == 0:
+                        rc = call(*args, P, ctypes.addressof(n), None)
+                        assert rc == 0, (rows, vocab, cols, dtype, backward, L.saber_ops_last_error())
+                    else:
+                        refused += 1
+                        assert rc == pk.binding.SABER_ERANGE and launches("kernel")[0] == before
+                    assert (rows <= (1 << 26) - 16) or rc != 0
+                    assert not (rows <= (1 << 26) - 16 and cols <= 9000) or rc == 0, (rows, vocab, cols, dtype, backward, L.saber_ops_last_error())
+    assert refused
+    """)
