@@ -63,7 +63,8 @@ __device__ __forceinline__ void each(F &&f) { each(std::make_integer_sequence<in
 // One product.  With 64 of them a wave's sums are 256 registers, which have to stay in accumulation registers, each in its place; the
 // compiler moves them about, so here they are bound in assembly.  Two waits are the program's then: an operand that a vector
 // instruction wrote may be read two states later (FIRST: of a row of fragments; all of them come from LDS, which has a counter), and
-// the sums may be read seven states after their last product (settled()).
+// the sums may be read seven states after their last product (settled()).  Waiting before every product would cost 2 to 4 % of a training
+// step, so that the compiler puts no vector instruction in between is checked in the built code (tests/test_ops_waits.py).
 template <class T, bool FIRST>
 __device__ __forceinline__ void mfma(u32x4 a, u32x4 b, f32x4 &c) {
     if constexpr (FIRST) asm volatile("s_nop 1");
@@ -85,7 +86,8 @@ __device__ __forceinline__ int slow_swizzle(int k) { return ((k & 3) | (U == 128
 
 // 16 bytes per lane from the buffer to LDS, lane after lane from `lds` on, past the registers.  Nothing waits for it but a wait for
 // the vector memory counter; in assembly, because the compiler puts such a wait in front of every later read of LDS.  The load has no
-// result register, so there is none that could be used too early.  m0 needs a state between its write and its use: the addition.
+// result register, so there is none that could be used too early.  m0 needs a state between its write and its use, the addition; the
+// descriptor five if a vector instruction wrote it, which the same test checks.
 __device__ __forceinline__ void load_to_lds(u32x4 rsrc, LdsBytes *lds, uint32_t off, uint32_t more) {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
     uint32_t sum;
