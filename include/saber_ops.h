@@ -67,8 +67,9 @@ int saber_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, 
 
 /*
  * An activation in 8 bits.  Every 128 columns of a row (the last block may be shorter) share a step
- * c = max|x| / 127 (binary32); an element is held as round(x / c), ties to even, within -127 .. 127, and restored as
- * that number times c: at most half a step off.  A block of zeros has step 0.  A block with an infinity or NaN is
+ * c = max|x| / 127 (binary32, and at most the largest c of which 127 c is finite); an element is held as round(x / c), ties
+ * to even, within -127 .. 127, and restored as that number times c: at most half a step off where c is a normal number
+ * (below, c itself is rounded coarsely).  A block of zeros has step 0.  A block with an infinity or NaN is
  * restored as NaN.
  *   q [rows][cols], scale [rows][ceil(cols / 128)]
  */

@@ -103,7 +103,8 @@ def _ptr(t):
 
 class Checkpoint8:
     """An activation in 8 bits: ``q`` (int8, the shape of the activation) times ``scale`` (float32, one step per 128
-    columns of a row).  An element is off by half a step at most, a 254th of its block's largest magnitude."""
+    columns of a row).  An element is off by half a step at most, a 254th of its block's largest magnitude (blocks whose
+    largest is below 2^-119, where steps are not normal numbers, are held more coarsely)."""
 
     __slots__ = ("q", "scale", "dtype")
 

@@ -117,14 +117,17 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 }
 
 // One lane's chunk of a block of 128 columns, in 8 bits: step c = max|x| / 127 of the block, whole numbers round(x / c), ties to
-// even.  A block of zeros has step 0.  A NaN or an infinity makes the step not finite: the block is restored as NaN.
+// even.  A block of zeros has step 0; a step ends where 127 of it are finite (kMostStep: the largest number of binary32, a mask's value
+// perhaps, is restored one unit lower, not as infinity).  A NaN or an infinity makes the step not finite: the block is restored as NaN.
 // All 16 lanes of the block call this together.
 __device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     top = row_max(top);
-    const float step = __uint_as_float(top) / 127.f;
+    constexpr float kMostStep = 0x1.020406p+121f;
+    float step = __uint_as_float(top) / 127.f;
+    step = top < 0x7f800000u ? fminf(step, kMostStep) : step;
     // x / step is rounded twice, to binary32 and to a whole number.  The product with the inverse is off by 2^-22 * 127 at most, so it
     // gives the same whole number unless it is as near as that to the middle of two: then, rarely, the division decides.
     // Adding 1.5 * 2^23 rounds to a whole number, which the sum's low byte then holds in two's complement.

@@ -217,3 +217,18 @@ def test_a_loss_may_be_changed_in_place():
         loss.sum().backward()
         grads.append((xs.grad, ws.grad))
     assert torch.equal(grads[0][0], grads[1][0]) and torch.equal(grads[0][1], grads[1][1])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_checkpoints_of_the_largest_numbers_are_finite(dtype):
+    """The type's largest and lowest value, as masks hold them, come back within half a step."""
+    most = torch.finfo(dtype).max
+    x = normal(1, 9, 300).to(dtype)
+    x[0, 5], x[1, 7], x[2, :] = most, -most, most
+    x[3, 100] = -most * (1 - 2.0 ** -8)
+    x[4, 200], x[4, 201] = most, most / 2
+    for c in (pk.ops.checkpoint8(x.cuda()), pk.ops.layer_norm_forward(x.cuda(), checkpoint=True)[1].checkpoint):
+        got = c.restore().double().cpu()
+        step = c.scale.double().cpu().repeat_interleave(128, 1)[:, :300]
+        assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(c.scale).all())
+        assert bool(((got - x.double()).abs() <= step * (0.5 + 2.0 ** -15) + ROUND[dtype] * x.double().abs()).all())
