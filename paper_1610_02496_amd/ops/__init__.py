@@ -241,6 +241,8 @@ def _head(x, weight, target):
     _device(weight, "weight", device)
     if weight.dtype != x.dtype:
         raise TypeError("weight must be %s like x, not %s" % (x.dtype, weight.dtype))
+    if not x.dim():
+        raise ValueError("x has no columns")
     if weight.dim() != 2 or weight.shape[1] != x.shape[-1]:
         raise ValueError("weight must be [words, %d] for features of that width" % x.shape[-1])
     _device(target, "target", device)

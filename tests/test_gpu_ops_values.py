@@ -232,3 +232,14 @@ def test_checkpoints_of_the_largest_numbers_are_finite(dtype):
         step = c.scale.double().cpu().repeat_interleave(128, 1)[:, :300]
         assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(c.scale).all())
         assert bool(((got - x.double()).abs() <= step * (0.5 + 2.0 ** -15) + ROUND[dtype] * x.double().abs()).all())
+
+
+def test_features_without_a_dimension_are_refused():
+    w, t = torch.zeros(10, 1, device="cuda"), torch.zeros((), dtype=torch.int64, device="cuda")
+    for x in (torch.tensor(1.0, device="cuda"), torch.zeros((), device="cuda")):
+        for call in (lambda: pk.ops.linear_cross_entropy(x, w, t), lambda: pk.ops.linear_cross_entropy_backward(x, x, w, t, x), lambda: pk.ops.layer_norm(x),
+                     lambda: pk.ops.checkpoint8(x)):
+            with pytest.raises(ValueError):
+                call()
+    loss, lse = pk.ops.linear_cross_entropy_forward(torch.ones(1, device="cuda"), w, t)   # a single row, of one column
+    assert loss.shape == () and abs(float(lse) - 2.302585) < 1e-6
