@@ -30,9 +30,11 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
 }
 
 // exp(l - m) by the hardware's 2^x.  The difference is rounded before it is scaled, so logits of any size keep their precision; the
-// scaling costs 2^-24 |l - m| log2(e), far below the 2^-9 (2^-12) with which a result of 16 bits is stored.  EXACT, for features of
+// scaling costs up to 2^-24 |l - m| log2(e) of each exponential.  Next to the rounding of the logits' own binary32 sums that is little:
+// a loss is off by 1e-7 at most where it was by 1e-8, d by far less than the 2^-9 (2^-12) with which it is stored.  EXACT, for features of
 // binary32: what the scaling's rounding left is put back, exp(d) = 2^h (1 + ln 2 (d log2 e - h)), to about an ulp (a call of expf, of
-// whose range little is needed, took a third of the logits' kernel).
+// whose range little is needed, took a third of the logits' kernel).  For 16-bit features that would cost 8 % of a score of 8192 rows of
+// 1000 and 141,000 words (2.56 -> 2.76 ms).
 template <bool EXACT>
 struct Exp {
     float m;
