@@ -55,7 +55,9 @@ int saber_layer_norm_backward_workspace(int64_t rows, int64_t cols, int64_t *byt
 /*
  * Gradients of the above: with h = (x - m) rstd and g = dy * weight
  *   dx = rstd (g - mean(g) - h mean(g h)),  dweight = sum over rows of dy h,  dbias = sum over rows of dy
- *   dy [rows][cols] of dtype; x as in the forward pass, or NULL with a checkpoint of it in q and scale
+ *   dy [rows][cols] of dtype; x as in the forward pass, or NULL with a checkpoint of it in q and scale: the values that
+ *                 the checkpoint stands for then take the place of x in h, with m and rstd of x itself (an approximation,
+ *                 half a step of the checkpoint off at most; h then has not exactly mean 0 and variance 1)
  *   dx [rows][cols] of dtype, dweight and dbias [cols] of wtype; any of them may be NULL (not computed)
  *   workspace     needed for dweight or dbias
  * No rows give zeros for dweight and dbias.  Errors: EINVAL, ERANGE, EDEVICE.

@@ -229,7 +229,9 @@ class _LayerNorm(torch.autograd.Function):
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, checkpoint=False):
     """Layer norm over the last dimension, differentiable in ``x``, ``weight`` and ``bias``.  With ``checkpoint`` its input is
-    held in 8 bits between the passes (a quarter to a half of the memory); the gradients then are those at the held values."""
+    held in 8 bits between the passes (a quarter to a half of the memory).  The gradients then are an approximation: the held values
+    stand in place of the input, half a step of the checkpoint off at most, but mean and deviation remain those of the input itself
+    (so a row of ``x``'s gradient adds up to zero only to that precision)."""
     return _LayerNorm.apply(x, weight, bias, eps, checkpoint)
 
 
@@ -310,7 +312,8 @@ class _LinearCrossEntropy(torch.autograd.Function):
 
 def linear_cross_entropy(x, weight, target, reduction="mean"):
     """Softmax cross entropy of ``x weight^T`` against ``target``, differentiable in ``x`` and ``weight``.  The logits are not in
-    memory in either pass; their gradient is, for one piece of the vocabulary at a time (256 MB at most).  Rows with a negative target are left out; ``reduction``: "mean" over the rows counted (0 if
+    memory in either pass; their gradient is, for one piece of the vocabulary at a time (256 MB at most).  In 16-bit types that
+    gradient is rounded to the type of ``x`` before the two products that follow.  Rows with a negative target are left out; ``reduction``: "mean" over the rows counted (0 if
     there is none), "sum" or "none"."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none, not %r" % (reduction,))

@@ -15,7 +15,8 @@
 // Rows and columns outside the operands are read as zeros (the bounds of the buffer descriptors), so no tile reads out of range.
 //
 // Operands of binary32 come as planes, and the products of planes that matter are added as further steps along k ("segments"):
-//   three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each), six segments, any range of values;
+//   three planes of bfloat16, x = x1 + x2 + x3 exactly (8 bits of the significand each), six segments, any range of values; what is left
+//   out (x2 y3, x3 y2, x3 y3) is up to 2^-21 of the product, always to the side of zero, as the planes are cut off;
 //   two planes of binary16, x = x1 + x2 to 2^-23, three segments, for operands whose rows were brought to one magnitude and hold little
 //   that is far below it; what is left out is up to 2^-22 of the product of two magnitudes.  Tiles of other rows are left to another
 //   kernel.

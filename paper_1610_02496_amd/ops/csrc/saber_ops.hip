@@ -237,9 +237,10 @@ namespace {
 
 // Up to 64 rows whose features fit LDS go through the kernel for few rows.  It reads the projection as it lies where the products would
 // have it packed first (us of few rows and of products: 61 rows of 777 in f16, 30,011 words, 31 and 39; 1 row of 2048 in f32, 100,000
-// words, 263 and 654), and shares out long rows of few words (9 rows in bf16: 2048 columns of 1000 words 15.8 and 23.0, 1024 of 30,000
-// 25.4 and 28.4).  Where a 16-bit projection lies well and is large the two are alike, within a sixth (1024 of 100,000 82.6 and 83.4, 2048
-// of 100,000 149 and 129).
+// words, 263 and 654), and shares out long rows of few words (9 rows in bf16, which the caches do not hold yet: 2048 columns of 1000 words
+// 15.8 and 23.0, 1024 of 30,000 25.4 and 28.4).  Where a 16-bit projection lies well and is large it gains nothing (9 rows of 1024 and
+// 100,000 words 82.6 and 83.4) or loses: 9 rows of 2048, 149 and 129; 60 rows of 64, 43 and 22.  The rule stays as simple as it is: what it
+// loses there is a part of a call that reads the whole projection for a handful of rows.
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewLds = 150 * 1024;
 // 16-bit values of d, and of packed words, per piece: 256 MB of each, what the last-level cache holds.  A value of binary32 is three of d,
