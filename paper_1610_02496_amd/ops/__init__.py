@@ -313,8 +313,8 @@ class _LinearCrossEntropy(torch.autograd.Function):
 def linear_cross_entropy(x, weight, target, reduction="mean"):
     """Softmax cross entropy of ``x weight^T`` against ``target``, differentiable in ``x`` and ``weight``.  The logits are not in
     memory in either pass; their gradient is, for one piece of the vocabulary at a time (256 MB at most).  In 16-bit types that
-    gradient is rounded to the type of ``x`` before the two products that follow.  Rows with a negative target are left out; ``reduction``: "mean" over the rows counted (0 if
-    there is none), "sum" or "none"."""
+    gradient is rounded to the type of ``x`` before the two products that follow.  Rows with a negative target are left out;
+    ``reduction``: "mean" over the rows counted (0 if there is none), "sum" or "none"."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none, not %r" % (reduction,))
     loss = _LinearCrossEntropy.apply(x, weight, target)
