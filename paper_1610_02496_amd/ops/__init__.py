@@ -8,10 +8,15 @@ The work is done by the HIP kernels behind the C ABI of ``include/saber_ops.h``;
 the graph of gradients.  Everything is enqueued on torch's current stream of the tensors' device: nothing is waited
 for, and calls may be captured into a graph.  Arguments are checked on the host (ValueError, TypeError, or SaberError
 from the library).  There is no CPU fallback.
+
+A program that uses the sampler as well imports torch before it: the library then runs on torch's HIP runtime.  Loaded
+first it brings the system's, which knows neither torch's streams nor the order of its work, and importing this module
+raises ImportError.
 """
 from __future__ import annotations
 
 import ctypes
+import os
 
 import torch
 
@@ -27,6 +32,18 @@ _int64 = ctypes.c_int64
 _F32 = torch.float32
 
 _L = load_library()
+
+
+def _check_runtime():
+    """That the library and torch share one HIP runtime: a second one in the process is the one the library was loaded with."""
+    with open("/proc/self/maps") as f:
+        paths = {os.path.realpath(line.split(None, 5)[5].strip()) for line in f if "/libamdhip64" in line}
+    if len(paths) > 1:
+        raise ImportError("libsaber.so was loaded before torch, on another HIP runtime than torch's (%s): import torch before the "
+                          "first use of paper_1610_02496_amd" % ", ".join(sorted(paths)))
+
+
+_check_runtime()
 _norm_forward, _norm_backward, _norm_space = (_L.saber_layer_norm_forward, _L.saber_layer_norm_backward,
                                               _L.saber_layer_norm_backward_workspace)
 _save8, _restore8 = _L.saber_checkpoint8_save, _L.saber_checkpoint8_restore
