@@ -1,9 +1,10 @@
 /*
  * saber_ops.h - operators of a head that is trained on a topic model's features (gfx950): layer norm, softmax cross
- * entropy together with its projection onto the vocabulary, and activation checkpoints in 8 bits.
+ * entropy together with its projection onto the vocabulary, and activation checkpoints in 8 bits; and of one that
+ * answers: root-mean-square norm of a residual stream, rows in 8 bits and their product, words drawn from logits.
  *
  * The head takes features of every token (its topic of saber_get_z, its document's row of A, an embedding of the word
- * before) through a norm to logits over the sampler's own vocabulary and scores the token's word.
+ * before) through a norm to logits over the sampler's own vocabulary and scores the token's word, or draws one.
  *
  * Conventions
  *   - Every pointer to data is a DEVICE pointer (tensors stay where they are); the caller owns all of them, the work
@@ -18,7 +19,8 @@
  *   - Every function returns SABER_OK or a negative saber_status (saber.h) and never throws;
  *     saber_ops_last_error() has the message of the calling thread's last failure.
  *   - Limits: fewer than 2^31 rows and words, at most 2^20 columns; cross entropy: at most 2^26 - 16 rows, and
- *     fewer than 2^40 values of the features in its backward pass (ERANGE).
+ *     fewer than 2^40 values of the features in its backward pass; products of 8-bit rows: at most 2^17 - 1 columns and
+ *     2^24 tiles of 256 x 256 logits; drawing: fewer than 2^31 words (ERANGE).
  */
 #ifndef SABER_OPS_H
 #define SABER_OPS_H
@@ -109,6 +111,83 @@ int saber_linear_xent_backward(const float *dloss, const void *x, int64_t x_stri
                                const void *target, int target64, const float *lse, int64_t rows, int64_t vocab,
                                int64_t cols, int dtype, void *dx, void *dweight, void *workspace,
                                int64_t *workspace_bytes, void *stream);
+
+/*
+ * Root-mean-square norm of every row of a residual stream: s = x + residual, rounded to the stream's type,
+ * r = 1 / sqrt(mean s^2 + eps), y = s r weight.  The norm is of the sum as it is held.
+ *   x [rows][cols] of dtype; residual [rows][cols] of rtype (dtype or SABER_F32), or NULL: then s = x, rtype is dtype and
+ *                 sum is NULL
+ *   weight [cols] of wtype, or NULL (ones)
+ *   sum [rows][cols] of rtype: s
+ *   y [rows][cols] of dtype; or y NULL and q, q_stride, scale: y in 8 bits (saber_rows8_save).  With t = s weight in
+ *                 binary32, c = max|t| / 127 of the row: q = round(t / c), scale = c r
+ *   rstd [rows]: r, what the backward pass needs; or NULL
+ * Errors: EINVAL, ERANGE, EDEVICE.
+ */
+int saber_rms_norm_forward(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                           const void *weight, int64_t rows, int64_t cols, int dtype, int rtype, int wtype, float eps,
+                           void *sum, void *y, float *rstd, int8_t *q, int64_t q_stride, float *scale, void *stream);
+
+/* Bytes of work space that saber_rms_norm_backward needs for dweight. */
+int saber_rms_norm_backward_workspace(int64_t rows, int64_t cols, int64_t *bytes);
+
+/*
+ * Gradients of the above (of y, not of its form in 8 bits): with h = s r and g = dy * weight
+ *   ds = r (g - h mean(g h)) + dsum,  dweight = sum over rows of dy h
+ *   dy [rows][cols] of dtype; dsum [rows][cols] of rtype, the gradient of the sum as the stream goes on with it, or NULL
+ *   s [rows][cols] of rtype: the sum (x, where there was no residual)
+ *   dx of dtype, dresidual of rtype, both [rows][cols]: ds, rounded to either type; dweight [cols] of wtype; any may be NULL
+ *   workspace     needed for dweight
+ * No rows give zeros for dweight.  Errors: EINVAL, ERANGE, EDEVICE.
+ */
+int saber_rms_norm_backward(const void *dy, int64_t dy_stride, const void *dsum, int64_t dsum_stride, const void *s,
+                            int64_t s_stride, const float *rstd, const void *weight, int64_t rows, int64_t cols, int dtype,
+                            int rtype, int wtype, void *dx, void *dresidual, void *dweight, void *workspace,
+                            int64_t workspace_bytes, void *stream);
+
+/*
+ * Rows in 8 bits, the operands of saber_linear8: a row has one step c = max|x| / 127 (binary32, and at most the largest c
+ * of which 127 c is finite), an element is held as round(x / c), ties to even, and restored as that number times c.  A row
+ * of zeros has step 0; one with an infinity or NaN is restored as NaN.
+ *   q: rows of cols bytes that start at multiples of 16 bytes, q_stride bytes apart (a multiple of 16); those up to the next
+ *      multiple of 16 are zeros (written by saber_rows8_save)
+ *   scale [rows]: the steps
+ */
+int saber_rows8_save(const void *x, int64_t x_stride, int64_t rows, int64_t cols, int dtype, int8_t *q, int64_t q_stride,
+                     float *scale, void *stream);
+int saber_rows8_restore(const int8_t *q, int64_t q_stride, const float *scale, int64_t rows, int64_t cols, int dtype,
+                        void *x, void *stream);
+
+/*
+ * Logits from rows in 8 bits: out_nv = (sum over k of x_nk weight_vk) x_scale_n w_scale_v.  The sums are int32 and exact, the
+ * scales are multiplied in binary32 in this order, the result is rounded once.
+ *   x [rows][cols], weight [words][cols] as above; values -128 .. 127; out [rows][words] of dtype
+ * Errors: EINVAL, ERANGE, EDEVICE.
+ */
+int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_scale, const int8_t *weight, int64_t w_stride,
+                  const float *w_scale, int64_t rows, int64_t words, int64_t cols, int dtype, void *out, void *stream);
+
+/*
+ * Draws a word for every row of logits l by the row's random number u: with z = (l - max l) / temperature and the words in
+ * falling order of their logits, equal ones in the order of their numbers, these are left:
+ *   the first top_k (0 or less: all), of them the fewest that hold top_p of their sum of exp z (1 or more: all), of them
+ *   those of exp z >= min_p; always the first one
+ * and the first word, by number, is taken at which the sum of exp z of the words left exceeds u times that of all of them.
+ * The masses are sums of whole multiples of 2^-45 (of 2^(ceil(log2 words) - 62) beyond 2^17 words) of the likeliest
+ * word's: what is below half of that has none.  The limits are compared in 64 bits.
+ *   logits [rows][words] of dtype; -inf leaves a word out, infinite ones share all of the mass
+ *   temperatures, top_ks (int32, or int64 if top_k64), top_ps, min_ps [rows]: a value per row, or NULL: then temperature,
+ *                 top_k, top_p, min_p hold for all rows (and are checked).  A temperature of 0 (or less, or NaN) takes the
+ *                 first word of the largest logit, whatever the limits.  As values per row a top_p or min_p below 0
+ *                 counts as 0, beyond 1 as 1, and NaN as no limit.
+ *   u [rows]: within [0, 1); what is outside counts as the next number within, NaN as 0
+ *   word [rows], p [rows]: the word and its share of the mass left.  A row of which nothing is left (all -inf): -1 and 0.
+ *                 One with a NaN: -1 and NaN.
+ * Errors: EINVAL, ERANGE, EDEVICE.
+ */
+int saber_sample(const void *logits, int64_t stride, int64_t rows, int64_t words, int dtype, const float *u,
+                 const float *temperatures, float temperature, const void *top_ks, int top_k64, int64_t top_k,
+                 const float *top_ps, float top_p, const float *min_ps, float min_p, int64_t *word, float *p, void *stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,9 @@ EXPORTS = ["saber_set_hooks", "saber_options_default", "saber_init_ex", "saber_i
            "saber_get_stream", "saber_bandwidth_probe", "saber_alias_build_probe", "saber_get_alias"]
 # and include/saber_ops.h (called from ops/)
 EXPORTS += ["saber_ops_last_error", "saber_layer_norm_forward", "saber_layer_norm_backward_workspace", "saber_layer_norm_backward",
-            "saber_checkpoint8_save", "saber_checkpoint8_restore", "saber_linear_xent_forward", "saber_linear_xent_backward"]
+            "saber_checkpoint8_save", "saber_checkpoint8_restore", "saber_linear_xent_forward", "saber_linear_xent_backward",
+            "saber_rms_norm_forward", "saber_rms_norm_backward_workspace", "saber_rms_norm_backward", "saber_rows8_save", "saber_rows8_restore",
+            "saber_linear8", "saber_sample"]
 
 
 class SaberError(RuntimeError):
@@ -107,6 +109,15 @@ def load_library():
         "saber_linear_xent_forward": (ctypes.c_int, [vp, i64, vp, i64, vp, ctypes.c_int, i64, i64, i64, ctypes.c_int, vp, vp, vp, vp, vp]),
         "saber_linear_xent_backward": (ctypes.c_int, [vp, vp, i64, vp, i64, vp, ctypes.c_int, vp, i64, i64, i64, ctypes.c_int, vp, vp,
                                                       vp, vp, vp]),
+        "saber_rms_norm_forward": (ctypes.c_int, [vp, i64, vp, i64, vp, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, f32, vp, vp, vp, vp, i64,
+                                                  vp, vp]),
+        "saber_rms_norm_backward_workspace": (ctypes.c_int, [i64, i64, vp]),
+        "saber_rms_norm_backward": (ctypes.c_int, [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, vp, vp,
+                                                   vp, i64, vp]),
+        "saber_rows8_save": (ctypes.c_int, [vp, i64, i64, i64, ctypes.c_int, vp, i64, vp, vp]),
+        "saber_rows8_restore": (ctypes.c_int, [vp, i64, vp, i64, i64, ctypes.c_int, vp, vp]),
+        "saber_linear8": (ctypes.c_int, [vp, i64, vp, vp, i64, vp, i64, i64, i64, ctypes.c_int, vp, vp]),
+        "saber_sample": (ctypes.c_int, [vp, i64, i64, i64, ctypes.c_int, vp, vp, f32, vp, ctypes.c_int, i64, vp, f32, vp, f32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

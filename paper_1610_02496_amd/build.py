@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsaber.so")
 OPS_CSRC = os.path.join(HERE, "ops", "csrc")
-SOURCES = [os.path.join(CSRC, "saber.hip"), os.path.join(OPS_CSRC, "saber_ops.hip")]
+SOURCES = [os.path.join(CSRC, "saber.hip"), os.path.join(OPS_CSRC, "saber_ops.hip"), os.path.join(OPS_CSRC, "saber_answer.hip")]
 # every header the sources include: an edit to any of them marks the library stale
 DEPS = SOURCES + sorted(glob.glob(os.path.join(CSRC, "*.hpp"))) + sorted(glob.glob(os.path.join(OPS_CSRC, "*.hpp"))) + sorted(glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
 

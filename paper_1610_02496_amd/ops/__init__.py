@@ -1,8 +1,11 @@
-"""Operators of a head that is trained on a topic model's features, on torch tensors in device memory.
+"""Operators of a head that is trained on a topic model's features and answers from them, on torch tensors in device memory.
 
-``layer_norm``, ``linear_cross_entropy``   differentiable, for a training loop written with torch
-``layer_norm_forward`` / ``_backward``, ``linear_cross_entropy_forward`` / ``_backward``   the passes themselves
+``layer_norm``, ``rms_norm``, ``linear_cross_entropy``   differentiable, for a training loop written with torch
+``layer_norm_forward`` / ``_backward``, ``rms_norm_forward`` / ``_backward``, ``linear_cross_entropy_forward`` / ``_backward``   the
+                                           passes themselves
 ``checkpoint8``                            an activation held in 8 bits
+``rms_norm8``, ``rows8``, ``linear8``      serving in 8 bits: the norm's output, rows of a matrix, logits from both
+``sample``                                 a word drawn for every row of logits: temperature, top-k, top-p, min-p
 
 The work is done by the HIP kernels behind the C ABI of ``include/saber_ops.h``; torch supplies memory, streams and
 the graph of gradients.  Everything is enqueued on torch's current stream of the tensors' device: nothing is waited
@@ -22,8 +25,9 @@ import torch
 
 from ..binding import SABER_OK, SaberError, load_library
 
-__all__ = ["Checkpoint8", "NormSaved", "checkpoint8", "layer_norm", "layer_norm_backward", "layer_norm_forward",
-           "linear_cross_entropy", "linear_cross_entropy_backward", "linear_cross_entropy_forward"]
+__all__ = ["Checkpoint8", "NormSaved", "RmsSaved", "Rows8", "checkpoint8", "layer_norm", "layer_norm_backward", "layer_norm_forward", "linear8",
+           "linear_cross_entropy", "linear_cross_entropy_backward", "linear_cross_entropy_forward", "rms_norm", "rms_norm8",
+           "rms_norm_backward", "rms_norm_forward", "rows8", "sample"]
 
 BLOCK = 128   # columns that share a step of a checkpoint
 
@@ -48,6 +52,8 @@ _norm_forward, _norm_backward, _norm_space = (_L.saber_layer_norm_forward, _L.sa
                                               _L.saber_layer_norm_backward_workspace)
 _save8, _restore8 = _L.saber_checkpoint8_save, _L.saber_checkpoint8_restore
 _xent_forward, _xent_backward = _L.saber_linear_xent_forward, _L.saber_linear_xent_backward
+_rms_forward, _rms_backward, _rms_space = _L.saber_rms_norm_forward, _L.saber_rms_norm_backward, _L.saber_rms_norm_backward_workspace
+_rows8_save, _rows8_restore, _linear8, _sample = _L.saber_rows8_save, _L.saber_rows8_restore, _L.saber_linear8, _L.saber_sample
 
 # without the objects that torch.cuda.current_stream() makes on every call (2 us of a call of 12)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -339,3 +345,258 @@ def linear_cross_entropy(x, weight, target, reduction="mean"):
         return loss
     loss = loss.sum()
     return loss / (target >= 0).sum().clamp_(min=1) if reduction == "mean" else loss
+
+
+# ---- root-mean-square norm of a residual stream -------------------------------------------------------------------------
+
+class RmsSaved:
+    """What the backward pass of a root-mean-square norm needs: the rows it is of (``x``: the sum with the residual, where there
+    was one, which the stream goes on with), its weight, 1 / root mean square of every row, and the features' type."""
+
+    __slots__ = ("x", "weight", "rstd", "dtype", "residual")
+
+    def __init__(self, x, weight, rstd, dtype, residual):
+        self.x, self.weight, self.rstd, self.dtype, self.residual = x, weight, rstd, dtype, residual
+
+
+def _rms(x, weight, residual, eps, held):
+    device = _device(x, "x")
+    code = rcode = wcode = _type("x", x)
+    m, rows, cols, stride = _rows(x, "x")
+    if weight is not None:
+        weight = _vector(weight, "weight", cols, device, "x")
+        wcode = _type("weight", weight)
+    r, r_stride, total = None, 0, None
+    if residual is not None:
+        _device(residual, "residual", device)
+        if residual.dtype not in (x.dtype, _F32):
+            raise TypeError("residual must be %s like x, or float32, not %s" % (x.dtype, residual.dtype))
+        if residual.shape != x.shape:
+            raise ValueError("residual must have the shape of x")
+        rcode = _TYPES[residual.dtype]
+        r, _, _, r_stride = _rows(residual, "residual")
+        total = torch.empty_like(r)
+    y, rstd, c, q, q_stride, scale = None, None, None, None, 0, None
+    if held:
+        c = _empty_rows8(x, rows, cols)
+        q, q_stride, scale = c.q.data_ptr(), c._stride, c.scale.data_ptr()
+    else:
+        y = torch.empty_like(m)
+        rstd = x.new_empty(rows, dtype=_F32)
+    _launch(_rms_forward, device, m.data_ptr(), stride, _ptr(r), r_stride, _ptr(weight), rows, cols, code, rcode, wcode, eps, _ptr(total), _ptr(y), _ptr(rstd),
+            q, q_stride, scale)
+    return y, c, m if total is None else total, weight, rstd
+
+
+def rms_norm_forward(x, weight=None, residual=None, eps=1e-6):
+    """Root-mean-square norm of ``x + residual`` over the last dimension: ``(y, saved)``; ``saved.x`` is the sum, in the type of
+    ``residual`` (that of ``x``, or float32), which the stream goes on with.  The norm is of the sum as it is held.  ``weight``: a
+    vector of a floating type, its own or that of ``x``."""
+    y, _, total, weight, rstd = _rms(x, weight, residual, eps, False)
+    return y, RmsSaved(total, weight, rstd, x.dtype, residual is not None)
+
+
+def rms_norm_backward(dy, saved, dsum=None, need_x=True, need_residual=True, need_weight=True):
+    """``(dx, dresidual, dweight)`` of a root-mean-square norm for the gradient ``dy`` of its output and, where the stream goes on,
+    ``dsum`` of the sum; None where not needed or not there.  Both of the first two are the gradient of the sum, in the type
+    of ``x`` and of the residual: one tensor if these are the same."""
+    s, rstd, weight = saved.x, saved.rstd, saved.weight
+    device = _device(dy, "dy", s.device)
+    if dy.dtype != saved.dtype:
+        raise TypeError("dy must be %s like the norm's input, not %s" % (saved.dtype, dy.dtype))
+    m, rows, cols, stride = _rows(dy, "dy")
+    if dy.shape != s.shape:
+        raise ValueError("dy must have the shape of the norm's input")
+    d, d_stride = None, 0
+    if dsum is not None:
+        _device(dsum, "dsum", device)
+        if dsum.dtype != s.dtype:
+            raise TypeError("dsum must be %s like the sum, not %s" % (s.dtype, dsum.dtype))
+        if dsum.shape != s.shape:
+            raise ValueError("dsum must have the shape of the sum")
+        d, _, _, d_stride = _rows(dsum, "dsum")
+    need_residual = need_residual and saved.residual
+    same = s.dtype == saved.dtype
+    dx = torch.empty_like(m) if need_x or (same and need_residual) else None
+    dresidual = torch.empty_like(m, dtype=s.dtype) if need_residual and not same else None
+    dweight = torch.empty_like(weight) if need_weight and weight is not None else None
+    space, nbytes = None, 0
+    if dweight is not None:
+        n = _int64()
+        _check(_rms_space(rows, cols, ctypes.addressof(n)))
+        nbytes = n.value
+        space = dy.new_empty(nbytes, dtype=torch.uint8)
+    code = _TYPES[saved.dtype]
+    x, _, _, x_stride = _rows(s, "s")
+    _launch(_rms_backward, device, m.data_ptr(), stride, _ptr(d), d_stride, x.data_ptr(), x_stride, rstd.data_ptr(), _ptr(weight), rows, cols, code,
+            _TYPES[s.dtype], code if weight is None else _TYPES[weight.dtype], _ptr(dx), _ptr(dresidual), _ptr(dweight), _ptr(space), nbytes)
+    return dx if need_x else None, (dx if same else dresidual) if need_residual else None, dweight
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, s = rms_norm_forward(x, weight, residual, eps)
+        ctx.save_for_backward(s.x, s.weight, s.rstd)
+        ctx.dtype, ctx.residual = s.dtype, s.residual
+        ctx.set_materialize_grads(False)
+        return (y, s.x) if s.residual else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dsum=None):
+        x, weight, rstd = ctx.saved_tensors
+        need_x, need_weight, need_residual = ctx.needs_input_grad[:3]
+        if dy is None:   # (only the sum was used)
+            if dsum is None:
+                return None, None, None, None
+            return dsum.to(ctx.dtype) if need_x else None, None, dsum if need_residual else None, None
+        dx, dresidual, dweight = rms_norm_backward(dy, RmsSaved(x, weight, rstd, ctx.dtype, ctx.residual), dsum, need_x, need_residual, need_weight)
+        return dx, dweight, dresidual, None
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6):
+    """Root-mean-square norm over the last dimension, differentiable in ``x``, ``weight`` and ``residual``: ``y``, or with a residual
+    stream ``(y, sum)``, the norm of ``x + residual`` and that sum, which the stream goes on with."""
+    return _RmsNorm.apply(x, weight, residual, eps)
+
+
+# ---- rows in 8 bits, and logits from them -------------------------------------------------------------------------------
+
+class Rows8:
+    """A matrix in 8 bits: ``q`` (int8; rows start at multiples of 16 bytes, with zeros in between) times ``scale`` (float32, one step
+    per row, a 127th of its largest magnitude).  What ``rows8`` makes of features and weights and ``linear8`` multiplies."""
+
+    __slots__ = ("q", "scale", "dtype", "_stride")
+
+    def __init__(self, q, scale, dtype, stride):
+        self.q, self.scale, self.dtype, self._stride = q, scale, dtype, stride
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    @staticmethod
+    def of(q, scale, dtype=torch.float32):
+        """Rows that were rounded elsewhere: ``q`` int8 [..., columns], ``scale`` float32 [...].  They are laid out anew, once."""
+        device = _device(q, "q")
+        _device(scale, "scale", device)
+        if q.dtype != torch.int8 or scale.dtype != _F32:
+            raise TypeError("q must be int8 and scale float32, not %s and %s" % (q.dtype, scale.dtype))
+        if not q.dim() or not q.shape[-1]:
+            raise ValueError("q has no columns")
+        if scale.shape != q.shape[:-1]:
+            raise ValueError("scale must hold one step per row of q")
+        if dtype not in _TYPES:
+            raise TypeError("dtype must be float32, float16 or bfloat16, not %s" % dtype)
+        cols = q.shape[-1]
+        wide = q.new_zeros(q.shape[:-1] + ((cols + 15) // 16 * 16,))
+        wide[..., :cols] = q
+        return Rows8(wide[..., :cols], scale.contiguous(), dtype, wide.shape[-1])
+
+    def restore(self, dtype=None):
+        """The matrix, in the type it had or another floating type."""
+        q = self.q
+        cols = q.shape[-1]
+        x = torch.empty(q.shape, dtype=dtype or self.dtype, device=q.device)
+        _launch(_rows8_restore, q.device, q.data_ptr(), self._stride, self.scale.data_ptr(), q.numel() // cols, cols, _type("dtype", x), x.data_ptr())
+        return x
+
+
+def _empty_rows8(x, rows, cols):
+    if not cols:
+        raise ValueError("x has no columns")
+    stride = (cols + 15) // 16 * 16
+    q = x.new_empty(x.shape[:-1] + (stride,), dtype=torch.int8)
+    return Rows8(q if stride == cols else q[..., :cols], x.new_empty(x.shape[:-1], dtype=_F32), x.dtype, stride)
+
+
+def rows8(x) -> Rows8:
+    """``x`` (any shape, rows run along its last dimension) in 8 bits, one step per row."""
+    device = _device(x, "x")
+    code = _type("x", x)
+    m, rows, cols, stride = _rows(x, "x")
+    c = _empty_rows8(x, rows, cols)
+    _launch(_rows8_save, device, m.data_ptr(), stride, rows, cols, code, c.q.data_ptr(), c._stride, c.scale.data_ptr())
+    return c
+
+
+def _no_gradient(call, *tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("%s has no gradient: call it under torch.no_grad(), or on detached tensors" % call)
+
+
+def rms_norm8(x, weight=None, residual=None, eps=1e-6):
+    """The output of ``rms_norm`` in 8 bits, for ``linear8``: ``(rows, sum)``; without a residual the sum is ``x``.  For serving:
+    without gradients."""
+    _no_gradient("rms_norm8", x, weight, residual)
+    _, c, total, _, _ = _rms(x, weight, residual, eps, True)
+    return c, x if residual is None else total
+
+
+def linear8(x, weight, dtype=None):
+    """Logits ``x weight^T`` of rows in 8 bits, ``[..., words]``.  ``x``: a ``Rows8``, or features, which are rounded by ``rows8`` first;
+    ``weight``: the ``Rows8`` of a projection [words, columns].  ``dtype``: of the logits, that of ``x`` if not given.  The sums are
+    exact integers.  For serving: without gradients."""
+    if not isinstance(weight, Rows8):
+        raise TypeError("weight must be Rows8 (rows8 of the projection), not %s" % type(weight).__name__)
+    if not isinstance(x, Rows8):
+        if isinstance(x, torch.Tensor):
+            _no_gradient("linear8", x)
+        x = rows8(x)
+    xq, wq = x.q, weight.q
+    device = wq.device
+    if xq.device != device:
+        raise ValueError("x is on %s, not on %s" % (xq.device, device))
+    cols = xq.shape[-1]
+    if wq.dim() != 2 or wq.shape[1] != cols:
+        raise ValueError("weight must be [words, %d] for features of that width" % cols)
+    words = wq.shape[0]
+    out = torch.empty(xq.shape[:-1] + (words,), dtype=dtype or x.dtype, device=device)
+    _launch(_linear8, device, xq.data_ptr(), x._stride, x.scale.data_ptr(), wq.data_ptr(), weight._stride, weight.scale.data_ptr(), xq.numel() // cols, words,
+            cols, _type("dtype", out), out.data_ptr())
+    return out
+
+
+# ---- words drawn from logits ---------------------------------------------------------------------------------------------
+
+def _limit(name, value, lead, device, types):
+    """(tensor with a value per row, or None; number for all rows) of a limit."""
+    if not isinstance(value, torch.Tensor):
+        return None, value
+    _device(value, name, device)
+    if value.dtype not in types:
+        raise TypeError("%s must be %s, not %s" % (name, " or ".join(str(t)[6:] for t in types), value.dtype))
+    if value.shape != lead:
+        raise ValueError("%s must be a number or hold one value per row of logits" % name)
+    return (value if value.is_contiguous() else value.contiguous()), 0
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Draws a word for every row of ``logits`` [..., words] by the row's random number ``u`` (float32, within [0, 1)): ``(word, p)``,
+    int64 and float32 in the shape of ``u``.  With z = (logits - their largest) / temperature, the words in falling order and equal ones
+    by their number, these are left: the first ``top_k`` (0: all), of them the fewest that hold ``top_p`` of their mass, of them those of
+    exp(z) >= ``min_p``.  The word is the first one, by number, at which the mass of the words left exceeds ``u`` of all of it; ``p`` is its
+    share of that mass.  Temperature 0 takes the first of the largest.  Every limit is a number, or a tensor with one value per row.
+    Words of logit -inf take no part; a row of which nothing is left gives -1 and 0, one with a NaN -1 and NaN."""
+    device = _device(logits, "logits")
+    code = _type("logits", logits)
+    m, rows, words, stride = _rows(logits, "logits")
+    if not words:
+        raise ValueError("logits has no words")
+    lead = logits.shape[:-1]
+    _device(u, "u", device)
+    if u.dtype != _F32:
+        raise TypeError("u must be float32, not %s" % u.dtype)
+    if u.shape != lead:
+        raise ValueError("u must hold one number per row of logits")
+    u = u if u.is_contiguous() else u.contiguous()
+    floats = (_F32,)
+    temperatures, temperature = _limit("temperature", temperature, lead, device, floats)
+    top_ks, top_k = _limit("top_k", top_k, lead, device, (torch.int32, torch.int64))
+    top_ps, top_p = _limit("top_p", top_p, lead, device, floats)
+    min_ps, min_p = _limit("min_p", min_p, lead, device, floats)
+    word, p = u.new_empty(lead, dtype=torch.int64), torch.empty_like(u)
+    _launch(_sample, device, m.data_ptr(), stride, rows, words, code, u.data_ptr(), _ptr(temperatures), temperature, _ptr(top_ks),
+            top_ks is not None and top_ks.dtype == torch.int64, top_k, _ptr(top_ps), top_p, _ptr(min_ps), min_p, word.data_ptr(), p.data_ptr())
+    return word, p

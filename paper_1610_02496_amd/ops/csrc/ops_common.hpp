@@ -116,21 +116,30 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
                max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
 }
 
-// One lane's chunk of a block of 128 columns, in 8 bits: step c = max|x| / 127 of the block, whole numbers round(x / c), ties to
-// even.  A block of zeros has step 0; a step ends where 127 of it are finite (kMostStep: the largest number of binary32, a mask's value
-// perhaps, is restored one unit lower, not as infinity).  A NaN or an infinity makes the step not finite: the block is restored as NaN.
-// All 16 lanes of the block call this together.
-__device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
-    uint32_t top = 0;
+// sum over the TPR threads of a row, the same value in all of them; `slot` alternates between calls so that one barrier is
+// enough
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *lds, int slot) {
+    v = wave_sum(v);
+    if constexpr (TPR == 64) return v;
+    else {
+        constexpr int W = TPR / 64;
+        if ((threadIdx.x & 63) == 0) lds[slot * W + (threadIdx.x >> 6)] = v;
+        __syncthreads();
+        float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = row_max(top);
-    constexpr float kMostStep = 0x1.020406p+121f;
-    float step = __uint_as_float(top) / 127.f;
-    step = top < 0x7f800000u ? fminf(step, kMostStep) : step;
-    // x / step is rounded twice, to binary32 and to a whole number.  The product with the inverse is off by 2^-22 * 127 at most, so it
-    // gives the same whole number unless it is as near as that to the middle of two: then, rarely, the division decides.
-    // Adding 1.5 * 2^23 rounds to a whole number, which the sum's low byte then holds in two's complement.
+        for (int i = 0; i < W; ++i) s += lds[slot * W + i];
+        return s;
+    }
+}
+
+// Whole numbers round(x / step) of a chunk, ties to even, within -127 .. 127; zeros where the step is zero or not finite.
+// The product with the inverse is off by 2^-22 * 127 at most, so it gives the whole number of the quotient unless that is as near as that to
+// the middle of two: then, rarely, a division decides.  EXACT: one of 64 bits, so that the number is that of the quotient itself; else the
+// quotient is rounded to binary32 before.  Adding 1.5 * 2^23 rounds to a whole number, which the sum's low byte then holds in two's
+// complement.
+template <bool EXACT>
+__device__ __forceinline__ void whole8(f32x8 x, float step, Bytes8 &q) {
     constexpr float kWhole = 12582912.f;
     const float inverse = __builtin_amdgcn_rcpf(step);
     uint32_t v[8];
@@ -144,11 +153,29 @@ __device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
     if (near) {
         const bool sound = step > 0.f && step < INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __float_as_uint((sound ? fminf(fmaxf(rintf(x[i] / step), -127.f), 127.f) : 0.f) + kWhole);
+        for (int i = 0; i < 8; ++i) {
+            const float n = EXACT ? (float)rint((double)x[i] / (double)step) : rintf(x[i] / step);
+            v[i] = __float_as_uint((sound ? fminf(fmaxf(n, -127.f), 127.f) : 0.f) + kWhole);
+        }
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
         q.v[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[4 * k + 3], v[4 * k + 2], 0x0c0c0400), __builtin_amdgcn_perm(v[4 * k + 1], v[4 * k], 0x0c0c0400), 0x05040100);
+}
+
+// One lane's chunk of a block of 128 columns, in 8 bits: step c = max|x| / 127 of the block, whole numbers round(x / c), ties to
+// even.  A block of zeros has step 0; a step ends where 127 of it are finite (kMostStep: the largest number of binary32, a mask's value
+// perhaps, is restored one unit lower, not as infinity).  A NaN or an infinity makes the step not finite: the block is restored as NaN.
+// All 16 lanes of the block call this together.
+__device__ __forceinline__ float quantise8(f32x8 x, Bytes8 &q) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = row_max(top);
+    constexpr float kMostStep = 0x1.020406p+121f;
+    float step = __uint_as_float(top) / 127.f;
+    step = top < 0x7f800000u ? fminf(step, kMostStep) : step;
+    whole8<false>(x, step, q);
     return step;
 }
 __device__ __forceinline__ void store_q(int8_t *p, int64_t n, const Bytes8 &q) {

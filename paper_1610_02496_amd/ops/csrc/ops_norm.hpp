@@ -28,23 +28,6 @@ struct NormBackward {
     float *partial; int parts;    // [parts][2][cols]: sums of dy h and of dy over a workgroup's rows; null: not wanted
 };
 
-// sum over the TPR threads of a row, the same value in all of them; `slot` alternates between calls so that one barrier is
-// enough
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float *lds, int slot) {
-    v = wave_sum(v);
-    if constexpr (TPR == 64) return v;
-    else {
-        constexpr int W = TPR / 64;
-        if ((threadIdx.x & 63) == 0) lds[slot * W + (threadIdx.x >> 6)] = v;
-        __syncthreads();
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) s += lds[slot * W + i];
-        return s;
-    }
-}
-
 // A row per wavefront (TPR = 64) or per workgroup (TPR = 256, 512); a lane holds NC chunks of eight columns of its row in registers, so
 // that x is read once.  A workgroup goes over several rows, keeps weight and bias in registers, and asks for a row before it works on the one
 // before.  Memory bounds it: 65,536 x 2048 in f16 (537 MB read and written) 98 us, 5.5 TB/s; 16,384 x 1024 in bf16 with the checkpoint

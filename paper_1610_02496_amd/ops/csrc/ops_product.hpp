@@ -66,10 +66,12 @@ __device__ __forceinline__ void each(F &&f) { each(std::make_integer_sequence<in
 // instruction wrote may be read two states later (FIRST: of a row of fragments; all of them come from LDS, which has a counter), and
 // the sums may be read seven states after their last product (settled()).  Waiting before every product would cost 2 to 4 % of a training
 // step, so that the compiler puts no vector instruction in between is checked in the built code (tests/test_ops_waits.py).
+struct Int8 {};   // the type of operands of 8-bit integers, in pairs: an element of 16 bits is two values of k, the sums' bits are int32
 template <class T, bool FIRST>
 __device__ __forceinline__ void mfma(u32x4 a, u32x4 b, f32x4 &c) {
     if constexpr (FIRST) asm volatile("s_nop 1");
-    if constexpr (std::is_same<T, bf16>::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    if constexpr (std::is_same<T, Int8>::value) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else if constexpr (std::is_same<T, bf16>::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 template <int M, int N>
@@ -79,6 +81,21 @@ __device__ __forceinline__ void settled(f32x4 (&c)[M][N]) {
 #pragma unroll
         for (int j = 0; j < N; j += 2) asm volatile("s_nop 7" : "+a"(c[i][j]), "+a"(c[i][j + 1]));
 }
+
+// Values of two neighbouring tiles of sums, i and i + 1, of which lane group g = lane / 16 holds rows 4 g .. + 3: afterwards a lane has
+// eight rows that follow each other, 8 (g / 2) .. + 7 of tile i + g % 2; `lo` and `hi` are their halves.
+template <int N>
+__device__ __forceinline__ void pair_rows(uint32_t (&lo)[N], uint32_t (&hi)[N]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const auto p = __builtin_amdgcn_permlane16_swap(lo[i], hi[i], false, false);
+        lo[i] = p[0];
+        hi[i] = p[1];
+    }
+#endif
+}
+__device__ __forceinline__ int paired_row(int lane) { return 16 * (lane >> 4 & 1) + 8 * (lane >> 5); }
 
 using LdsBytes = __attribute__((address_space(3))) char;
 

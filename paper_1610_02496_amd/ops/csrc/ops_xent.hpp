@@ -49,21 +49,6 @@ struct Exp {
     }
 };
 
-// Values of two neighbouring tiles of sums, i and i + 1, of which lane group g = lane / 16 holds rows 4 g .. + 3: afterwards a lane has
-// eight rows that follow each other, 8 (g / 2) .. + 7 of tile i + g % 2; `lo` and `hi` are their halves.
-template <int N>
-__device__ __forceinline__ void pair_rows(uint32_t (&lo)[N], uint32_t (&hi)[N]) {
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const auto p = __builtin_amdgcn_permlane16_swap(lo[i], hi[i], false, false);
-        lo[i] = p[0];
-        hi[i] = p[1];
-    }
-#endif
-}
-__device__ __forceinline__ int paired_row(int lane) { return 16 * (lane >> 4 & 1) + 8 * (lane >> 5); }
-
 // the largest, the sum of a value over the four lane groups that hold the same column: the same in all of them
 __device__ __forceinline__ float groups_max(float v) {
     v = fmaxf(v, __shfl_xor(v, 16));
