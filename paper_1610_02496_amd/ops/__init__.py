@@ -464,7 +464,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6):
 # ---- rows in 8 bits, and logits from them -------------------------------------------------------------------------------
 
 class Rows8:
-    """A matrix in 8 bits: ``q`` (int8; rows start at multiples of 16 bytes, with zeros in between) times ``scale`` (float32, one step
+    """A matrix in 8 bits: ``q`` (int8; rows start at multiples of 16 or 128 bytes) times ``scale`` (float32, one step
     per row, a 127th of its largest magnitude).  What ``rows8`` makes of features and weights and ``linear8`` multiplies."""
 
     __slots__ = ("q", "scale", "dtype", "_stride")
@@ -490,7 +490,7 @@ class Rows8:
         if dtype not in _TYPES:
             raise TypeError("dtype must be float32, float16 or bfloat16, not %s" % dtype)
         cols = q.shape[-1]
-        wide = q.new_zeros(q.shape[:-1] + ((cols + 15) // 16 * 16,))
+        wide = q.new_zeros(q.shape[:-1] + (_stride8(cols),))
         wide[..., :cols] = q
         return Rows8(wide[..., :cols], scale.contiguous(), dtype, wide.shape[-1])
 
@@ -503,10 +503,17 @@ class Rows8:
         return x
 
 
+def _stride8(cols):
+    """Bytes from row to row: multiples of 128, as the caches' lines, where that adds an eighth at most, else of 16 (8192 rows of 1000
+    and 141,000 words: 2.23 ms with rows of 1024 bytes, 2.50 ms with 1008, whose pieces of 128 lie on two lines each)."""
+    whole = (cols + 127) // 128 * 128
+    return whole if whole * 8 <= cols * 9 else (cols + 15) // 16 * 16
+
+
 def _empty_rows8(x, rows, cols):
     if not cols:
         raise ValueError("x has no columns")
-    stride = (cols + 15) // 16 * 16
+    stride = _stride8(cols)
     q = x.new_empty(x.shape[:-1] + (stride,), dtype=torch.int8)
     return Rows8(q if stride == cols else q[..., :cols], x.new_empty(x.shape[:-1], dtype=_F32), x.dtype, stride)
 

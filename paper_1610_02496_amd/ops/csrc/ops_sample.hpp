@@ -8,8 +8,8 @@
 // The borders are found without sorting, by histograms of counts and of masses.
 //
 // Masses are whole numbers, round(e^z 2^S) with S = 45 (less beyond 2^17 words, so that the sum of all stays below 2^62): their sums are
-// exact, so that neither their order nor atomics change a result, and e^z is computed to 2^-50, so that a border falls where 64-bit arithmetic
-// puts it.  A word of less than 2^-(S + 1) of the likeliest one's mass has none and is never drawn.
+// exact, so that neither their order nor atomics change a result, and e^z is computed in 64 bits to 1.1e-12, so that a border falls where 64-bit
+// arithmetic puts it but for some 1e-7 of the random numbers (V 1e-12; in 32 bits it would be one in a hundred).  A word of less than 2^-(S + 1) of the likeliest one's mass has none and is never drawn.
 #pragma once
 #include "ops_common.hpp"
 
@@ -29,23 +29,29 @@ struct Sample {
 };
 
 constexpr int kBins = 2048;         // of a histogram
-constexpr int kList = 2048;         // logits of a bin that are looked at in LDS
-constexpr int kTiles = 2048;        // of a row, at most
+constexpr int kList = 2048;         // logits that are looked at in LDS
 constexpr float kBinsPerUnit = 64.f;
 constexpr int kZeroBin = 2046;      // bins from here on hold no mass: z < -31.9, e^z 2^45 < 1/2
 
-// 2^r, |r| <= 1/2, to 3e-16: the interpolation at the Chebyshev nodes of degree 10
+// p r + c with c in scalar registers.  (The compiler keeps such constants in vector registers, two each, and has none left for them.)
+__device__ __forceinline__ double times_plus(double p, double r, double c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    double o;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(o) : "v"(p), "v"(r), "s"(c));
+    return o;
+#else
+    return fma(p, r, c);
+#endif
+}
+// 2^r, |r| <= 1/2, to 1.1e-12: the interpolation at the Chebyshev nodes of degree 8
 __device__ __forceinline__ double exp2_near(double r) {
-    double p = 0x1.e6063f7217bc6p-28;
-    p = fma(p, r, 0x1.b675bca4eeebbp-24);
-    p = fma(p, r, 0x1.62bfd47773353p-20);
-    p = fma(p, r, 0x1.ffcb54062e698p-17);
-    p = fma(p, r, 0x1.430913096fd9fp-13);
-    p = fma(p, r, 0x1.5d87fe9d7a584p-10);
-    p = fma(p, r, 0x1.3b2ab6fba1ddap-7);
-    p = fma(p, r, 0x1.c6b08d703ce49p-5);
-    p = fma(p, r, 0x1.ebfbdff82c598p-3);
-    p = fma(p, r, 0x1.62e42fefa3a19p-1);
+    double p = times_plus(0x1.63d136366db24p-20, r, 0x1.00dc4a532fb8ep-16);
+    p = times_plus(p, r, 0x1.4308ac85aa947p-13);
+    p = times_plus(p, r, 0x1.5d8745a728441p-10);
+    p = times_plus(p, r, 0x1.3b2ab7181b755p-7);
+    p = times_plus(p, r, 0x1.c6b08dd6fd234p-5);
+    p = times_plus(p, r, 0x1.ebfbdff823cedp-3);
+    p = times_plus(p, r, 0x1.62e42fef84cf0p-1);
     return fma(p, r, 1.0);
 }
 
@@ -68,10 +74,11 @@ struct Scale {
         const uint64_t bits = __double_as_longlong(e) + ((uint64_t)__double_as_longlong(n) << 52);
         return t > -64.0 ? __longlong_as_double((long long)bits) : 0.0;
     }
-    __device__ __forceinline__ uint64_t mass(float l) const {
-        const double v = fma(part(down(l)), up, 0x1p52);   // rounded to a whole number
+    __device__ __forceinline__ uint64_t mass_of(double d) const {
+        const double v = fma(part(d), up, 0x1p52);   // rounded to a whole number
         return (uint64_t)__double_as_longlong(v) & 0xfffffffffffffull;
     }
+    __device__ __forceinline__ uint64_t mass(float l) const { return mass_of(down(l)); }
 };
 
 __device__ __forceinline__ uint32_t key_of(float f) {   // the order of the floats; -0 and 0 are equal
@@ -79,6 +86,12 @@ __device__ __forceinline__ uint32_t key_of(float f) {   // the order of the floa
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+// a value that all lanes share, in scalar registers
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+__device__ __forceinline__ double uniform(double v) { return __longlong_as_double((long long)uniform((uint64_t)__double_as_longlong(v))); }
 
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp64(uint64_t v) { return (uint64_t)dpp<CTRL>((uint32_t)(v >> 32)) << 32 | dpp<CTRL>((uint32_t)v); }
@@ -108,93 +121,103 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
     return v;
 }
 
-template <int THREADS>
+struct Border { float value; uint64_t ties; };   // all logits above the value, and the first few of those equal to it
+
+template <int THREADS, int TILES>
 struct SampleLds {
-    uint64_t mass[kBins];            // of a bin; later of a tile
-    uint32_t count[kBins];           // the same; of a tile: logits equal to the border
+    uint64_t sums[kBins];            // of a bin's masses, or the number of its logits
+    uint64_t tile_mass[TILES];       // above the border
+    uint32_t tile_equal[TILES];      // logits equal to it
     float list[kList];
+    uint32_t at[kList];              // their words
     uint64_t waves[2][THREADS / 64];
-    uint64_t found[4];
+    uint64_t found[3];
     uint32_t listed, key_lo, key_hi;
 };
 
-// sum over the threads up to and including this one, and over all of them
-template <int THREADS>
-__device__ __forceinline__ uint64_t block_scan(SampleLds<THREADS> &s, int which, uint64_t v, uint64_t &total) {
-    const uint64_t own = wave_scan(v);
-    if ((threadIdx.x & 63) == 63) s.waves[which][threadIdx.x >> 6] = own;
-    __syncthreads();
-    uint64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        const uint64_t x = s.waves[which][w];
-        if (w < (int)(threadIdx.x >> 6)) before += x;
-        total += x;
-    }
-    __syncthreads();
-    return before + own;
-}
-
-// f(first word, eight logits, how many of them exist) for all of a row, a tile of 512 words per wavefront at a time; four are on their way.
-template <class T, int THREADS, class F>
-__device__ __forceinline__ void walk(const T *row, int64_t words, F &&f) {
+// f(first word, four logits) for all of a row, a tile of 512 words per wavefront at a time, AHEAD of them on their way; done(first word of
+// the lane in the tile) after a lane's eight.  Logits past the row's end are -inf.
+template <class T, int THREADS, int AHEAD, class F, class D>
+__device__ __forceinline__ void walk(const T *row, int64_t words, F &&f, D &&done) {
+    typedef float f32x4_ __attribute__((ext_vector_type(4)));
     const int lane = threadIdx.x & 63;
-    const int64_t step = THREADS / 64 * 512;
-    for (int64_t c0 = (int64_t)(threadIdx.x >> 6) * 512; c0 < words; c0 += 4 * step) {
-        Raw8<T> raw[4];
+    constexpr int64_t step = THREADS / 64 * 512;
+    for (int64_t c0 = (int64_t)uniform(threadIdx.x >> 6) * 512; c0 < words; c0 += AHEAD * step) {
+        Raw8<T> raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < AHEAD; ++k) {
             const int64_t c = c0 + k * step + lane * 8;
             raw[k] = load_raw8(row + c, words - c);
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < AHEAD; ++k)
             if (c0 + k * step < words) {
                 const int64_t c = c0 + k * step + lane * 8, left = words - c;
-                f(c, widen(raw[k]), left < 8 ? (int)left : 8);
+                f32x8 v = widen(raw[k]);
+                if (left < 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : -INFINITY;
+                }
+                const f32x4_ lo = v.lo, hi = v.hi;
+                f(c, lo);
+                __builtin_amdgcn_sched_barrier(0);
+                f(c + 4, hi);
+                __builtin_amdgcn_sched_barrier(0);
+                done(c);
             }
     }
 }
+template <class T, int THREADS, int AHEAD, class F>
+__device__ __forceinline__ void walk(const T *row, int64_t words, F &&f) { walk<T, THREADS, AHEAD>(row, words, f, [](int64_t) {}); }
 
-// The border of the fewest logits in falling order that hold `goal` (a count, or a mass): its value, and how many of those equal to it take
-// part.  Only logits above `above` count, and `ties` of those equal to it.  Fewer than goal in all bins that have mass: -inf.
-struct Border { float value; uint64_t ties; };
+// A row of logits and a workgroup's work on it.
+template <class T, int THREADS, int TILES>
+struct Row {
+    SampleLds<THREADS, TILES> &s;
+    const T *row;
+    int64_t words;
+    int tile_log;
+    Scale sc;
+    bool all_listed;                 // the list holds every logit that can be left
+    int tid = threadIdx.x;
 
-template <class T, int THREADS, bool MASS>
-__device__ __forceinline__ Border find_border(SampleLds<THREADS> &s, const T *row, int64_t words, const Scale &sc, Border above, double share, uint64_t goal) {
-    const int tid = threadIdx.x;
-    constexpr int EACH = kBins / THREADS;
-    auto clear = [&] {
-        for (int i = tid; i < kBins; i += THREADS) {
-            s.mass[i] = 0;
-            s.count[i] = 0;
+    __device__ __forceinline__ void clear() {
+        __syncthreads();
+        for (int i = tid; i < kBins; i += THREADS) s.sums[i] = 0;
+        __syncthreads();
+    }
+    // sum over the threads up to and including this one, and over all of them
+    __device__ __forceinline__ uint64_t scan(int which, uint64_t v, uint64_t &total) {
+        const uint64_t own = wave_scan(v);
+        if ((tid & 63) == 63) s.waves[which][tid >> 6] = own;
+        __syncthreads();
+        uint64_t before = 0;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            const uint64_t x = s.waves[which][w];
+            if (w < (tid >> 6)) before += x;
+            total += x;
         }
-    };
-    auto add = [&](int bin, float l) {
-        if constexpr (MASS) {
-            const uint64_t m = sc.mass(l);
-            if (m) atomicAdd((unsigned long long *)&s.mass[bin], (unsigned long long)m);
-        } else
-            atomicAdd(&s.count[bin], 1u);
-    };
-    auto add_ties = [&](int bin) {   // by one thread
-        if constexpr (MASS)
-            if (above.value > -INFINITY) atomicAdd((unsigned long long *)&s.mass[bin], (unsigned long long)(above.ties * sc.mass(above.value)));
-    };
-    // the bin in which the sum from the first bin on reaches the goal, and the sum before it; kBins if there is none
-    auto reach = [&](uint64_t before, bool first) {
+        total = uniform(total);
+        __syncthreads();
+        return before + own;
+    }
+    // The bin at which the sum of the bins from the first one on, and `before`, reaches the goal (kBins if there is none); `before` is then the
+    // sum before it.  Where a share is asked for, the goal is that of the whole.
+    __device__ __forceinline__ int reach(uint64_t &before, bool of_whole, double share, uint64_t &goal) {
+        constexpr int EACH = kBins / THREADS;
+        __syncthreads();
         uint64_t v[EACH], sum = 0, total;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) sum += v[i] = MASS ? s.mass[tid * EACH + i] : s.count[tid * EACH + i];
+        for (int i = 0; i < EACH; ++i) sum += v[i] = s.sums[tid * EACH + i];
         if (tid == 0) s.found[0] = kBins;
-        const uint64_t upto = block_scan(s, 0, sum, total);
-        if (MASS && first) {
+        const uint64_t upto = scan(0, sum, total);
+        if (of_whole) {
             const double want = share * (double)total;
             goal = (uint64_t)want;
             goal += (double)goal < want;
-            if (goal < 1) goal = 1;
-            if (goal > total) goal = total;
+            goal = uniform(goal < 1 ? 1 : goal > total ? total : goal);
         }
         uint64_t at = before + upto - sum;
         if (at < goal && at + sum >= goal) {
@@ -203,116 +226,216 @@ __device__ __forceinline__ Border find_border(SampleLds<THREADS> &s, const T *ro
                 if (at < goal && at + v[i] >= goal) {
                     s.found[0] = (uint64_t)(tid * EACH + i);
                     s.found[1] = at;
-                    s.found[2] = v[i];
                 }
                 at += v[i];
             }
         }
         __syncthreads();
-    };
-
-    __syncthreads();
-    clear();
-    __syncthreads();
-    walk<T, THREADS>(row, words, [&](int64_t, f32x8 v, int n) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int b = sc.bin(v[i]);
-            if (i < n && b < kZeroBin && v[i] > above.value) add(b, v[i]);
+        before = uniform(s.found[1]);
+        return (int)uniform((uint32_t)s.found[0]);
+    }
+    // what a logit adds to its bin
+    __device__ __forceinline__ void add(bool mass, int bin, float l) {
+        atomicAdd((unsigned long long *)&s.sums[bin], mass ? (unsigned long long)sc.mass(l) : 1ull);
+    }
+    // the mass of the logits equal to the border above that count; by one thread
+    __device__ __forceinline__ void add_ties(int bin, Border above) {
+        atomicAdd((unsigned long long *)&s.sums[bin], (unsigned long long)(above.ties * sc.mass(above.value)));
+    }
+    __device__ __forceinline__ void put(float l, int64_t word) {
+        const uint32_t n = atomicAdd(&s.listed, 1u);
+        if (n < kList) {
+            s.list[n] = l;
+            s.at[n] = (uint32_t)word;
         }
-    });
-    if (tid == 0 && above.value > -INFINITY && sc.bin(above.value) < kZeroBin) add_ties(sc.bin(above.value));
-    __syncthreads();
-    reach(0, true);
-    if (s.found[0] >= kBins) return above;
-    const int bin = (int)s.found[0];
-    uint64_t before = s.found[1];
+    }
+    __device__ __forceinline__ int tile_of(int64_t word) const { return (int)(word >> (9 + tile_log)); }
 
-    // the logits of that bin (those at the border above stay out): a list of them, if they are few, and their range
-    if (tid == 0) { s.listed = 0; s.key_lo = 0xffffffffu; s.key_hi = 0; }
-    __syncthreads();
-    uint32_t lo = 0xffffffffu, hi = 0;
-    walk<T, THREADS>(row, words, [&](int64_t, f32x8 v, int n) {
+    // Lists all logits of the bins up to `last`; false if they are too many.
+    __device__ __forceinline__ bool list_upto(int last) {
+        if (tid == 0) s.listed = 0;
+        __syncthreads();
+        walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
+            bool hit[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n && v[i] > above.value && sc.bin(v[i]) == bin) {
-                const uint32_t at = atomicAdd(&s.listed, 1u);
-                if (at < kList) s.list[at] = v[i];
-                const uint32_t k = key_of(v[i]);
-                lo = min(lo, k);
-                hi = max(hi, k);
+            for (int i = 0; i < 4; ++i) hit[i] = v[i] > -INFINITY && sc.bin(v[i]) <= last;
+            if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (hit[i]) put(v[i], c + i);
             }
-    });
-    const bool tied = MASS && above.value > -INFINITY && sc.bin(above.value) == bin;
-    if (tied) lo = key_of(above.value);
-    if (lo <= hi || tied) { atomicMin(&s.key_lo, lo); atomicMax(&s.key_hi, max(lo, hi)); }
-    __syncthreads();
-    lo = s.key_lo; hi = s.key_hi;
-    const uint32_t listed = s.listed;
-    // a histogram of the keys lo .. hi, the largest first, in ever smaller ranges
-    while (lo < hi) {
-        const int shift = 32 - __builtin_clz((hi - lo) >> 10 | 1u) - 1;   // ((hi - lo) >> shift) < 2048
+        });
         __syncthreads();
+        return uniform(s.listed) <= (uint32_t)kList;
+    }
+
+    // First half of a border's search: the bin in which the logits in falling order reach the goal, or kZeroBin if they do not.  Only logits
+    // above `above` count, and above.ties of those equal to it.
+    __device__ __forceinline__ int find_bin(bool mass, Border above, double share, uint64_t &goal, uint64_t &before) {
         clear();
-        __syncthreads();
         auto take = [&](float l) {
-            const uint32_t k = key_of(l);
-            if (k >= lo && k <= hi) add((int)((hi - k) >> shift), l);
+            const int b = sc.bin(l);
+            if (b < kZeroBin && l > above.value) add(mass, b, l);
         };
-        if (listed <= kList) {
-            for (uint32_t i = tid; i < listed; i += THREADS) take(s.list[i]);
-        } else {
-            walk<T, THREADS>(row, words, [&](int64_t, f32x8 v, int n) {
+        if (all_listed) {
+            for (uint32_t i = tid; i < s.listed; i += THREADS) take(s.list[i]);
+        } else
+            walk<T, THREADS, 4>(row, words, [&](int64_t, auto v) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n && v[i] > above.value && sc.bin(v[i]) == bin) take(v[i]);
+                for (int i = 0; i < 4; ++i) take(v[i]);
+            });
+        if (mass && tid == 0 && above.value > -INFINITY && sc.bin(above.value) < kZeroBin) add_ties(sc.bin(above.value), above);
+        before = 0;
+        const int bin = reach(before, mass, share, goal);
+        return bin < kZeroBin ? bin : kZeroBin;
+    }
+
+    // Masses of the tiles (if `sums`) of the bins before `bin`, of logits that min_p leaves; and a list of that bin's logits, unless all are
+    // listed.
+    __device__ __forceinline__ void sum_and_list(bool sums, int bin) {
+        __syncthreads();
+        for (int i = tid; i < TILES; i += THREADS) {
+            s.tile_mass[i] = 0;
+            s.tile_equal[i] = 0;
+        }
+        if (tid == 0 && !all_listed) s.listed = 0;
+        __syncthreads();
+        if (all_listed) {
+            if (sums)
+                for (uint32_t i = tid; i < s.listed; i += THREADS) {
+                    const float l = s.list[i];
+                    if (sc.bin(l) < bin && sc.down(l) >= sc.least) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(s.at[i])], (unsigned long long)sc.mass(l));
+                }
+        } else {
+            uint64_t sum = 0;
+            walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
+                bool hit[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int b = sc.bin(v[i]);
+                    hit[i] = b == bin && b < kZeroBin;
+                    if (sums) {
+                        const double d = sc.down(v[i]);
+                        const uint64_t m = sc.mass_of(d);
+                        sum += b < bin && d >= sc.least ? m : 0;
+                    }
+                }
+                if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (hit[i]) put(v[i], c + i);
+                }
+            }, [&](int64_t c) {
+                if (sums) {
+                    sum = wave_total(sum);
+                    if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(c)], (unsigned long long)sum);
+                    sum = 0;
+                }
             });
         }
-        if (tid == 0 && tied && key_of(above.value) >= lo && key_of(above.value) <= hi) add_ties((int)((hi - key_of(above.value)) >> shift));
         __syncthreads();
-        reach(before, false);
-        if (s.found[0] >= kBins) break;   // (cannot be: the range holds what is missing)
-        const uint32_t part = (uint32_t)s.found[0], top = hi - (part << shift), width = (1u << shift) - 1;
-        before = s.found[1];
-        lo = top - lo > width ? top - width : lo;
-        hi = top;
     }
-    __syncthreads();
-    const float value = of_key(hi);
-    uint64_t ties = goal - before;
-    if constexpr (MASS) {
-        const uint64_t m = sc.mass(value);
-        ties = m ? (ties + m - 1) / m : 1;
-    }
-    if (value == above.value && ties > above.ties) ties = above.ties;
-    return Border{value, ties};
-}
 
-// A row per workgroup, read once for its largest logit, again for every histogram, and for the sums of its tiles; the word is found in its
-// tile.
-template <class T, int THREADS>
-__global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
-    __shared__ SampleLds<THREADS> s;
+    // f(logit, word) for the logits of a bin: of the list, or if they did not fit, of the row.
+    template <class F>
+    __device__ __forceinline__ void of_bin(int bin, F &&f) {
+        if (s.listed <= (uint32_t)kList) {
+            for (uint32_t i = tid; i < s.listed; i += THREADS)
+                if (sc.bin(s.list[i]) == bin) f(s.list[i], (int64_t)s.at[i]);
+        } else
+            walk<T, THREADS, 1>(row, words, [&](int64_t c, auto v) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (sc.bin(v[i]) == bin) f(v[i], c + i);
+            });
+    }
+
+    // Second half: within the bin, by histograms of the keys lo .. hi, the largest first, in ever smaller ranges.
+    __device__ __forceinline__ Border border_in(bool mass, int bin, Border above, uint64_t goal, uint64_t before) {
+        if (tid == 0) { s.key_lo = 0xffffffffu; s.key_hi = 0; }
+        __syncthreads();
+        uint32_t lo = 0xffffffffu, hi = 0;
+        of_bin(bin, [&](float l, int64_t) {
+            if (l > above.value) {
+                lo = min(lo, key_of(l));
+                hi = max(hi, key_of(l));
+            }
+        });
+        const uint32_t above_key = key_of(above.value);
+        const bool tied = mass && above.value > -INFINITY && sc.bin(above.value) == bin;
+        if (tied) {
+            lo = min(lo, above_key);
+            hi = max(hi, above_key);
+        }
+        if (lo <= hi) {
+            atomicMin(&s.key_lo, lo);
+            atomicMax(&s.key_hi, hi);
+        }
+        __syncthreads();
+        lo = uniform(s.key_lo);
+        hi = uniform(s.key_hi);
+#pragma unroll 1
+        while (lo < hi) {
+            const int shift = 31 - __builtin_clz((hi - lo) >> 10 | 1u);   // ((hi - lo) >> shift) < 2048
+            clear();
+            of_bin(bin, [&](float l, int64_t) {
+                const uint32_t k = key_of(l);
+                if (l > above.value && k >= lo && k <= hi) add(mass, (int)((hi - k) >> shift), l);
+            });
+            if (tied && tid == 0 && above_key >= lo && above_key <= hi) add_ties((int)((hi - above_key) >> shift), above);
+            const int part = reach(before, false, 0.0, goal);
+            if (part >= kBins) break;   // (cannot be: the range holds what is missing)
+            const uint32_t top = hi - ((uint32_t)part << shift), width = (1u << shift) - 1;
+            lo = top - lo > width ? top - width : lo;
+            hi = top;
+        }
+        const float value = of_key(hi);
+        uint64_t ties = goal - before;
+        if (mass) {
+            const uint64_t m = uniform(sc.mass(value));
+            ties = m ? (ties + m - 1) / m : 1;
+        }
+        if (value == above.value && ties > above.ties) ties = above.ties;
+        return Border{value, ties};
+    }
+
+    // what of the border's bin is above it, and how many are equal
+    __device__ __forceinline__ void add_bin(int bin, Border border) {
+        of_bin(bin, [&](float l, int64_t word) {
+            if (l > border.value) {
+                if (sc.down(l) >= sc.least) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(word)], (unsigned long long)sc.mass(l));
+            } else if (l == border.value)
+                atomicAdd(&s.tile_equal[tile_of(word)], 1u);
+        });
+        __syncthreads();
+    }
+};
+
+// A row per workgroup.  It is read once for its largest logit; then, if top_k is small, once to list the few logits that can be left, among them
+// the top_k largest of the threads' own maxima; else once for every limit's histogram, and once for the masses of its tiles of 512 words and
+// a list of the bin with the border.  The word is found in its tile.
+template <class T, int THREADS, int TILES>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 2) void sample_kernel(Sample a) {
+    __shared__ SampleLds<THREADS, TILES> s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *logits = static_cast<const T *>(a.logits) + row * a.stride;
         const int64_t V = a.words;
-        const float temperature = a.temperatures ? a.temperatures[row] : a.temperature;
-        const int64_t top_k = a.top_ks ? (a.top_k64 ? static_cast<const int64_t *>(a.top_ks)[row] : (int64_t)static_cast<const int32_t *>(a.top_ks)[row]) : a.top_k;
-        const float top_p = a.top_ps ? a.top_ps[row] : a.top_p, min_p = a.min_ps ? a.min_ps[row] : a.min_p;
+        const float temperature = uniform(a.temperatures ? a.temperatures[row] : a.temperature);
+        const int64_t top_k = (int64_t)uniform((uint64_t)(a.top_ks ? (a.top_k64 ? static_cast<const int64_t *>(a.top_ks)[row] : (int64_t)static_cast<const int32_t *>(a.top_ks)[row]) : a.top_k));
+        const float top_p = uniform(a.top_ps ? a.top_ps[row] : a.top_p), min_p = uniform(a.min_ps ? a.min_ps[row] : a.min_p);
         const float u = a.u[row];
 
-        float top = -INFINITY;
+        float own = -INFINITY;
         bool odd = false;
-        walk<T, THREADS>(logits, V, [&](int64_t, f32x8 v, int n) {
+        walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float l = i < n ? v[i] : -INFINITY;
-                top = fmaxf(top, l);
-                odd |= l != l;
+            for (int i = 0; i < 4; ++i) {
+                own = fmaxf(own, v[i]);
+                odd |= v[i] != v[i];
             }
         });
-        top = wave_largest(top);
+        float top = wave_largest(own);
         odd = __builtin_amdgcn_ballot_w64(odd) != 0;
         __syncthreads();             // (the row before is done)
         if (lane == 0) s.waves[0][wave] = (uint64_t)odd << 32 | __float_as_uint(top);
@@ -323,6 +446,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
             odd |= (s.waves[0][w] >> 32) != 0;
             top = fmaxf(top, __uint_as_float((uint32_t)s.waves[0][w]));
         }
+        top = uniform(top);
         __syncthreads();
         if (odd || top == -INFINITY) {   // a NaN among the logits, or nothing to draw from
             if (tid == 0) {
@@ -333,10 +457,10 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
         }
         if (!(temperature > 0.f)) {      // the first of the largest
             uint32_t at = 0xffffffffu;
-            walk<T, THREADS>(logits, V, [&](int64_t c, f32x8 v, int n) {
+            walk<T, THREADS, 4>(logits, V, [&](int64_t c, auto v) {
 #pragma unroll
-                for (int i = 7; i >= 0; --i)
-                    if (i < n && v[i] == top) at = min(at, (uint32_t)(c + i));
+                for (int i = 0; i < 4; ++i)
+                    if (v[i] == top) at = min(at, (uint32_t)(c + i));
             });
             if (tid == 0) s.listed = 0xffffffffu;
             __syncthreads();
@@ -350,49 +474,44 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
         }
         Scale sc;
         sc.top = top;
-        sc.per = kBinsPerUnit / temperature;
-        sc.log2_per = 1.44269504088896340736 / (double)temperature;
-        sc.least = min_p > 0.f ? (min_p < 1.f ? log((double)min_p) * (double)temperature : 0.0) : -INFINITY;
+        sc.per = uniform(kBinsPerUnit / temperature);
+        sc.log2_per = uniform(1.44269504088896340736 / (double)temperature);
+        sc.least = uniform(min_p > 0.f ? (min_p < 1.f ? log((double)min_p) * (double)temperature : 0.0) : -INFINITY);
         sc.up = (double)((uint64_t)1 << a.mass_log);
+        Row<T, THREADS, TILES> r{s, logits, V, a.tile_log, sc, false};
 
+        const bool has_k = top_k > 0 && top_k < V, has_p = top_p < 1.f;
         Border border{-INFINITY, 0};
-        if (top_k > 0 && top_k < V) border = find_border<T, THREADS, false>(s, logits, V, sc, border, 0.0, (uint64_t)top_k);
-        if (top_p < 1.f) border = find_border<T, THREADS, true>(s, logits, V, sc, border, top_p > 0.f ? (double)top_p : 0.0, 0);
-
-        // masses of the tiles above the border, and how many logits are equal to it
-        __syncthreads();
-        for (int i = tid; i < kTiles; i += THREADS) {
-            s.mass[i] = 0;
-            s.count[i] = 0;
+        uint64_t goal = (uint64_t)top_k, before = 0;
+        if (has_k && top_k <= THREADS / 2) {
+            // the k-th largest logit is not below the k-th largest of the threads' maxima
+            r.clear();
+            if (own > -INFINITY && sc.bin(own) < kZeroBin) r.add(false, sc.bin(own), own);
+            const int last = r.reach(before, false, 0.0, goal);
+            if (last < kZeroBin) r.all_listed = r.list_upto(last);
         }
-        __syncthreads();
-        auto above = [&](float l) { return l > border.value && sc.down(l) >= sc.least; };
-        walk<T, THREADS>(logits, V, [&](int64_t c, f32x8 v, int n) {
-            uint64_t sum = 0;
-            uint32_t equal = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i < n && above(v[i])) sum += sc.mass(v[i]);
-                equal += i < n && v[i] == border.value;
+#pragma unroll 1
+        for (int limit = 0; limit < 3; ++limit) {       // top_k, top_p, and where there is neither the sums alone
+            if (limit == 0 ? !has_k : limit == 1 ? !has_p : has_k || has_p) continue;
+            const bool mass = limit == 1, sums = limit > 0 || !has_p;
+            const int bin = limit == 2 ? kZeroBin : r.find_bin(mass, border, top_p > 0.f ? (double)top_p : 0.0, goal, before);
+            r.sum_and_list(sums, bin);
+            if (bin < kZeroBin) {
+                border = r.border_in(mass, bin, border, goal, before);
+                if (sums) r.add_bin(bin, border);
             }
-            sum = wave_total(sum);
-            if (__builtin_amdgcn_ballot_w64(equal != 0)) equal = (uint32_t)wave_total(equal);
-            if (lane == 0) {
-                const int tile = (int)(c >> (9 + a.tile_log));
-                if (sum) atomicAdd((unsigned long long *)&s.mass[tile], (unsigned long long)sum);
-                if (equal) atomicAdd(&s.count[tile], equal);
-            }
-        });
-        __syncthreads();
-        constexpr int EACH = kTiles / THREADS;
+        }
+
+        constexpr int EACH = (TILES + THREADS - 1) / THREADS;
         const uint64_t tie = border.value > -INFINITY && sc.down(border.value) >= sc.least ? sc.mass(border.value) : 0;
         uint64_t masses[EACH], equals[EACH], sum = 0, equal = 0, total;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            masses[i] = s.mass[tid * EACH + i];
-            equal += equals[i] = border.value > -INFINITY ? s.count[tid * EACH + i] : 0;
+            const bool is = tid * EACH + i < TILES;
+            masses[i] = is ? s.tile_mass[tid * EACH + i] : 0;
+            equal += equals[i] = is ? s.tile_equal[tid * EACH + i] : 0;
         }
-        uint64_t equal_before = block_scan(s, 0, equal, total) - equal;
+        uint64_t equal_before = r.scan(0, equal, total) - equal;
         const uint64_t first_equal = equal_before;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
@@ -401,9 +520,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
             equal_before += equals[i];
             sum += masses[i];
         }
-        uint64_t at = block_scan(s, 1, sum, total) - sum;
-        const float v01 = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-        const uint64_t target = (uint64_t)((double)v01 * (double)total);
+        uint64_t at = r.scan(1, sum, total) - sum;
+        const float within = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+        const uint64_t target = (uint64_t)((double)within * (double)total);
         equal_before = first_equal;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
@@ -418,7 +537,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
         __syncthreads();
         if (wave == 0) {                 // the word, in its tile
             int64_t c = (int64_t)s.found[0] << (9 + a.tile_log);
-            uint64_t before = s.found[1], seen = s.found[2];
+            uint64_t sum_before = s.found[1], seen = s.found[2];
             const int64_t end = c + ((int64_t)512 << a.tile_log) < V ? c + ((int64_t)512 << a.tile_log) : V;
             for (; c < end; c += 512) {
                 const int64_t first = c + lane * 8;
@@ -428,19 +547,20 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) mine += i < n && tie && v[i] == border.value;
                 const uint64_t to_here = wave_scan(mine);
-                uint64_t rank = seen + to_here - mine, m[8], own = 0;
+                uint64_t rank = seen + to_here - mine, m[8], own_sum = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     m[i] = 0;
                     if (i < n) {
-                        if (above(v[i])) m[i] = sc.mass(v[i]);
+                        if (v[i] > border.value && sc.down(v[i]) >= sc.least) m[i] = sc.mass(v[i]);
                         else if (tie && v[i] == border.value) m[i] = rank++ < border.ties ? tie : 0;
                     }
-                    own += m[i];
+                    own_sum += m[i];
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                const uint64_t upto = wave_scan(own);
-                uint64_t sum_at = before + upto - own;
-                if (sum_at <= target && sum_at + own > target) {
+                const uint64_t upto = wave_scan(own_sum);
+                uint64_t sum_at = sum_before + upto - own_sum;
+                if (sum_at <= target && sum_at + own_sum > target) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         if (sum_at <= target && sum_at + m[i] > target) {
@@ -450,7 +570,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(Sample a) {
                         sum_at += m[i];
                     }
                 }
-                before += lane64(upto, 63);
+                sum_before += lane64(upto, 63);
                 seen += lane64(to_here, 63);
             }
         }

@@ -217,7 +217,9 @@ namespace {
 
 constexpr int64_t kMaxCols8 = ((int64_t)1 << 17) - 1;   // products of a sum in int32: each up to 2^14
 
-// The tile of a product of `steps` steps of 128 columns: the rule of the 16-bit products, whose steps take as long.
+// The tile of a product of `steps` steps of 128 columns: the rule of the 16-bit products, whose steps and ends take about as long.  Measured in
+// us with 256, 128 and 64 in turn (bf16): 8192 x 1000 x 141,000: 1597, 1694, 2579; 4096 x 1000 x 100,000: 570, 590, 938; 4096 x 777 x 30,011: 179, 165,
+// 221; 300 x 777 x 30,011: 26.2, 20.9, 24.4; 61 x 777 x 30,011: 21.2, 9.6, 9.4; 1 x 1024 x 100,000: 41.7, 25.2, 20.9.
 int tile8_of(int64_t m, int64_t n, int64_t steps) {
     auto tiles = [&](int64_t t) { return parts_of(m, t) * parts_of(n, t); };
     const int64_t large = tiles(256), middle = tiles(128), small = tiles(64);
@@ -255,7 +257,7 @@ extern "C" int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_s
     return with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
         using E = Linear8Epilogue<T>;
-        const E ep{static_cast<T *>(out), rows, words, x_scale, w_scale};
+        const E ep{static_cast<T *>(out), rows, words, x_scale, w_scale, words % 8 == 0 && aligned(out, 16)};
         if (tile == 256) product_kernel<Int8, false, false, 256, 256, 2, 2, E, None><<<(unsigned)grid, 256, 0, st>>>(p, ep, None{});
         else if (tile == 128) product_kernel<Int8, false, false, 128, 128, 2, 2, E, None><<<(unsigned)grid, 256, 0, st>>>(p, ep, None{});
         else product_kernel<Int8, false, false, 64, 64, 2, 2, E, None><<<(unsigned)grid, 256, 0, st>>>(p, ep, None{});
@@ -265,6 +267,10 @@ extern "C" int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_s
 }
 
 // ---- words drawn from logits -------------------------------------------------------------------------------------------------
+
+namespace {
+constexpr int kFewTiles = 16, kManyTiles = 2048;   // of 512 words or more
+}
 
 extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, int64_t words, int dtype, const float *u, const float *temperatures,
                             float temperature, const void *top_ks, int top_k64, int64_t top_k, const float *top_ps, float top_p, const float *min_ps,
@@ -290,13 +296,13 @@ extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, in
     int bits = 0;
     while (((int64_t)1 << bits) < words) ++bits;
     Sample a{logits, stride, rows, words, u, temperatures, temperature, top_ks, top_k64, top_k, top_ps, top_p, min_ps, min_p, word, p, 0, bits < 17 ? 45 : 62 - bits};
-    while (parts_of(words, (int64_t)512 << a.tile_log) > kTiles) ++a.tile_log;
+    while (parts_of(words, (int64_t)512 << a.tile_log) > kManyTiles) ++a.tile_log;
     const unsigned grid = (unsigned)(rows < 16 * kCus ? rows : 16 * kCus);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
-        if (words <= 8192) sample_kernel<T, 256><<<grid, 256, 0, st>>>(a);
-        else sample_kernel<T, 1024><<<grid, 1024, 0, st>>>(a);
+        if (words <= 512 * kFewTiles) sample_kernel<T, 256, kFewTiles><<<grid, 256, 0, st>>>(a);
+        else sample_kernel<T, 512, kManyTiles><<<grid, 512, 0, st>>>(a);
         OPS_HIP(hipGetLastError());
         return SABER_OK;
     });
