@@ -174,7 +174,8 @@ int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_scale, const
  *   those of exp z >= min_p; always the first one
  * and the first word, by number, is taken at which the sum of exp z of the words left exceeds u times that of all of them.
  * The masses are sums of whole multiples of 2^-45 (of 2^(ceil(log2 words) - 62) beyond 2^17 words) of the likeliest
- * word's: what is below half of that has none.  The limits are compared in 64 bits.
+ * word's: what is below half of that has none.  The limits are compared in 64 bits; a share of the whole counts as held from
+ * 2^-40 of the whole below it.
  *   logits [rows][words] of dtype; -inf leaves a word out, infinite ones share all of the mass
  *   temperatures, top_ks (int32, or int64 if top_k64), top_ps, min_ps [rows]: a value per row, or NULL: then temperature,
  *                 top_k, top_p, min_p hold for all rows (and are checked).  A temperature of 0 (or less, or NaN) takes the

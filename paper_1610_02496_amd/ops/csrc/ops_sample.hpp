@@ -10,6 +10,9 @@
 // Masses are whole numbers, round(e^z 2^S) with S = 45 (less beyond 2^17 words, so that the sum of all stays below 2^62): their sums are
 // exact, so that neither their order nor atomics change a result, and e^z is computed in 64 bits to 1.1e-12, so that a border falls where 64-bit
 // arithmetic puts it but for some 1e-7 of the random numbers (V 1e-12; in 32 bits it would be one in a hundred).  A word of less than 2^-(S + 1) of the likeliest one's mass has none and is never drawn.
+// The histogram of all words adds up e^z relative to the middle of a bin, in whole multiples of 2^-40, which takes half the arithmetic and no
+// largest logit; one factor per bin makes masses of its sums.  They differ from the sums of the masses by less than 1e-12, so a share counts
+// as held from 2^-40 of the whole below it.
 #pragma once
 #include "ops_common.hpp"
 
@@ -17,7 +20,7 @@ namespace saber_ops {
 
 struct Sample {
     const void *logits; int64_t stride;
-    int64_t rows, words;
+    int64_t first_row, words;   // of the launch, a workgroup per row
     const float *u;
     // a value per row, or null: the same for all rows
     const float *temperatures; float temperature;
@@ -29,9 +32,12 @@ struct Sample {
 };
 
 constexpr int kBins = 2048;         // of a histogram
-constexpr int kList = 2048;         // logits that are looked at in LDS
-constexpr float kBinsPerUnit = 64.f;
+template <int THREADS> constexpr int kList = THREADS == 256 ? 2048 : 4096;   // logits that are looked at in LDS
+constexpr int kMaxima = 4;          // that a thread keeps
+constexpr float kBinsPerUnit = 32.f;
 constexpr int kZeroBin = 2046;      // bins from here on hold no mass: z < -31.9, e^z 2^45 < 1/2
+constexpr float kRoom = 31.f;       // z of the first bin above the first logits' largest, where that of all is not known yet
+constexpr double kBinLog2 = 1.44269504088896340736 / 32;   // log2 of e^z over a bin
 
 // p r + c with c in scalar registers.  (The compiler keeps such constants in vector registers, two each, and has none left for them.)
 __device__ __forceinline__ double times_plus(double p, double r, double c) {
@@ -55,25 +61,48 @@ __device__ __forceinline__ double exp2_near(double r) {
     return fma(p, r, 1.0);
 }
 
+// 2^r, |r| <= kBinLog2 / 2 and a hundredth more, to 5.2e-13: the same of degree 4
+__device__ __forceinline__ double exp2_in_bin(double r) {
+    double p = times_plus(0x1.3b2b8f7b7e9dfp-7, r, 0x1.c6b25d473c852p-5);
+    p = times_plus(p, r, 0x1.ebfbdff7b8a25p-3);
+    p = times_plus(p, r, 0x1.62e42feead6b2p-1);
+    return fma(p, r, 1.0);
+}
+
 // The logits of a row relative to its largest.
 struct Scale {
     float top, per;      // largest logit; bins per unit of a logit
+    float edge;          // where the first bin begins: at the largest logit or above it
     double log2_per;     // log2(e) / T
     double least;        // least difference that min_p leaves
     double up;           // 2^S
+    double bin_up;       // 2^40, or 2^S if that is less
     // (of two infinities too)
     __device__ __forceinline__ double down(float l) const { return l == top ? 0.0 : (double)l - (double)top; }
-    __device__ __forceinline__ int bin(float l) const {   // rises as the logit falls, by steps of 1/64 of z
-        const float b = l == top ? 0.f : (top - l) * per;
+    __device__ __forceinline__ int bin(float l) const {   // rises as the logit falls, by steps of 1/32 of z
+        const float b = l == edge ? 0.f : (edge - l) * per;
         return b < (float)kZeroBin ? (int)b : kZeroBin;   // (NaN, of -inf and T = inf, as well)
     }
-    // e^z; 0 for what is too small to have a mass
-    __device__ __forceinline__ double part(double d) const {
-        const double t = d * log2_per, n = t + 0x1.8p52, r = t - (n - 0x1.8p52);
+    // the same for a finite edge, and 0 above it; and e^z relative to the middle of that bin, in multiples of 1 / bin_up
+    __device__ __forceinline__ int bin_below(float l) const { return (int)fminf(fmaxf((edge - l) * per, 0.f), (float)kZeroBin); }
+    __device__ __forceinline__ uint64_t mass_in_bin(float l, int b) const {
+        const double r = fma((double)l - (double)edge, log2_per, times_plus((double)b, kBinLog2, kBinLog2 / 2));
+        return (uint64_t)__double_as_longlong(fma(exp2_in_bin(r), bin_up, 0x1p52)) & 0xfffffffffffffull;
+    }
+    // masses of a bin, from the sum of the above
+    __device__ __forceinline__ uint64_t mass_of_bin(uint64_t sum, int b) const {
+        const double t = ((double)edge - (double)top) * log2_per - ((double)b + 0.5) * kBinLog2;
+        return b < kZeroBin ? (uint64_t)((double)sum * (power(t) * (up / bin_up)) + 0.5) : 0;
+    }
+    // 2^t; 0 for what is too small to have a mass
+    __device__ __forceinline__ double power(double t) const {
+        const double n = t + 0x1.8p52, r = t - (n - 0x1.8p52);
         const double e = exp2_near(r);
         const uint64_t bits = __double_as_longlong(e) + ((uint64_t)__double_as_longlong(n) << 52);
         return t > -64.0 ? __longlong_as_double((long long)bits) : 0.0;
     }
+    // e^z
+    __device__ __forceinline__ double part(double d) const { return power(d * log2_per); }
     __device__ __forceinline__ uint64_t mass_of(double d) const {
         const double v = fma(part(d), up, 0x1p52);   // rounded to a whole number
         return (uint64_t)__double_as_longlong(v) & 0xfffffffffffffull;
@@ -106,30 +135,44 @@ __device__ __forceinline__ uint64_t wave_total(uint64_t v) {
     return lane64(v, 0) + lane64(v, 16) + lane64(v, 32) + lane64(v, 48);
 }
 __device__ __forceinline__ float wave_largest(float v) {
-#pragma unroll
-    for (int i = 32; i; i >>= 1) v = fmaxf(v, __shfl_xor(v, i));
-    return v;
+    v = fmaxf(v, dpp<0x128>(v));
+    v = fmaxf(v, dpp<0x124>(v));
+    v = fmaxf(v, dpp<0x122>(v));
+    v = fmaxf(v, dpp<0x121>(v));
+    const int b = __float_as_int(v);
+    return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 0)), __int_as_float(__builtin_amdgcn_readlane(b, 16))),
+                 fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
 }
-// sum over this lane and those before it
+// sum over this lane and those before it: within the rows of 16 lanes by shifts (0 comes in), then the last lane of a row to the next one, then
+// that of the second row to the third and fourth
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t from_below(uint64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, true);
+    return (uint64_t)hi << 32 | lo;
+}
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const uint64_t below = (uint64_t)__shfl_up((unsigned long long)v, i);
-        if (lane >= i) v += below;
-    }
+    v += from_below<0x111, 0xf>(v);   // row_shr:1
+    v += from_below<0x112, 0xf>(v);
+    v += from_below<0x114, 0xf>(v);
+    v += from_below<0x118, 0xf>(v);
+    v += from_below<0x142, 0xa>(v);   // row_bcast:15, to rows 1 and 3
+    v += from_below<0x143, 0xc>(v);   // row_bcast:31, to rows 2 and 3
     return v;
 }
 
 struct Border { float value; uint64_t ties; };   // all logits above the value, and the first few of those equal to it
 
-template <int THREADS, int TILES>
+template <int THREADS, int TILES, int LIST>
 struct SampleLds {
-    uint64_t sums[kBins];            // of a bin's masses, or the number of its logits
+    union {
+        uint64_t sums[kBins];                // of a bin's masses, or the number of its logits
+        float some[THREADS / 64][512];       // a wavefront's logits of a tile that are left
+    };
     uint64_t tile_mass[TILES];       // above the border
     uint32_t tile_equal[TILES];      // logits equal to it
-    float list[kList];
-    uint32_t at[kList];              // their words
+    float list[LIST];
+    uint32_t at[LIST];              // their words
     uint64_t waves[2][THREADS / 64];
     uint64_t found[3];
     uint32_t listed, key_lo, key_hi;
@@ -173,7 +216,7 @@ __device__ __forceinline__ void walk(const T *row, int64_t words, F &&f) { walk<
 // A row of logits and a workgroup's work on it.
 template <class T, int THREADS, int TILES>
 struct Row {
-    SampleLds<THREADS, TILES> &s;
+    SampleLds<THREADS, TILES, kList<THREADS>> &s;
     const T *row;
     int64_t words;
     int tile_log;
@@ -214,7 +257,7 @@ struct Row {
         if (tid == 0) s.found[0] = kBins;
         const uint64_t upto = scan(0, sum, total);
         if (of_whole) {
-            const double want = share * (double)total;
+            const double want = (share - 0x1p-40) * (double)total;
             goal = (uint64_t)want;
             goal += (double)goal < want;
             goal = uniform(goal < 1 ? 1 : goal > total ? total : goal);
@@ -244,21 +287,42 @@ struct Row {
     }
     __device__ __forceinline__ void put(float l, int64_t word) {
         const uint32_t n = atomicAdd(&s.listed, 1u);
-        if (n < kList) {
+        if (n < kList<THREADS>) {
             s.list[n] = l;
             s.at[n] = (uint32_t)word;
         }
     }
     __device__ __forceinline__ int tile_of(int64_t word) const { return (int)(word >> (9 + tile_log)); }
 
-    // Lists all logits of the bins up to `last`; false if they are too many.
+    // The least logit that holds, where all above a logit that holds do; NaN if the largest does not.  The 64 lanes try as many at a time.
+    template <class F>
+    __device__ __forceinline__ float least_of(F &&holds) const {
+        if (!holds(sc.top)) return NAN;
+        uint32_t lo = key_of(-INFINITY), hi = key_of(sc.top);
+#pragma unroll 1
+        while (lo < hi) {
+            const uint32_t step = (hi - lo) / 64 + 1, at = (uint32_t)(tid & 63) * step;
+            const uint64_t yes = __builtin_amdgcn_ballot_w64(at <= hi - lo && holds(of_key(lo + at)));
+            const uint32_t first = yes ? (uint32_t)__builtin_ctzll(yes) : 64u;   // (64: beyond the last one tried)
+            const uint32_t from = first ? lo + (first - 1) * step + 1 : lo;
+            if (yes) hi = lo + first * step;
+            lo = from < hi ? from : hi;
+        }
+        return of_key(hi);
+    }
+    __device__ __forceinline__ float least_of_bin(int bin) const {
+        return least_of([&](float l) { return sc.bin(l) <= bin; });
+    }
+
+    // Lists all logits of the bins up to `last`, which is before kZeroBin; false if they are too many.
     __device__ __forceinline__ bool list_upto(int last) {
         if (tid == 0) s.listed = 0;
         __syncthreads();
+        const float least = least_of_bin(last);
         walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
             bool hit[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) hit[i] = v[i] > -INFINITY && sc.bin(v[i]) <= last;
+            for (int i = 0; i < 4; ++i) hit[i] = v[i] >= least;
             if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -266,18 +330,19 @@ struct Row {
             }
         });
         __syncthreads();
-        return uniform(s.listed) <= (uint32_t)kList;
+        return uniform(s.listed) <= (uint32_t)kList<THREADS>;
     }
 
     // First half of a border's search: the bin in which the logits in falling order reach the goal, or kZeroBin if they do not.  Only logits
-    // above `above` count, and above.ties of those equal to it.
-    __device__ __forceinline__ int find_bin(bool mass, Border above, double share, uint64_t &goal, uint64_t &before) {
-        clear();
+    // above `above` count, and above.ties of those equal to it.  `ready`: the sums are there.
+    __device__ __forceinline__ int find_bin(bool ready, bool mass, Border above, double share, uint64_t &goal, uint64_t &before) {
+        if (!ready) clear();
         auto take = [&](float l) {
             const int b = sc.bin(l);
             if (b < kZeroBin && l > above.value) add(mass, b, l);
         };
-        if (all_listed) {
+        if (ready) ;
+        else if (all_listed) {
             for (uint32_t i = tid; i < s.listed; i += THREADS) take(s.list[i]);
         } else
             walk<T, THREADS, 4>(row, words, [&](int64_t, auto v) {
@@ -291,7 +356,8 @@ struct Row {
     }
 
     // Masses of the tiles (if `sums`) of the bins before `bin`, of logits that min_p leaves; and a list of that bin's logits, unless all are
-    // listed.
+    // listed.  Of a tile's logits few are left, as a rule: a wavefront puts them side by side first, so that it computes 64 masses that count at
+    // a time (2048 rows of 141,000 words in binary32, min_p 0.05: 390 us; without a limit, with the masses of all, 451).
     __device__ __forceinline__ void sum_and_list(bool sums, int bin) {
         __syncthreads();
         for (int i = tid; i < TILES; i += THREADS) {
@@ -306,18 +372,23 @@ struct Row {
                     const float l = s.list[i];
                     if (sc.bin(l) < bin && sc.down(l) >= sc.least) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(s.at[i])], (unsigned long long)sc.mass(l));
                 }
-        } else {
-            uint64_t sum = 0;
+        } else if (bin < kZeroBin || sc.least > -INFINITY) {
+            const int lane = tid & 63;
+            float *const some = s.some[uniform(threadIdx.x >> 6)];
+            const float in = bin < kZeroBin ? least_of_bin(bin) : NAN;                    // NaN: none
+            float above = bin == kZeroBin ? -INFINITY : bin ? least_of_bin(bin - 1) : NAN, left = above;
+            if (sc.least > -INFINITY && above == above) left = fmaxf(above, least_of([&](float l) { return sc.down(l) >= sc.least; }));
+            uint32_t n = 0;
             walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
                 bool hit[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int b = sc.bin(v[i]);
-                    hit[i] = b == bin && b < kZeroBin;
+                    hit[i] = v[i] >= in && !(v[i] >= above);
                     if (sums) {
-                        const double d = sc.down(v[i]);
-                        const uint64_t m = sc.mass_of(d);
-                        sum += b < bin && d >= sc.least ? m : 0;
+                        const bool is = v[i] >= left;
+                        const uint64_t all = __builtin_amdgcn_ballot_w64(is);
+                        if (is) some[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = v[i];
+                        n += (uint32_t)__builtin_popcountll(all);
                     }
                 }
                 if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
@@ -326,11 +397,27 @@ struct Row {
                         if (hit[i]) put(v[i], c + i);
                 }
             }, [&](int64_t c) {
-                if (sums) {
-                    sum = wave_total(sum);
-                    if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(c)], (unsigned long long)sum);
-                    sum = 0;
-                }
+                if (!n) return;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+                __builtin_amdgcn_wave_barrier();
+                uint64_t sum = 0;
+#pragma unroll 1
+                for (uint32_t i = 0; i < n; i += 64) sum += sc.mass(i + lane < n ? some[i + lane] : -INFINITY);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+                __builtin_amdgcn_wave_barrier();
+                n = 0;
+                sum = wave_total(sum);
+                if (lane == 0 && sum) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(c)], (unsigned long long)sum);
+            });
+        } else if (sums) {
+            uint64_t sum = 0;
+            walk<T, THREADS, 4>(row, words, [&](int64_t, auto v) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += sc.mass(v[i]);
+            }, [&](int64_t c) {
+                sum = wave_total(sum);
+                if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(c)], (unsigned long long)sum);
+                sum = 0;
             });
         }
         __syncthreads();
@@ -339,7 +426,7 @@ struct Row {
     // f(logit, word) for the logits of a bin: of the list, or if they did not fit, of the row.
     template <class F>
     __device__ __forceinline__ void of_bin(int bin, F &&f) {
-        if (s.listed <= (uint32_t)kList) {
+        if (s.listed <= (uint32_t)kList<THREADS>) {
             for (uint32_t i = tid; i < s.listed; i += THREADS)
                 if (sc.bin(s.list[i]) == bin) f(s.list[i], (int64_t)s.at[i]);
         } else
@@ -384,7 +471,11 @@ struct Row {
             });
             if (tied && tid == 0 && above_key >= lo && above_key <= hi) add_ties((int)((hi - above_key) >> shift), above);
             const int part = reach(before, false, 0.0, goal);
-            if (part >= kBins) break;   // (cannot be: the range holds what is missing)
+            if (part >= kBins) {        // the bin's sum in the histogram of all words was greater by its rounding: all of the bin
+                hi = lo;
+                goal = ~0ull >> 2;
+                break;
+            }
             const uint32_t top = hi - ((uint32_t)part << shift), width = (1u << shift) - 1;
             lo = top - lo > width ? top - width : lo;
             hi = top;
@@ -411,168 +502,215 @@ struct Row {
     }
 };
 
-// A row per workgroup.  It is read once for its largest logit; then, if top_k is small, once to list the few logits that can be left, among them
-// the top_k largest of the threads' own maxima; else once for every limit's histogram, and once for the masses of its tiles of 512 words and
-// a list of the bin with the border.  The word is found in its tile.
+// A row per workgroup.  It is read once for its largest logit and, if top_k is not small or top_p is given, the first limit's histogram; then, if
+// top_k is small, once to list the few logits that can be left, among them the top_k largest of the threads' own maxima; else once for the masses of
+// its tiles of 512 words and a list of the bin with the border (top_k not small and top_p: both a second time, for top_p).  The word is found
+// in its tile.  (No loop over rows: what the compiler moved out of one did not fit the registers, 690 us instead of 515 for 2048 rows of 141,000 words in
+// binary32 with top_p, 67 instead of 20 for 4096 largest of 5000 in bf16.)
 template <class T, int THREADS, int TILES>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 2) void sample_kernel(Sample a) {
-    __shared__ SampleLds<THREADS, TILES> s;
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
+    __shared__ SampleLds<THREADS, TILES, kList<THREADS>> s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *logits = static_cast<const T *>(a.logits) + row * a.stride;
-        const int64_t V = a.words;
-        const float temperature = uniform(a.temperatures ? a.temperatures[row] : a.temperature);
-        const int64_t top_k = (int64_t)uniform((uint64_t)(a.top_ks ? (a.top_k64 ? static_cast<const int64_t *>(a.top_ks)[row] : (int64_t)static_cast<const int32_t *>(a.top_ks)[row]) : a.top_k));
-        const float top_p = uniform(a.top_ps ? a.top_ps[row] : a.top_p), min_p = uniform(a.min_ps ? a.min_ps[row] : a.min_p);
-        const float u = a.u[row];
+    const int64_t row = a.first_row + blockIdx.x;
+    const T *logits = static_cast<const T *>(a.logits) + row * a.stride;
+    const int64_t V = a.words;
+    const float temperature = uniform(a.temperatures ? a.temperatures[row] : a.temperature);
+    const int64_t top_k = (int64_t)uniform((uint64_t)(a.top_ks ? (a.top_k64 ? static_cast<const int64_t *>(a.top_ks)[row] : (int64_t)static_cast<const int32_t *>(a.top_ks)[row]) : a.top_k));
+    const float top_p = uniform(a.top_ps ? a.top_ps[row] : a.top_p), min_p = uniform(a.min_ps ? a.min_ps[row] : a.min_p);
+    const float u = a.u[row];
 
-        float own = -INFINITY;
-        bool odd = false;
-        walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                own = fmaxf(own, v[i]);
-                odd |= v[i] != v[i];
-            }
-        });
-        float top = wave_largest(own);
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-        __syncthreads();             // (the row before is done)
-        if (lane == 0) s.waves[0][wave] = (uint64_t)odd << 32 | __float_as_uint(top);
+    const bool greedy = !(temperature > 0.f), has_k = !greedy && top_k > 0 && top_k < V, has_p = !greedy && top_p < 1.f;
+    const bool few = has_k && top_k <= kMaxima * THREADS / 2;
+    Scale sc;
+    sc.per = uniform(fminf(kBinsPerUnit / temperature, 0x1.fffffep127f));
+    sc.log2_per = uniform(1.44269504088896340736 / (double)temperature);
+    sc.up = (double)((uint64_t)1 << a.mass_log);
+    sc.bin_up = (double)((uint64_t)1 << (a.mass_log < 40 ? a.mass_log : 40));
+    Row<T, THREADS, TILES> r{s, logits, V, a.tile_log, sc, false};
+
+    // a wave's largest value and whether any is odd, over the workgroup
+    auto join = [&](float &most, bool &any) {
+        most = wave_largest(most);
+        any = __builtin_amdgcn_ballot_w64(any) != 0;
         __syncthreads();
-        odd = false;
+        if (lane == 0) s.waves[0][wave] = (uint64_t)any << 32 | __float_as_uint(most);
+        __syncthreads();
+        any = false;
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) {
-            odd |= (s.waves[0][w] >> 32) != 0;
-            top = fmaxf(top, __uint_as_float((uint32_t)s.waves[0][w]));
+            any |= (s.waves[0][w] >> 32) != 0;
+            most = fmaxf(most, __uint_as_float((uint32_t)s.waves[0][w]));
         }
-        top = uniform(top);
-        __syncthreads();
-        if (odd || top == -INFINITY) {   // a NaN among the logits, or nothing to draw from
-            if (tid == 0) {
-                a.word[row] = -1;
-                a.p[row] = odd ? NAN : 0.f;
-            }
-            continue;
-        }
-        if (!(temperature > 0.f)) {      // the first of the largest
-            uint32_t at = 0xffffffffu;
-            walk<T, THREADS, 4>(logits, V, [&](int64_t c, auto v) {
+        most = uniform(most);
+    };
+    bool ready = !few && (has_k || has_p), odd = false;
+    if (ready) {                     // a histogram at once, from the largest of the first logits plus some room on
+        const int64_t c = (int64_t)tid * 8;
+        const f32x8 v = load8(logits + c, V - c);
+        float first = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (v[i] == top) at = min(at, (uint32_t)(c + i));
-            });
-            if (tid == 0) s.listed = 0xffffffffu;
-            __syncthreads();
-            if (at != 0xffffffffu) atomicMin(&s.listed, at);
-            __syncthreads();
-            if (tid == 0) {
-                a.word[row] = (int64_t)s.listed;
-                a.p[row] = 1.f;
+        for (int i = 0; i < 8; ++i) first = fmaxf(first, c + i < V ? v[i] : -INFINITY);
+        join(first, odd);
+        r.sc.edge = uniform(first + kRoom * temperature);
+        ready = fabsf(r.sc.edge) < INFINITY;
+        r.clear();
+    }
+    float own[kMaxima];
+#pragma unroll
+    for (int i = 0; i < kMaxima; ++i) own[i] = -INFINITY;
+    odd = false;
+    auto largest = [&](auto v) {
+#pragma unroll
+        for (int i = 0; i < kMaxima; ++i) {
+            own[i] = fmaxf(own[i], v[i]);
+            odd |= v[i] != v[i];
+        }
+    };
+    if (ready && has_k)
+        walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
+            largest(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicAdd((unsigned long long *)&s.sums[r.sc.bin_below(v[i])], 1ull);
+        });
+    else if (ready)
+        walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
+            largest(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = r.sc.bin_below(v[i]);
+                atomicAdd((unsigned long long *)&s.sums[b], (unsigned long long)r.sc.mass_in_bin(v[i], b));
             }
-            continue;
+        });
+    else
+        walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) { largest(v); });
+    float top = fmaxf(fmaxf(own[0], own[1]), fmaxf(own[2], own[3]));
+    join(top, odd);
+    __syncthreads();
+    if (odd || top == -INFINITY) {   // a NaN among the logits, or nothing to draw from
+        if (tid == 0) {
+            a.word[row] = -1;
+            a.p[row] = odd ? NAN : 0.f;
         }
-        Scale sc;
-        sc.top = top;
-        sc.per = uniform(kBinsPerUnit / temperature);
-        sc.log2_per = uniform(1.44269504088896340736 / (double)temperature);
-        sc.least = uniform(min_p > 0.f ? (min_p < 1.f ? log((double)min_p) * (double)temperature : 0.0) : -INFINITY);
-        sc.up = (double)((uint64_t)1 << a.mass_log);
-        Row<T, THREADS, TILES> r{s, logits, V, a.tile_log, sc, false};
+        return;
+    }
+    if (greedy) {                    // the first of the largest
+        uint32_t at = 0xffffffffu;
+        walk<T, THREADS, 4>(logits, V, [&](int64_t c, auto v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[i] == top) at = min(at, (uint32_t)(c + i));
+        });
+        if (tid == 0) s.listed = 0xffffffffu;
+        __syncthreads();
+        if (at != 0xffffffffu) atomicMin(&s.listed, at);
+        __syncthreads();
+        if (tid == 0) {
+            a.word[row] = (int64_t)s.listed;
+            a.p[row] = 1.f;
+        }
+        return;
+    }
+    ready = ready && top <= r.sc.edge;   // (else a later logit was far above the first ones)
+    r.sc.top = top;
+    if (!ready) r.sc.edge = top;
+    r.sc.least = uniform(min_p > 0.f ? (min_p < 1.f ? log((double)min_p) * (double)temperature : 0.0) : -INFINITY);
+    if (ready && !has_k)
+        for (int i = tid; i < kBins; i += THREADS) s.sums[i] = r.sc.mass_of_bin(s.sums[i], i);
 
-        const bool has_k = top_k > 0 && top_k < V, has_p = top_p < 1.f;
-        Border border{-INFINITY, 0};
-        uint64_t goal = (uint64_t)top_k, before = 0;
-        if (has_k && top_k <= THREADS / 2) {
-            // the k-th largest logit is not below the k-th largest of the threads' maxima
-            r.clear();
-            if (own > -INFINITY && sc.bin(own) < kZeroBin) r.add(false, sc.bin(own), own);
-            const int last = r.reach(before, false, 0.0, goal);
-            if (last < kZeroBin) r.all_listed = r.list_upto(last);
-        }
+    Border border{-INFINITY, 0};
+    uint64_t goal = (uint64_t)top_k, before = 0;
+    if (few) {
+        // the k-th largest logit is not below the k-th largest of the threads' maxima
+        r.clear();
+#pragma unroll
+        for (int i = 0; i < kMaxima; ++i)
+            if (own[i] > -INFINITY && r.sc.bin(own[i]) < kZeroBin) r.add(false, r.sc.bin(own[i]), own[i]);
+        const int last = r.reach(before, false, 0.0, goal);
+        if (last < kZeroBin) r.all_listed = r.list_upto(last);
+    }
 #pragma unroll 1
-        for (int limit = 0; limit < 3; ++limit) {       // top_k, top_p, and where there is neither the sums alone
-            if (limit == 0 ? !has_k : limit == 1 ? !has_p : has_k || has_p) continue;
-            const bool mass = limit == 1, sums = limit > 0 || !has_p;
-            const int bin = limit == 2 ? kZeroBin : r.find_bin(mass, border, top_p > 0.f ? (double)top_p : 0.0, goal, before);
-            r.sum_and_list(sums, bin);
-            if (bin < kZeroBin) {
-                border = r.border_in(mass, bin, border, goal, before);
-                if (sums) r.add_bin(bin, border);
-            }
+    for (int limit = 0; limit < 3; ++limit) {       // top_k, top_p, and where there is neither the sums alone
+        if (limit == 0 ? !has_k : limit == 1 ? !has_p : has_k || has_p) continue;
+        const bool mass = limit == 1, sums = limit > 0 || !has_p;
+        const int bin = limit == 2 ? kZeroBin : r.find_bin(ready, mass, border, top_p > 0.f ? (double)top_p : 0.0, goal, before);
+        ready = false;
+        r.sum_and_list(sums, bin);
+        if (bin < kZeroBin) {
+            border = r.border_in(mass, bin, border, goal, before);
+            if (sums) r.add_bin(bin, border);
         }
+    }
 
-        constexpr int EACH = (TILES + THREADS - 1) / THREADS;
-        const uint64_t tie = border.value > -INFINITY && sc.down(border.value) >= sc.least ? sc.mass(border.value) : 0;
-        uint64_t masses[EACH], equals[EACH], sum = 0, equal = 0, total;
+    constexpr int EACH = (TILES + THREADS - 1) / THREADS;
+    const uint64_t tie = border.value > -INFINITY && r.sc.down(border.value) >= r.sc.least ? r.sc.mass(border.value) : 0;
+    uint64_t masses[EACH], equals[EACH], sum = 0, equal = 0, total;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const bool is = tid * EACH + i < TILES;
-            masses[i] = is ? s.tile_mass[tid * EACH + i] : 0;
-            equal += equals[i] = is ? s.tile_equal[tid * EACH + i] : 0;
+    for (int i = 0; i < EACH; ++i) {
+        const bool is = tid * EACH + i < TILES;
+        masses[i] = is ? s.tile_mass[tid * EACH + i] : 0;
+        equal += equals[i] = is ? s.tile_equal[tid * EACH + i] : 0;
+    }
+    uint64_t equal_before = r.scan(0, equal, total) - equal;
+    const uint64_t first_equal = equal_before;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint64_t room = equal_before < border.ties ? border.ties - equal_before : 0;
+        masses[i] += (equals[i] < room ? equals[i] : room) * tie;
+        equal_before += equals[i];
+        sum += masses[i];
+    }
+    uint64_t at = r.scan(1, sum, total) - sum;
+    const float within = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+    const uint64_t target = (uint64_t)((double)within * (double)total);
+    equal_before = first_equal;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (at <= target && at + masses[i] > target) {
+            s.found[0] = (uint64_t)(tid * EACH + i);
+            s.found[1] = at;
+            s.found[2] = equal_before;
         }
-        uint64_t equal_before = r.scan(0, equal, total) - equal;
-        const uint64_t first_equal = equal_before;
+        at += masses[i];
+        equal_before += equals[i];
+    }
+    __syncthreads();
+    if (wave == 0) {                 // the word, in its tile
+        int64_t c = (int64_t)s.found[0] << (9 + a.tile_log);
+        uint64_t sum_before = s.found[1], seen = s.found[2];
+        const int64_t end = c + ((int64_t)512 << a.tile_log) < V ? c + ((int64_t)512 << a.tile_log) : V;
+        for (; c < end; c += 512) {
+            const int64_t first = c + lane * 8;
+            const int n = end - first < 8 ? (end - first > 0 ? (int)(end - first) : 0) : 8;
+            const f32x8 v = load8(logits + first, n);
+            uint32_t mine = 0;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const uint64_t room = equal_before < border.ties ? border.ties - equal_before : 0;
-            masses[i] += (equals[i] < room ? equals[i] : room) * tie;
-            equal_before += equals[i];
-            sum += masses[i];
-        }
-        uint64_t at = r.scan(1, sum, total) - sum;
-        const float within = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-        const uint64_t target = (uint64_t)((double)within * (double)total);
-        equal_before = first_equal;
+            for (int i = 0; i < 8; ++i) mine += i < n && tie && v[i] == border.value;
+            const uint64_t to_here = wave_scan(mine);
+            uint64_t rank = seen + to_here - mine, m[8], own_sum = 0;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            if (at <= target && at + masses[i] > target) {
-                s.found[0] = (uint64_t)(tid * EACH + i);
-                s.found[1] = at;
-                s.found[2] = equal_before;
+            for (int i = 0; i < 8; ++i) {
+                m[i] = 0;
+                if (i < n) {
+                    if (v[i] > border.value && r.sc.down(v[i]) >= r.sc.least) m[i] = r.sc.mass(v[i]);
+                    else if (tie && v[i] == border.value) m[i] = rank++ < border.ties ? tie : 0;
+                }
+                own_sum += m[i];
+                __builtin_amdgcn_sched_barrier(0);
             }
-            at += masses[i];
-            equal_before += equals[i];
-        }
-        __syncthreads();
-        if (wave == 0) {                 // the word, in its tile
-            int64_t c = (int64_t)s.found[0] << (9 + a.tile_log);
-            uint64_t sum_before = s.found[1], seen = s.found[2];
-            const int64_t end = c + ((int64_t)512 << a.tile_log) < V ? c + ((int64_t)512 << a.tile_log) : V;
-            for (; c < end; c += 512) {
-                const int64_t first = c + lane * 8;
-                const int n = end - first < 8 ? (end - first > 0 ? (int)(end - first) : 0) : 8;
-                const f32x8 v = load8(logits + first, n);
-                uint32_t mine = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mine += i < n && tie && v[i] == border.value;
-                const uint64_t to_here = wave_scan(mine);
-                uint64_t rank = seen + to_here - mine, m[8], own_sum = 0;
+            const uint64_t upto = wave_scan(own_sum);
+            uint64_t sum_at = sum_before + upto - own_sum;
+            if (sum_at <= target && sum_at + own_sum > target) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    m[i] = 0;
-                    if (i < n) {
-                        if (v[i] > border.value && sc.down(v[i]) >= sc.least) m[i] = sc.mass(v[i]);
-                        else if (tie && v[i] == border.value) m[i] = rank++ < border.ties ? tie : 0;
+                    if (sum_at <= target && sum_at + m[i] > target) {
+                        a.word[row] = first + i;
+                        a.p[row] = (float)(r.sc.part(r.sc.down(v[i])) / ((double)total / r.sc.up));
                     }
-                    own_sum += m[i];
-                    __builtin_amdgcn_sched_barrier(0);
+                    sum_at += m[i];
                 }
-                const uint64_t upto = wave_scan(own_sum);
-                uint64_t sum_at = sum_before + upto - own_sum;
-                if (sum_at <= target && sum_at + own_sum > target) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (sum_at <= target && sum_at + m[i] > target) {
-                            a.word[row] = first + i;
-                            a.p[row] = (float)(sc.part(sc.down(v[i])) / ((double)total / sc.up));
-                        }
-                        sum_at += m[i];
-                    }
-                }
-                sum_before += lane64(upto, 63);
-                seen += lane64(to_here, 63);
             }
+            sum_before += lane64(upto, 63);
+            seen += lane64(to_here, 63);
         }
     }
 }

@@ -269,7 +269,8 @@ extern "C" int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_s
 // ---- words drawn from logits -------------------------------------------------------------------------------------------------
 
 namespace {
-constexpr int kFewTiles = 16, kManyTiles = 2048;   // of 512 words or more
+constexpr int kFewTiles = 16, kManyTiles = 512;   // of 512 words or more
+constexpr int64_t kMostRows = (int64_t)1 << 21;    // of a launch (of fewer than 2^32 threads)
 }
 
 extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, int64_t words, int dtype, const float *u, const float *temperatures,
@@ -295,15 +296,18 @@ extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, in
     OPS_TRY(check_pointer(who, "p", p, 4));
     int bits = 0;
     while (((int64_t)1 << bits) < words) ++bits;
-    Sample a{logits, stride, rows, words, u, temperatures, temperature, top_ks, top_k64, top_k, top_ps, top_p, min_ps, min_p, word, p, 0, bits < 17 ? 45 : 62 - bits};
+    Sample a{logits, stride, 0, words, u, temperatures, temperature, top_ks, top_k64, top_k, top_ps, top_p, min_ps, min_p, word, p, 0, bits < 17 ? 45 : 62 - bits};
     while (parts_of(words, (int64_t)512 << a.tile_log) > kManyTiles) ++a.tile_log;
-    const unsigned grid = (unsigned)(rows < 16 * kCus ? rows : 16 * kCus);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto e) -> int {
         using T = decltype(e);
-        if (words <= 512 * kFewTiles) sample_kernel<T, 256, kFewTiles><<<grid, 256, 0, st>>>(a);
-        else sample_kernel<T, 512, kManyTiles><<<grid, 512, 0, st>>>(a);
-        OPS_HIP(hipGetLastError());
+        for (; a.first_row < rows; a.first_row += kMostRows) {
+            const unsigned grid = (unsigned)(rows - a.first_row < kMostRows ? rows - a.first_row : kMostRows);
+            if (words <= 512 * kFewTiles) sample_kernel<T, 256, kFewTiles><<<grid, 256, 0, st>>>(a);
+            else if (rows <= kCus) sample_kernel<T, 1024, kManyTiles><<<grid, 1024, 0, st>>>(a);
+            else sample_kernel<T, 512, kManyTiles><<<grid, 512, 0, st>>>(a);
+            OPS_HIP(hipGetLastError());
+        }
         return SABER_OK;
     });
 }
