@@ -84,7 +84,7 @@ struct Scale {
         return b < (float)kZeroBin ? (int)b : kZeroBin;   // (NaN, of -inf and T = inf, as well)
     }
     // the same for a finite edge, and 0 above it; and e^z relative to the middle of that bin, in multiples of 1 / bin_up
-    __device__ __forceinline__ int bin_below(float l) const { return (int)fminf(fmaxf((edge - l) * per, 0.f), (float)kZeroBin); }
+    __device__ __forceinline__ int bin_below(float l) const { return (int)__builtin_amdgcn_fmed3f((edge - l) * per, 0.f, (float)kZeroBin); }
     __device__ __forceinline__ uint64_t mass_in_bin(float l, int b) const {
         const double r = fma((double)l - (double)edge, log2_per, times_plus((double)b, kBinLog2, kBinLog2 / 2));
         return (uint64_t)__double_as_longlong(fma(exp2_in_bin(r), bin_up, 0x1p52)) & 0xfffffffffffffull;
@@ -94,13 +94,14 @@ struct Scale {
         const double t = ((double)edge - (double)top) * log2_per - ((double)b + 0.5) * kBinLog2;
         return b < kZeroBin ? (uint64_t)((double)sum * (power(t) * (up / bin_up)) + 0.5) : 0;
     }
-    // 2^t; 0 for what is too small to have a mass
-    __device__ __forceinline__ double power(double t) const {
+    // 2^t, t > -64
+    __device__ __forceinline__ double power_near(double t) const {
         const double n = t + 0x1.8p52, r = t - (n - 0x1.8p52);
         const double e = exp2_near(r);
-        const uint64_t bits = __double_as_longlong(e) + ((uint64_t)__double_as_longlong(n) << 52);
-        return t > -64.0 ? __longlong_as_double((long long)bits) : 0.0;
+        return __longlong_as_double(__double_as_longlong(e) + (long long)((uint64_t)__double_as_longlong(n) << 52));
     }
+    // 0 for what is too small to have a mass
+    __device__ __forceinline__ double power(double t) const { return t > -64.0 ? power_near(t) : 0.0; }
     // e^z
     __device__ __forceinline__ double part(double d) const { return power(d * log2_per); }
     __device__ __forceinline__ uint64_t mass_of(double d) const {
@@ -108,6 +109,12 @@ struct Scale {
         return (uint64_t)__double_as_longlong(v) & 0xfffffffffffffull;
     }
     __device__ __forceinline__ uint64_t mass(float l) const { return mass_of(down(l)); }
+    // of a logit of a bin before kZeroBin, or one that min_p leaves: finite, or equal to the largest
+    __device__ __forceinline__ uint64_t mass_left(float l) const {
+        const double d = (double)fminf(l, 0x1.fffffep127f) - (double)fminf(top, 0x1.fffffep127f);
+        const double v = fma(power_near(fmax(d * log2_per, -64.0)), up, 0x1p52);
+        return (uint64_t)__double_as_longlong(v) & 0xfffffffffffffull;
+    }
 };
 
 __device__ __forceinline__ uint32_t key_of(float f) {   // the order of the floats; -0 and 0 are equal
@@ -167,7 +174,7 @@ template <int THREADS, int TILES, int LIST>
 struct SampleLds {
     union {
         uint64_t sums[kBins];                // of a bin's masses, or the number of its logits
-        float some[THREADS / 64][512];       // a wavefront's logits of a tile that are left
+        struct { float l[512]; uint32_t at[512]; } some[THREADS / 64];   // a wavefront's logits of a tile that are left, and their words
     };
     uint64_t tile_mass[TILES];       // above the border
     uint32_t tile_equal[TILES];      // logits equal to it
@@ -175,32 +182,32 @@ struct SampleLds {
     uint32_t at[LIST];              // their words
     uint64_t waves[2][THREADS / 64];
     uint64_t found[3];
-    uint32_t listed, key_lo, key_hi;
+    uint32_t listed;
 };
 
 // f(first word, four logits) for all of a row, a tile of 512 words per wavefront at a time, AHEAD of them on their way; done(first word of
-// the lane in the tile) after a lane's eight.  Logits past the row's end are -inf.
+// the lane in the tile) after a lane's eight.  The logits after the last whole tile come one by one, -inf past the row's end (the kernel's code
+// has to fit the instruction cache: with a check at every load it was 85 KB).
 template <class T, int THREADS, int AHEAD, class F, class D>
 __device__ __forceinline__ void walk(const T *row, int64_t words, F &&f, D &&done) {
     typedef float f32x4_ __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(1))) Any { Raw8<T> r; };
     const int lane = threadIdx.x & 63;
     constexpr int64_t step = THREADS / 64 * 512;
-    for (int64_t c0 = (int64_t)uniform(threadIdx.x >> 6) * 512; c0 < words; c0 += AHEAD * step) {
+    const int64_t whole = words & ~(int64_t)511;
+#pragma unroll 1
+    for (int64_t c0 = (int64_t)uniform(threadIdx.x >> 6) * 512; c0 < whole; c0 += AHEAD * step) {
         Raw8<T> raw[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int64_t c = c0 + k * step + lane * 8;
-            raw[k] = load_raw8(row + c, words - c);
+            const int64_t c = c0 + (c0 + k * step < whole ? k * step : 0);   // (past the end: any)
+            raw[k] = reinterpret_cast<const Any *>(row + c + lane * 8)->r;
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (c0 + k * step < words) {
-                const int64_t c = c0 + k * step + lane * 8, left = words - c;
-                f32x8 v = widen(raw[k]);
-                if (left < 8) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : -INFINITY;
-                }
+            if (c0 + k * step < whole) {
+                const int64_t c = c0 + k * step + lane * 8;
+                const f32x8 v = widen(raw[k]);
                 const f32x4_ lo = v.lo, hi = v.hi;
                 f(c, lo);
                 __builtin_amdgcn_sched_barrier(0);
@@ -208,6 +215,15 @@ __device__ __forceinline__ void walk(const T *row, int64_t words, F &&f, D &&don
                 __builtin_amdgcn_sched_barrier(0);
                 done(c);
             }
+    }
+#pragma unroll 1
+    for (int64_t c0 = whole + (int64_t)uniform(threadIdx.x >> 6) * 256; c0 < words; c0 += THREADS * 4) {
+        const int64_t c = c0 + lane * 4;
+        f32x4_ v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = c + i < words ? (float)row[c + i] : -INFINITY;
+        f(c, v);
+        done(c);
     }
 }
 template <class T, int THREADS, int AHEAD, class F>
@@ -231,18 +247,19 @@ struct Row {
     }
     // sum over the threads up to and including this one, and over all of them
     __device__ __forceinline__ uint64_t scan(int which, uint64_t v, uint64_t &total) {
+        constexpr int W = THREADS / 64;
+        static_assert(W <= 16, "a row of lanes");
         const uint64_t own = wave_scan(v);
         if ((tid & 63) == 63) s.waves[which][tid >> 6] = own;
         __syncthreads();
-        uint64_t before = 0;
-        total = 0;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) {
-            const uint64_t x = s.waves[which][w];
-            if (w < (tid >> 6)) before += x;
-            total += x;
-        }
-        total = uniform(total);
+        uint64_t upto = s.waves[which][tid & (W - 1)];   // the wavefronts' sums, in every row of lanes
+        upto += from_below<0x111, 0xf>(upto);
+        upto += from_below<0x112, 0xf>(upto);
+        upto += from_below<0x114, 0xf>(upto);
+        upto += from_below<0x118, 0xf>(upto);
+        total = lane64(upto, W - 1);
+        const int wave = (int)uniform(threadIdx.x >> 6);
+        const uint64_t before = wave ? lane64(upto, wave - 1) : 0;
         __syncthreads();
         return before + own;
     }
@@ -374,27 +391,24 @@ struct Row {
                 }
         } else if (bin < kZeroBin || sc.least > -INFINITY) {
             const int lane = tid & 63;
-            float *const some = s.some[uniform(threadIdx.x >> 6)];
-            const float in = bin < kZeroBin ? least_of_bin(bin) : NAN;                    // NaN: none
-            float above = bin == kZeroBin ? -INFINITY : bin ? least_of_bin(bin - 1) : NAN, left = above;
-            if (sc.least > -INFINITY && above == above) left = fmaxf(above, least_of([&](float l) { return sc.down(l) >= sc.least; }));
+            auto &some = s.some[uniform(threadIdx.x >> 6)];
+            // from `above` on: before the bin; from `left` on: of them, what min_p leaves; NaN: none
+            const float above = bin == kZeroBin ? -INFINITY : bin ? least_of_bin(bin - 1) : NAN;
+            float left = sums ? above : NAN;
+            if (sums && sc.least > -INFINITY && above == above) left = fmaxf(above, least_of([&](float l) { return sc.down(l) >= sc.least; }));
+            const float from = bin < kZeroBin ? least_of_bin(bin) : left;
             uint32_t n = 0;
             walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
-                bool hit[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    hit[i] = v[i] >= in && !(v[i] >= above);
-                    if (sums) {
-                        const bool is = v[i] >= left;
-                        const uint64_t all = __builtin_amdgcn_ballot_w64(is);
-                        if (is) some[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = v[i];
-                        n += (uint32_t)__builtin_popcountll(all);
+                    const bool is = v[i] >= from && (sums || !(v[i] >= above));
+                    const uint64_t all = __builtin_amdgcn_ballot_w64(is);
+                    if (is) {
+                        const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, n));
+                        some.l[to] = v[i];
+                        some.at[to] = (uint32_t)c + i;
                     }
-                }
-                if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (hit[i]) put(v[i], c + i);
+                    n += (uint32_t)__builtin_popcountll(all);
                 }
             }, [&](int64_t c) {
                 if (!n) return;
@@ -402,10 +416,15 @@ struct Row {
                 __builtin_amdgcn_wave_barrier();
                 uint64_t sum = 0;
 #pragma unroll 1
-                for (uint32_t i = 0; i < n; i += 64) sum += sc.mass(i + lane < n ? some[i + lane] : -INFINITY);
+                for (uint32_t i = lane; i < n; i += 64) {
+                    const float l = some.l[i];
+                    if (l >= left) sum += sc.mass_left(l);
+                    else if (!(l >= above)) put(l, some.at[i]);
+                }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
                 __builtin_amdgcn_wave_barrier();
                 n = 0;
+                if (!sums) return;
                 sum = wave_total(sum);
                 if (lane == 0 && sum) atomicAdd((unsigned long long *)&s.tile_mass[tile_of(c)], (unsigned long long)sum);
             });
@@ -439,30 +458,35 @@ struct Row {
 
     // Second half: within the bin, by histograms of the keys lo .. hi, the largest first, in ever smaller ranges.
     __device__ __forceinline__ Border border_in(bool mass, int bin, Border above, uint64_t goal, uint64_t before) {
-        if (tid == 0) { s.key_lo = 0xffffffffu; s.key_hi = 0; }
-        __syncthreads();
-        uint32_t lo = 0xffffffffu, hi = 0;
-        of_bin(bin, [&](float l, int64_t) {
-            if (l > above.value) {
-                lo = min(lo, key_of(l));
-                hi = max(hi, key_of(l));
-            }
-        });
         const uint32_t above_key = key_of(above.value);
         const bool tied = mass && above.value > -INFINITY && sc.bin(above.value) == bin;
-        if (tied) {
-            lo = min(lo, above_key);
-            hi = max(hi, above_key);
-        }
-        if (lo <= hi) {
-            atomicMin(&s.key_lo, lo);
-            atomicMax(&s.key_hi, hi);
-        }
-        __syncthreads();
-        lo = uniform(s.key_lo);
-        hi = uniform(s.key_hi);
+        uint32_t lo = 0, hi = 0xffffffffu;
 #pragma unroll 1
-        while (lo < hi) {
+        while (true) {
+            // to the keys that are there: often a single one
+            uint32_t least = 0xffffffffu, most = 0;
+            of_bin(bin, [&](float l, int64_t) {
+                const uint32_t k = key_of(l);
+                if (l > above.value && k >= lo && k <= hi) {
+                    least = min(least, k);
+                    most = max(most, k);
+                }
+            });
+            if (tied && above_key >= lo && above_key <= hi) {
+                least = min(least, above_key);
+                most = max(most, above_key);
+            }
+            least = ~wave_max(~least);
+            most = wave_max(most);
+            if ((tid & 63) == 0) s.waves[0][tid >> 6] = (uint64_t)least << 32 | most;
+            __syncthreads();
+            const uint64_t other = s.waves[0][tid & (THREADS / 64 - 1)];
+            lo = uniform(~wave_max(~(uint32_t)(other >> 32)));
+            hi = uniform(wave_max((uint32_t)other));
+            if (lo >= hi) {
+                __syncthreads();
+                break;
+            }
             const int shift = 31 - __builtin_clz((hi - lo) >> 10 | 1u);   // ((hi - lo) >> shift) < 2048
             clear();
             of_bin(bin, [&](float l, int64_t) {
@@ -535,13 +559,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
         __syncthreads();
         if (lane == 0) s.waves[0][wave] = (uint64_t)any << 32 | __float_as_uint(most);
         __syncthreads();
-        any = false;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) {
-            any |= (s.waves[0][w] >> 32) != 0;
-            most = fmaxf(most, __uint_as_float((uint32_t)s.waves[0][w]));
-        }
-        most = uniform(most);
+        const uint64_t other = s.waves[0][lane & (THREADS / 64 - 1)];
+        any = __builtin_amdgcn_ballot_w64((other >> 32) != 0) != 0;
+        most = wave_largest(__uint_as_float((uint32_t)other));
     };
     bool ready = !few && (has_k || has_p), odd = false;
     if (ready) {                     // a histogram at once, from the largest of the first logits plus some room on
@@ -563,14 +583,17 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
 #pragma unroll
         for (int i = 0; i < kMaxima; ++i) {
             own[i] = fmaxf(own[i], v[i]);
-            odd |= v[i] != v[i];
+            if (i & 1) odd |= __builtin_isunordered(v[i - 1], v[i]);
         }
     };
     if (ready && has_k)
         walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
             largest(v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) atomicAdd((unsigned long long *)&s.sums[r.sc.bin_below(v[i])], 1ull);
+            for (int i = 0; i < 4; ++i) {
+                const int b = r.sc.bin_below(v[i]);
+                if (b < kZeroBin) atomicAdd((unsigned long long *)&s.sums[b], 1ull);
+            }
         });
     else if (ready)
         walk<T, THREADS, 4>(logits, V, [&](int64_t, auto v) {
@@ -578,7 +601,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int b = r.sc.bin_below(v[i]);
-                atomicAdd((unsigned long long *)&s.sums[b], (unsigned long long)r.sc.mass_in_bin(v[i], b));
+                if (b < kZeroBin) atomicAdd((unsigned long long *)&s.sums[b], (unsigned long long)r.sc.mass_in_bin(v[i], b));   // (many masked words would meet there)
             }
         });
     else
