@@ -337,13 +337,23 @@ struct Row {
         __syncthreads();
         const float least = least_of_bin(last);
         walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
-            bool hit[4];
+            uint64_t hit[4], any = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) hit[i] = v[i] >= least;
-            if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
+            for (int i = 0; i < 4; ++i) any |= hit[i] = __builtin_amdgcn_ballot_w64(v[i] >= least);
+            if (!any) return;
+            uint32_t at = 0, n = 0;      // one place for all of the wavefront's
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (hit[i]) put(v[i], c + i);
+            for (int i = 0; i < 4; ++i) n += (uint32_t)__builtin_popcountll(hit[i]);
+            if ((tid & 63) == 0) at = atomicAdd(&s.listed, n);
+            at = uniform(at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit[i], at));
+                if (v[i] >= least && to < (uint32_t)kList<THREADS>) {
+                    s.list[to] = v[i];
+                    s.at[to] = (uint32_t)(c + i);
+                }
+                at += (uint32_t)__builtin_popcountll(hit[i]);
             }
         });
         __syncthreads();
