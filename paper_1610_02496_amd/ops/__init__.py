@@ -9,7 +9,8 @@
 
 The work is done by the HIP kernels behind the C ABI of ``include/saber_ops.h``; torch supplies memory, streams and
 the graph of gradients.  Everything is enqueued on torch's current stream of the tensors' device: nothing is waited
-for, and calls may be captured into a graph.  Arguments are checked on the host (ValueError, TypeError, or SaberError
+for, and calls may be captured into a graph (a backward pass by autograd as any of torch's: while no graph of gradients
+that was made outside of the capture is alive on the same leaves; the passes themselves always).  Arguments are checked on the host (ValueError, TypeError, or SaberError
 from the library).  There is no CPU fallback.
 
 A program that uses the sampler as well imports torch before it: the library then runs on torch's HIP runtime.  Loaded
@@ -19,6 +20,7 @@ raises ImportError.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import torch
@@ -570,7 +572,7 @@ def linear8(x, weight, dtype=None):
 def _limit(name, value, lead, device, types):
     """(tensor with a value per row, or None; number for all rows) of a limit."""
     if not isinstance(value, torch.Tensor):
-        return None, value
+        return None, float(value) if types[0] is _F32 else min(operator.index(value), 1 << 62)
     _device(value, name, device)
     if value.dtype not in types:
         raise TypeError("%s must be %s, not %s" % (name, " or ".join(str(t)[6:] for t in types), value.dtype))

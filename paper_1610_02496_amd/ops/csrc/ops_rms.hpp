@@ -81,10 +81,14 @@ __device__ __forceinline__ void row_join(float &sum, uint32_t &top, float *lds, 
     }
 }
 
-// 1 / sqrt(ss / H + eps).  A sum of squares beyond binary32 is taken again of 2^-80 s, next to which eps is nothing.
-constexpr float kDown = 0x1p-80f;
+// 1 / sqrt(ss / H + eps).  A sum of squares beyond binary32 is taken again of 2^-80 s, next to which eps is nothing; one below 2^-100, where
+// squares are no normal numbers, of 2^90 s, unless eps is more than that.  (Without eps a row of zeros has the largest finite r, and stays zeros.)
 __device__ __forceinline__ float rstd_of(float ss, float inv, float eps) { return 1.f / sqrtf(ss * inv + eps); }
-__device__ __forceinline__ float rstd_of_large(float ss, float inv) { return kDown / sqrtf(ss * inv); }
+__device__ __forceinline__ float scale_of_sum(float ss, float eps) { return !(ss < INFINITY) ? 0x1p-80f : ss < 0x1p-100f && eps < 0x1p-100f ? 0x1p90f : 0.f; }
+__device__ __forceinline__ float rstd_of_scaled(float ss, float inv, float eps, float by) {
+    if (by < 1.f) return by / sqrtf(ss * inv);
+    return fminf(by / sqrtf(ss * inv + eps * by * by), 0x1.fffffep127f);
+}
 
 template <int TPR> constexpr int kRmsThreads = TPR > 256 ? TPR : 256;   // of a workgroup
 
@@ -136,14 +140,14 @@ __global__ __launch_bounds__(kRmsThreads<TPR>) void rms_forward_kernel(RmsForwar
         }
         row_join<TPR, HELD8>(ss, top, lds, slot);
         float rstd = rstd_of(ss, inv, a.eps);
-        if (!(ss < INFINITY)) {
+        if (const float by = scale_of_sum(ss, a.eps); by != 0.f) {
             ss = 0.f;
 #pragma unroll
             for (int j = 0; j < NC; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i] * kDown, v[j][i] * kDown, ss);
+                for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i] * by, v[j][i] * by, ss);
             ss = row_sum<TPR>(ss, lds + 4 * (TPR / 64), 0);
-            rstd = rstd_of_large(ss, inv);
+            rstd = rstd_of_scaled(ss, inv, a.eps, by);
         }
         if constexpr (HELD8) {
             const float step = step_of(top);
@@ -314,15 +318,15 @@ __global__ __launch_bounds__(1024) void rms_forward_wide_kernel(RmsForward a) {
         row_join<1024, HELD8>(ss, top, lds, slot);
         auto again = [&](int64_t c) { return a.res ? load8(static_cast<const R *>(sum) + c, H - c) : load8(x + c, H - c); };
         float rstd = rstd_of(ss, inv, a.eps);
-        if (!(ss < INFINITY)) {
+        if (const float by = scale_of_sum(ss, a.eps); by != 0.f) {
             ss = 0.f;
             for (int64_t c = (int64_t)threadIdx.x * 8; c < H; c += 8192) {
                 const f32x8 v = again(c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(v[i] * kDown, v[i] * kDown, ss);
+                for (int i = 0; i < 8; ++i) ss = fmaf(v[i] * by, v[i] * by, ss);
             }
             ss = row_sum<1024>(ss, lds + 4 * 16, 0);
-            rstd = rstd_of_large(ss, inv);
+            rstd = rstd_of_scaled(ss, inv, a.eps, by);
         }
         const float step = HELD8 ? step_of(top) : 0.f;
         for (int64_t c = (int64_t)threadIdx.x * 8; c < (HELD8 ? (H + 15) / 16 * 16 : H); c += 8192) {
