@@ -318,12 +318,12 @@ struct Row {
         uint32_t lo = key_of(-INFINITY), hi = key_of(sc.top);
 #pragma unroll 1
         while (lo < hi) {
-            const uint32_t step = (hi - lo) / 64 + 1, at = (uint32_t)(tid & 63) * step;
-            const uint64_t yes = __builtin_amdgcn_ballot_w64(at <= hi - lo && holds(of_key(lo + at)));
+            const uint32_t step = (hi - lo) / 64 + 1;
+            const uint64_t yes = __builtin_amdgcn_ballot_w64(holds(of_key(lo + min((uint32_t)(tid & 63) * step, hi - lo))));   // (that of hi holds)
             const uint32_t first = yes ? (uint32_t)__builtin_ctzll(yes) : 64u;   // (64: beyond the last one tried)
             const uint32_t from = first ? lo + (first - 1) * step + 1 : lo;
-            if (yes) hi = lo + first * step;
-            lo = from < hi ? from : hi;
+            if (yes) hi = lo + min(first * step, hi - lo);
+            lo = from;
         }
         return of_key(hi);
     }
