@@ -411,7 +411,7 @@ struct Row {
             walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool is = v[i] >= from && (sums || !(v[i] >= above));
+                    const bool is = v[i] >= from;
                     const uint64_t all = __builtin_amdgcn_ballot_w64(is);
                     if (is) {
                         const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, n));
