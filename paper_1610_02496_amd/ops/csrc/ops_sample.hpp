@@ -331,29 +331,40 @@ struct Row {
         return least_of([&](float l) { return sc.bin(l) <= bin; });
     }
 
+    // Four logits of a lane that are not below `from`, after the n that the wavefront has put side by side already.
+    template <class S, class V>
+    __device__ __forceinline__ void side_by_side(S &some, uint32_t &n, int64_t c, V v, float from) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool is = v[i] >= from;
+            const uint64_t all = __builtin_amdgcn_ballot_w64(is);
+            if (is) {
+                const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, n));
+                some.l[to] = v[i];
+                some.at[to] = (uint32_t)c + i;
+            }
+            n += (uint32_t)__builtin_popcountll(all);
+        }
+    }
+    // the wavefront's lanes see what they wrote to LDS
+    __device__ __forceinline__ void wave_lds_fence() const {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+    }
+
     // Lists all logits of the bins up to `last`, which is before kZeroBin; false if they are too many.
     __device__ __forceinline__ bool list_upto(int last) {
         if (tid == 0) s.listed = 0;
         __syncthreads();
         const float least = least_of_bin(last);
-        walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
-            uint64_t hit[4], any = 0;
+        walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {   // (few: each takes its place by itself)
+            bool hit[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) any |= hit[i] = __builtin_amdgcn_ballot_w64(v[i] >= least);
-            if (!any) return;
-            uint32_t at = 0, n = 0;      // one place for all of the wavefront's
+            for (int i = 0; i < 4; ++i) hit[i] = v[i] >= least;
+            if (__builtin_amdgcn_ballot_w64(hit[0] | hit[1] | hit[2] | hit[3])) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) n += (uint32_t)__builtin_popcountll(hit[i]);
-            if ((tid & 63) == 0) at = atomicAdd(&s.listed, n);
-            at = uniform(at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(hit[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit[i], at));
-                if (v[i] >= least && to < (uint32_t)kList<THREADS>) {
-                    s.list[to] = v[i];
-                    s.at[to] = (uint32_t)(c + i);
-                }
-                at += (uint32_t)__builtin_popcountll(hit[i]);
+                for (int i = 0; i < 4; ++i)
+                    if (hit[i]) put(v[i], c + i);
             }
         });
         __syncthreads();
@@ -408,22 +419,9 @@ struct Row {
             if (sums && sc.least > -INFINITY && above == above) left = fmaxf(above, least_of([&](float l) { return sc.down(l) >= sc.least; }));
             const float from = bin < kZeroBin ? least_of_bin(bin) : left;
             uint32_t n = 0;
-            walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool is = v[i] >= from;
-                    const uint64_t all = __builtin_amdgcn_ballot_w64(is);
-                    if (is) {
-                        const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, n));
-                        some.l[to] = v[i];
-                        some.at[to] = (uint32_t)c + i;
-                    }
-                    n += (uint32_t)__builtin_popcountll(all);
-                }
-            }, [&](int64_t c) {
+            walk<T, THREADS, 4>(row, words, [&](int64_t c, auto v) { side_by_side(some, n, c, v, from); }, [&](int64_t c) {
                 if (!n) return;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-                __builtin_amdgcn_wave_barrier();
+                wave_lds_fence();
                 uint64_t sum = 0;
 #pragma unroll 1
                 for (uint32_t i = lane; i < n; i += 64) {
@@ -431,8 +429,7 @@ struct Row {
                     if (l >= left) sum += sc.mass_left(l);
                     else if (!(l >= above)) put(l, some.at[i]);
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-                __builtin_amdgcn_wave_barrier();
+                wave_lds_fence();
                 n = 0;
                 if (!sums) return;
                 sum = wave_total(sum);
