@@ -271,6 +271,10 @@ extern "C" int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_s
 namespace {
 constexpr int kFewTiles = 16, kManyTiles = 512;   // of 512 words or more
 constexpr int64_t kMostRows = (int64_t)1 << 21;    // of a launch (of fewer than 2^32 threads)
+// Threads of a workgroup: 256 for many short rows, of which a CU then holds four; 1,024 where there is a CU for every row and the row is long; else
+// 512.  Measured in us with top_p 0.95: 250 rows of 1000 20.0 (256), 19.6 (512); of 8000 in binary32 25.4, 22.3; of 10,000 22.7 (512), 22.5 (1024); 61
+// of 30,011 30.5, 28.5; 250 of 100,000 62.6, 53.5; 300 of 100,000 118, 148; 2048 of 141,000 in binary32 690, 867 (before the loop over rows was gone).
+constexpr int64_t kFewWords = 20000;
 }
 
 extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, int64_t words, int dtype, const float *u, const float *temperatures,
@@ -303,9 +307,9 @@ extern "C" int saber_sample(const void *logits, int64_t stride, int64_t rows, in
         using T = decltype(e);
         for (; a.first_row < rows; a.first_row += kMostRows) {
             const unsigned grid = (unsigned)(rows - a.first_row < kMostRows ? rows - a.first_row : kMostRows);
-            if (words <= 512 * kFewTiles) sample_kernel<T, 256, kFewTiles><<<grid, 256, 0, st>>>(a);
-            else if (rows <= kCus) sample_kernel<T, 1024, kManyTiles><<<grid, 1024, 0, st>>>(a);
-            else sample_kernel<T, 512, kManyTiles><<<grid, 512, 0, st>>>(a);
+            if (rows > kCus && words <= 512 * kFewTiles) sample_kernel<T, 256, kFewTiles><<<grid, 256, 0, st>>>(a);
+            else if (rows > kCus || words <= kFewWords) sample_kernel<T, 512, kManyTiles><<<grid, 512, 0, st>>>(a);
+            else sample_kernel<T, 1024, kManyTiles><<<grid, 1024, 0, st>>>(a);
             OPS_HIP(hipGetLastError());
         }
         return SABER_OK;
