@@ -14,29 +14,38 @@ namespace {
 
 // ---- root-mean-square norm ---------------------------------------------------------------------------------------------------
 
-// Rows of up to 1,024 columns belong to a wavefront, up to 4,096 to a workgroup of 256, up to 8,192 to one of 512; wider ones are read again.
+// Rows of up to 1,024 columns belong to a wavefront, up to 4,096 to a workgroup of 256, up to 8,192 to one of 512; wider ones are read again.  Rows of up
+// to 2,048 belong to a wavefront as well (32 elements a lane), which needs no barrier, where the result is in 8 bits and where there are enough rows to
+// keep the CUs busy with fewer of them.  us with a wavefront and a workgroup: 65,536 x 2048 in bf16, stream in binary32, forward 295 and 309, backward
+// 407 and 432, in 8 bits 270 and 288; rows in 8 bits of 65,536 x 2048 85 and 140, of 5000 10.3 and 13.4; but 9000 x 1100 forward 21.1 and 19.3,
+// backward 44.5 and 30.8, and 32,768 x 1500 in binary32 forward 161 and 167, backward 156 and 153.  16,384 x 1024 in bf16 forward 21.5 and 23.7, in 8 bits
+// 21.5 and 42.5.
 constexpr int64_t kRmsCols = 8192;
+constexpr int64_t kManyRows = 16384, kManyValues = (int64_t)1 << 27;   // from which on a wavefront's rows have up to 2,048 columns, forward and backward
 
 template <class F>
-int with_rms_shape(int64_t cols, F &&f) {
-    using C1 = std::integral_constant<int, 1>; using C2 = std::integral_constant<int, 2>;
+int with_rms_shape(int64_t cols, bool wavefront, F &&f) {
+    using C1 = std::integral_constant<int, 1>; using C2 = std::integral_constant<int, 2>; using C4 = std::integral_constant<int, 4>;
     using W = std::integral_constant<int, 64>; using G = std::integral_constant<int, 256>; using GG = std::integral_constant<int, 512>;
     if (cols <= 512) return f(W{}, C1{});
     if (cols <= 1024) return f(W{}, C2{});
-    if (cols <= 2048) return f(G{}, C1{});
+    if (cols <= 2048) return wavefront ? f(W{}, C4{}) : f(G{}, C1{});
     if (cols <= 4096) return f(G{}, C2{});
     return f(GG{}, C2{});
 }
-int64_t rows_per_group(int64_t cols) { return cols <= 1024 ? 4 : 1; }
-unsigned rms_grid(int64_t rows, int64_t cols) {
-    const int64_t groups = parts_of(rows, rows_per_group(cols));
+// workgroups for the rows that a workgroup has at a time: four if they belong to wavefronts
+unsigned rms_grid(int64_t rows, int tpr) {
+    const int64_t groups = parts_of(rows, tpr == 64 ? 4 : 1);
     return (unsigned)(groups < 8 * kCus ? groups : 8 * kCus);
 }
 unsigned wide_grid(int64_t rows) { return (unsigned)(rows < 64 * kCus ? rows : 64 * kCus); }
+bool rms_backward_wavefront(int64_t rows, int64_t cols) { return cols <= 1024 || (cols <= 2048 && rows * cols >= kManyValues); }
 // workgroups of the backward pass, as many as the CUs hold at a time: each leaves a partial row
 int64_t rms_parts(int64_t rows, int64_t cols) {
     if (cols > kRmsCols) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
-    const int64_t groups = parts_of(rows > 0 ? rows : 1, rows_per_group(cols)), most = (cols <= 1024 ? 3 : cols <= 4096 ? 4 : 2) * kCus;
+    const bool wavefront = rms_backward_wavefront(rows, cols);
+    const int64_t groups = parts_of(rows > 0 ? rows : 1, wavefront ? 4 : 1);
+    const int64_t most = (cols <= 1024 ? 3 : wavefront || cols > 4096 ? 2 : 4) * kCus;
     return groups < most ? groups : most;
 }
 
@@ -101,9 +110,9 @@ extern "C" int saber_rms_norm_forward(const void *x, int64_t x_stride, const voi
             if (q) rms_forward_wide_kernel<T, R, true><<<wide_grid(rows), 1024, 0, st>>>(a);
             else rms_forward_wide_kernel<T, R, false><<<wide_grid(rows), 1024, 0, st>>>(a);
         } else
-            OPS_TRY(with_rms_shape(cols, [&](auto tpr, auto nc) -> int {
-                if (q) rms_forward_kernel<T, R, tpr.value, nc.value, true><<<rms_grid(rows, cols), kRmsThreads<tpr.value>, 0, st>>>(a);
-                else rms_forward_kernel<T, R, tpr.value, nc.value, false><<<rms_grid(rows, cols), kRmsThreads<tpr.value>, 0, st>>>(a);
+            OPS_TRY(with_rms_shape(cols, q || rows >= kManyRows, [&](auto tpr, auto nc) -> int {
+                if (q) rms_forward_kernel<T, R, tpr.value, nc.value, true><<<rms_grid(rows, tpr.value), kRmsThreads<tpr.value>, 0, st>>>(a);
+                else rms_forward_kernel<T, R, tpr.value, nc.value, false><<<rms_grid(rows, tpr.value), kRmsThreads<tpr.value>, 0, st>>>(a);
                 return SABER_OK;
             }));
         OPS_HIP(hipGetLastError());
@@ -157,7 +166,7 @@ extern "C" int saber_rms_norm_backward(const void *dy, int64_t dy_stride, const 
                 }
                 if (dweight) rms_columns_wide_kernel<T, R><<<dim3((unsigned)parts_of(cols, 2048), (unsigned)parts), 256, 0, st>>>(a);
             } else
-                OPS_TRY(with_rms_shape(cols, [&](auto tpr, auto nc) -> int {
+                OPS_TRY(with_rms_shape(cols, rms_backward_wavefront(rows, cols), [&](auto tpr, auto nc) -> int {
                     rms_backward_kernel<T, R, tpr.value, nc.value><<<(unsigned)parts, kRmsThreads<tpr.value>, 0, st>>>(a);
                     return SABER_OK;
                 }));
@@ -188,8 +197,8 @@ extern "C" int saber_rows8_save(const void *x, int64_t x_stride, int64_t rows, i
         using T = decltype(e);
         if (cols > kRmsCols) rows8_save_wide_kernel<T><<<wide_grid(rows), 1024, 0, st>>>(a);
         else
-            OPS_TRY(with_rms_shape(cols, [&](auto tpr, auto nc) -> int {
-                rows8_save_kernel<T, tpr.value, nc.value><<<rms_grid(rows, cols), kRmsThreads<tpr.value>, 0, st>>>(a);
+            OPS_TRY(with_rms_shape(cols, true, [&](auto tpr, auto nc) -> int {
+                rows8_save_kernel<T, tpr.value, nc.value><<<rms_grid(rows, tpr.value), kRmsThreads<tpr.value>, 0, st>>>(a);
                 return SABER_OK;
             }));
         OPS_HIP(hipGetLastError());

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_1610_02496_amd as pk
-from tests.test_gpu_answer import BF16, E, F16, F32, HALF, LIMITS, answer, check_draws, dev, make, natural, within
+from tests.test_gpu_answer import BF16, E, F16, F32, HALF, LIMITS, TINY, answer, check_draws, dev, make, natural, within
 
 pytestmark = pytest.mark.gpu
 
@@ -163,3 +163,39 @@ def test_logits_of_strided_features():
     words = pk.ops.Rows8.of(w8.q.t().contiguous().t(), wide.abs())
     assert torch.equal(pk.ops.linear8(x.t(), words), pk.ops.linear8(x.t(), pk.ops.Rows8.of(w8.q.contiguous(), wide.abs().contiguous())))
     assert HALF[F16] == 2.0 ** -11
+
+
+@pytest.mark.parametrize("rows,cols,dtype,rtype", [(16390, 1030, BF16, F32), (16385, 2048, F32, F32), (65540, 2048, BF16, F32), (65600, 2047, F16, F16)])
+def test_rms_norm_of_many_rows(rows, cols, dtype, rtype):
+    """So many rows that those of up to 2,048 columns belong to a wavefront; the reference in 64 bits on the device, some rows at a time."""
+    print("rms", rows, cols, dtype, rtype, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rand = lambda t, *s: torch.randn(*s, device="cuda", generator=g).to(t)  # noqa: E731
+    x, res, dy, dsum, w = rand(dtype, rows, cols), rand(rtype, rows, cols), rand(dtype, rows, cols), rand(rtype, rows, cols), 1 + 0.2 * rand(F32, cols)
+    y, saved = pk.ops.rms_norm_forward(x, w, res)
+    dx, dres, dw = pk.ops.rms_norm_backward(dy, saved, dsum)
+    rel, dw64, size = 30 * E, torch.zeros(cols, device="cuda", dtype=torch.float64), torch.zeros(cols, device="cuda", dtype=torch.float64)
+    for lo in range(0, rows, 8192):
+        part = slice(lo, min(rows, lo + 8192))
+        s = (x[part].float() + res[part].float()).to(rtype)
+        assert torch.equal(saved.x[part], s)
+        s = s.double()
+        r = 1 / (s.square().mean(1, keepdim=True) + 1e-6).sqrt()
+        h, gw = s * r, dy[part].double() * w.double()
+        y64 = h * w.double()
+        assert bool(((y[part].double() - y64).abs() <= HALF[dtype] * y64.abs() + TINY[dtype] + rel * y64.abs() * (1 + HALF[dtype])).all())
+        mean = (gw * h).mean(1, keepdim=True)
+        d = r * (gw - h * mean) + dsum[part].double()
+        err = rel * r * (gw.abs() + h.abs() * mean.abs()) + r * h.abs() * 50 * E * 3 * (gw * h).abs().mean(1, keepdim=True) + 2 * E * (d.abs() + dsum[part].double().abs())
+        assert bool(((dx[part].double() - d).abs() <= HALF[dtype] * d.abs() + TINY[dtype] + err * (1 + HALF[dtype])).all())
+        assert bool(((dres[part].double() - d).abs() <= HALF[rtype] * d.abs() + TINY[rtype] + err * (1 + HALF[rtype])).all())
+        dw64 += (dy[part].double() * h).sum(0)
+        size += (dy[part].double() * h).abs().sum(0)
+    # a lane adds up the rows of its wavefront (a workgroup: of 2,048 wavefronts; else of 768 or 1,024 workgroups), the rest is joined in some 100 additions
+    lines = rows / 768 + 100
+    assert bool(((dw.double() - dw64).abs() <= HALF[F32] * dw64.abs() + (lines + 40) * E * size).all())
+    c, total = pk.ops.rms_norm8(x, w, res)
+    assert torch.equal(total, saved.x)
+    s = saved.x[-100:].float() * w
+    step = (s.double().abs().amax(1, keepdim=True) / 127).float().double()
+    assert torch.equal(c.q[-100:].double(), (s.double() / step).round().clamp(-127, 127))
