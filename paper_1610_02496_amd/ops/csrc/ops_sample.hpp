@@ -583,7 +583,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
         for (int i = 0; i < 8; ++i) first = fmaxf(first, c + i < V ? v[i] : -INFINITY);
         join(first, odd);
         r.sc.edge = uniform(first + kRoom * temperature);
-        ready = fabsf(r.sc.edge) < INFINITY;
+        // (its masses are of bins of 1/32 of z: not where 32 / T is no number of binary32 and `per` is less)
+        ready = fabsf(r.sc.edge) < INFINITY && kBinsPerUnit / temperature < INFINITY;
         r.clear();
     }
     float own[kMaxima];
