@@ -75,8 +75,11 @@ __device__ __forceinline__ double exp2_in_bin(double r) {
 
 // The logits of a row relative to its largest.
 struct Scale {
-    float top, per;      // largest logit; bins per unit of a logit
+    float top, per;      // largest logit; bins per unit of a logit times `unit`
     float edge;          // where the first bin begins: at the largest logit or above it
+    // 1, and 1/2 from T of 2^122 on: there a word may have mass whose logit is further from the largest than binary32 reaches, so both are halved
+    // before they are subtracted (below, such a difference is 2046 bins or more)
+    float unit;
     double log2_per;     // log2(e) / T
     double least;        // least difference that min_p leaves
     double up;           // 2^S
@@ -84,10 +87,10 @@ struct Scale {
     // (of two infinities too)
     __device__ __forceinline__ double down(float l) const { return l == top ? 0.0 : (double)l - (double)top; }
     __device__ __forceinline__ int bin(float l) const {   // rises as the logit falls, by steps of 1/32 of z
-        const float b = l == edge ? 0.f : (edge - l) * per;
+        const float b = l == edge ? 0.f : fmaf(l, -unit, edge * unit) * per;
         return b < (float)kZeroBin ? (int)b : kZeroBin;   // (NaN, of -inf and T = inf, as well)
     }
-    // the same for a finite edge, and 0 above it; and e^z relative to the middle of that bin, in multiples of 1 / bin_up
+    // the same for a finite edge and a unit of 1, and 0 above the edge; and e^z relative to the middle of that bin, in multiples of 1 / bin_up
     __device__ __forceinline__ int bin_below(float l) const { return (int)__builtin_amdgcn_fmed3f((edge - l) * per, 0.f, (float)kZeroBin); }
     __device__ __forceinline__ uint64_t mass_in_bin(float l, int b) const {
         const double r = fma((double)l - (double)edge, log2_per, times_plus((double)b, kBinLog2, kBinLog2 / 2));
@@ -557,7 +560,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
     const bool greedy = !(temperature > 0.f), has_k = !greedy && top_k > 0 && top_k < V, has_p = !greedy && top_p < 1.f;
     const bool few = has_k && top_k <= kMaxima * THREADS / 2;
     Scale sc;
-    sc.per = uniform(fminf(kBinsPerUnit / temperature, 0x1.fffffep127f));
+    sc.unit = uniform(temperature > 0x1p122f ? 0.5f : 1.f);
+    sc.per = uniform(fminf(kBinsPerUnit / temperature, 0x1.fffffep127f) / sc.unit);
     sc.log2_per = uniform(1.44269504088896340736 / (double)temperature);
     sc.up = (double)((uint64_t)1 << a.mass_log);
     sc.bin_up = (double)((uint64_t)1 << (a.mass_log < 40 ? a.mass_log : 40));
@@ -583,8 +587,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
         for (int i = 0; i < 8; ++i) first = fmaxf(first, c + i < V ? v[i] : -INFINITY);
         join(first, odd);
         r.sc.edge = uniform(first + kRoom * temperature);
-        // (its masses are of bins of 1/32 of z: not where 32 / T is no number of binary32 and `per` is less)
-        ready = fabsf(r.sc.edge) < INFINITY && kBinsPerUnit / temperature < INFINITY;
+        // (its masses are of bins of 1/32 of z: not where 32 / T is no number of binary32 and `per` is less; its differences are not halved)
+        ready = fabsf(r.sc.edge) < INFINITY && kBinsPerUnit / temperature < INFINITY && r.sc.unit == 1.f;
         r.clear();
     }
     float own[kMaxima];
