@@ -1,10 +1,12 @@
-"""The operators of a head that answers in the corners of what they accept: temperatures and logits at the ends of binary32."""
+"""The operators of a head that answers in the corners of what they accept: temperatures and logits at the ends of binary32, shares that
+fall on a border of whole masses."""
 import math
 
 import pytest
 import torch
 
-from tests.test_gpu_answer import F32, check_draws, natural
+import paper_1610_02496_amd as pk
+from tests.test_gpu_answer import E, F32, check_draws, dev, natural
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +50,41 @@ def test_sample_differences_beyond_binary32(words, temperature):
     half = int(upper.sum())
     for limits in ({}, {"top_p": 0.999}, {"top_p": 0.6}, {"top_k": half + 70}, {"top_k": half + 70, "top_p": 0.9}, {"top_k": 4000, "top_p": 0.99}, {"min_p": 1e-4}):
         check_draws(l, u, temperature=temperature, **limits)
+
+
+# ---- a share of the whole, where it falls on a border -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("words,deep", [(100000, -31.95), (131072, -31.9), ((1 << 22) + 5, -27.9)])
+def test_sample_share_of_whole_masses(words, deep):
+    """Two words that share all of the mass: half of it is the first one's.  The others are too deep to have a mass (they round to none), but
+    there are so many of them that what is left out would move the border.  Wherever the two are, and at every temperature."""
+    print("sample", words, deep, flush=True)
+    places = [(3, 900), (5, words - 2), (words - 9, words - 5), (words // 2, words // 2 + 1)]
+    l = torch.full((len(places), words), deep)
+    for i, at in enumerate(places):
+        l[i, list(at)] = 0.0
+    for temperature in (1.0, 0.25, 8.0):
+        for u, share, which, p in ((0.75, 0.5, 0, 1.0), (0.75, 0.501, 1, 0.5), (0.25, 0.501, 0, 0.5), (0.999, 0.0, 0, 1.0)):
+            word, got = pk.ops.sample(dev(l * temperature), torch.full((len(places),), u, device="cuda"), temperature=temperature, top_p=share)
+            assert word.tolist() == [at[which] for at in places], (temperature, u, share)
+            assert bool((got - p).abs().max() <= 2 * E)
+
+
+@pytest.mark.parametrize("words", [64, 1024, 8192, 65536])
+def test_sample_share_of_equal_logits(words):
+    """Of n equal words an exact share of n are left, at any temperature and magnitude: p is 1 / (share n)."""
+    shares = [0.5, 0.75, 0.875, 0.9375, 0.96875, 0.984375]
+    rows = 400 * len(shares)
+    print("sample", words, rows, flush=True)
+    g = torch.Generator().manual_seed(words)
+    temperature = torch.exp(torch.rand(rows, generator=g) * 8 - 4)
+    top_p = torch.tensor(shares).repeat(400)
+    level = torch.randn(rows, 1, generator=g) * 3
+    for some in range(0, rows, 600):
+        part = slice(some, some + 600)
+        word, p = pk.ops.sample(dev(level[part]).repeat(1, words), torch.full((600,), 1 - 2.0 ** -24, device="cuda"), temperature=dev(temperature[part]), top_p=dev(top_p[part]))
+        left = (top_p[part] * words).to(torch.int64)
+        last = torch.floor((1 - 2.0 ** -24) * left.double()).to(torch.int64)
+        bad = (word.cpu() != last).nonzero()[:, 0]
+        assert not len(bad), (len(bad), word.cpu()[bad][:5], last[bad][:5], temperature[part][bad][:5], top_p[part][bad][:5])
+        assert bool((p.cpu().double() * left - 1).abs().max() <= 2 * E)
