@@ -283,10 +283,10 @@ struct Row {
         if (tid == 0) s.found[0] = kBins;
         const uint64_t upto = scan(0, sum, total);
         if (of_whole) {
-            const double want = (share - 0x1p-40) * (double)total;
+            const double want = fmax((share - 0x1p-40) * (double)total, 1.0);   // (a share of 0: one word's, the likeliest)
             goal = (uint64_t)want;
             goal += (double)goal < want;
-            goal = uniform(goal < 1 ? 1 : goal > total ? total : goal);
+            goal = uniform(goal > total ? total : goal);
             if (tid == 0) s.found[2] = total;
         }
         uint64_t at = before + upto - sum;

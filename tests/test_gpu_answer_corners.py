@@ -88,3 +88,16 @@ def test_sample_share_of_equal_logits(words):
         bad = (word.cpu() != last).nonzero()[:, 0]
         assert not len(bad), (len(bad), word.cpu()[bad][:5], last[bad][:5], temperature[part][bad][:5], top_p[part][bad][:5])
         assert bool((p.cpu().double() * left - 1).abs().max() <= 2 * E)
+
+
+@pytest.mark.parametrize("equal", [2, 4096])
+def test_sample_no_share_of_very_many_words(equal):
+    """top_p of 0, and less than the 2^-40 that a share may lack, leave the likeliest word; where masses are as coarse as they get, too."""
+    words = (1 << 30) + 8
+    l = torch.full((1, words), -math.inf, dtype=torch.bfloat16, device="cuda")
+    at = [5 + i * (words // equal) for i in range(equal)]
+    l[0, torch.tensor(at, device="cuda")] = 2.0
+    for share, left in ((0.0, 1), (1e-13, 1), (0.5, equal // 2), (0.75, (3 * equal + 3) // 4)):
+        print("sample", words, equal, share, flush=True)
+        word, p = pk.ops.sample(l, torch.tensor([0.999], device="cuda"), top_p=share)
+        assert int(word) == at[int(0.999 * left)] and abs(float(p) * left - 1) <= 2 * E, share
