@@ -1,12 +1,12 @@
 """The operators of a head that answers in the corners of what they accept: temperatures and logits at the ends of binary32, shares that
-fall on a border of whole masses."""
+fall on a border of whole masses, one tensor as both inputs of a norm."""
 import math
 
 import pytest
 import torch
 
 import paper_1610_02496_amd as pk
-from tests.test_gpu_answer import E, F32, check_draws, dev, natural
+from tests.test_gpu_answer import BF16, E, F16, F32, HALF, TINY, check_draws, dev, make, natural, within
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,29 @@ def test_sample_no_share_of_very_many_words(equal):
         print("sample", words, equal, share, flush=True)
         word, p = pk.ops.sample(l, torch.tensor([0.999], device="cuda"), top_p=share)
         assert int(word) == at[int(0.999 * left)] and abs(float(p) * left - 1) <= 2 * E, share
+
+
+# ---- one tensor as both inputs of a norm ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(10, 64), (33, 1000), (5, 2500), (3, 9000)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_rms_norm_gradient_of_one_tensor_as_both(rows, cols, dtype):
+    """x as features and as residual: twice the gradient of the sum, of a loss in which half of it, none, or one of the other sign is far off."""
+    print("rms", rows, cols, dtype, flush=True)
+    x, a, b = (make(i, rows, cols, dtype=dtype) for i in (4, 5, 6))
+    leaf = dev(x).requires_grad_()
+    y, s = pk.ops.rms_norm(leaf, None, leaf)
+    ((y * dev(a)).float().sum() + (s * dev(b)).float().sum()).backward()
+    t = 2 * x.double()
+    r = 1 / (t.square().mean(1, keepdim=True) + 1e-6).sqrt()
+    h, g = t * r, a.double()
+    mgh = (g * h).mean(1, keepdim=True)
+    ds = r * (g - h * mgh) + b.double()
+    # as in test_rms_norm_both_passes: h by rel, the mean by its additions and h's error in each term, then three roundings each; both gradients are
+    # rounded to the type and their sum, of equal numbers, is not
+    adds = 40.0 + cols / 1024
+    rel = (adds / 2 + 4) * E
+    err = (rel + 4 * E) * r * (g.abs() + h.abs() * mgh.abs()) + r * h.abs() * (adds + 4) * E * 3 * (g * h).abs().mean(1, keepdim=True) + 2 * E * (ds.abs() + b.double().abs())
+    bound = 2 * (HALF[dtype] * ds.abs() + TINY[dtype] + err * (1 + HALF[dtype]))
+    assert bool((bound < 0.1 * ds.abs().mean()).all())
+    within(leaf.grad, 2 * ds, bound, "gradient of both")
