@@ -572,7 +572,8 @@ def linear8(x, weight, dtype=None):
 def _limit(name, value, lead, device, types):
     """(tensor with a value per row, or None; number for all rows) of a limit."""
     if not isinstance(value, torch.Tensor):
-        return None, float(value) if types[0] is _F32 else min(operator.index(value), 1 << 62)
+        # (a whole number of any size: what ctypes does not hold it would wrap)
+        return None, float(value) if types[0] is _F32 else max(-1, min(operator.index(value), 1 << 62))
     _device(value, name, device)
     if value.dtype not in types:
         raise TypeError("%s must be %s, not %s" % (name, " or ".join(str(t)[6:] for t in types), value.dtype))
