@@ -24,6 +24,7 @@ import operator
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 from ..binding import SABER_OK, SaberError, load_library
 
@@ -521,7 +522,7 @@ def _empty_rows8(x, rows, cols):
 
 
 def rows8(x) -> Rows8:
-    """``x`` (any shape, rows run along its last dimension) in 8 bits, one step per row."""
+    """``x`` (any shape, rows run along its last dimension) in 8 bits, one step per row: its values, no gradient goes back to it."""
     device = _device(x, "x")
     code = _type("x", x)
     m, rows, cols, stride = _rows(x, "x")
@@ -533,6 +534,8 @@ def rows8(x) -> Rows8:
 def _no_gradient(call, *tensors):
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         raise ValueError("%s has no gradient: call it under torch.no_grad(), or on detached tensors" % call)
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("%s has no derivative in forward mode either: call it on detached tensors" % call)
 
 
 def rms_norm8(x, weight=None, residual=None, eps=1e-6):
@@ -588,8 +591,10 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     by their number, these are left: the first ``top_k`` (0: all), of them the fewest that hold ``top_p`` of their mass, of them those of
     exp(z) >= ``min_p``.  The word is the first one, by number, at which the mass of the words left exceeds ``u`` of all of it; ``p`` is its
     share of that mass.  Temperature 0 takes the first of the largest.  Every limit is a number, or a tensor with one value per row.
-    Words of logit -inf take no part; a row of which nothing is left gives -1 and 0, one with a NaN -1 and NaN."""
+    Words of logit -inf take no part; a row of which nothing is left gives -1 and 0, one with a NaN -1 and NaN.  Without gradients:
+    ``p`` has none, so logits and temperatures that ask for one are refused."""
     device = _device(logits, "logits")
+    _no_gradient("sample", logits, temperature if isinstance(temperature, torch.Tensor) else None)
     code = _type("logits", logits)
     m, rows, words, stride = _rows(logits, "logits")
     if not words:

@@ -1,5 +1,6 @@
 """The operators of a head that answers in the corners of what they accept: temperatures and logits at the ends of binary32, shares that
-fall on a border of whole masses, one tensor as both inputs of a norm."""
+fall on a border of whole masses, one tensor as both inputs of a norm, gradients that a call does
+not have."""
 import math
 
 import pytest
@@ -127,3 +128,37 @@ def test_rms_norm_gradient_of_one_tensor_as_both(rows, cols, dtype):
     bound = 2 * (HALF[dtype] * ds.abs() + TINY[dtype] + err * (1 + HALF[dtype]))
     assert bool((bound < 0.1 * ds.abs().mean()).all())
     within(leaf.grad, 2 * ds, bound, "gradient of both")
+
+
+# ---- gradients that a call does not have -----------------------------------------------------------------------------------------
+
+def test_calls_without_gradients_refuse_to_lose_one():
+    """Logits, temperatures and features that ask for a gradient, or that carry one of forward mode."""
+    ops, x, w8 = pk.ops, dev(make(1, 4, 64)), pk.ops.rows8(dev(make(2, 100, 64)))
+    l, u, t = ops.linear8(x, w8), torch.rand(4, device="cuda"), torch.full((4,), 0.7, device="cuda")
+    want = ops.sample(l, u, temperature=t, top_p=0.9)
+    asks = lambda a: a.clone().requires_grad_()  # noqa: E731
+    calls = [lambda f: ops.sample(f(l), u, temperature=t, top_p=0.9), lambda f: ops.sample(l, u, temperature=f(t)), lambda f: ops.linear8(f(x), w8),
+             lambda f: ops.rms_norm8(f(x)), lambda f: ops.rms_norm8(x, residual=f(x)), lambda f: ops.rms_norm8(x, f(x[0]))]
+    for call in calls:
+        with pytest.raises(ValueError, match="no gradient"):
+            call(asks)
+        with torch.no_grad():
+            call(asks)
+        call(lambda a: asks(a).detach())
+        with torch.autograd.forward_ad.dual_level():
+            dual = lambda a: torch.autograd.forward_ad.make_dual(a, torch.ones_like(a))  # noqa: E731
+            with pytest.raises(ValueError, match="forward mode"):
+                call(dual)
+            with torch.no_grad(), pytest.raises(ValueError, match="forward mode"):
+                call(dual)
+            call(lambda a: dual(a).detach())
+            call(lambda a: a)
+    with torch.no_grad():
+        got = ops.sample(asks(l), u, temperature=asks(t), top_p=0.9)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and not got[1].requires_grad
+    # numbers and limits that only choose words carry nothing to lose
+    got = ops.sample(l, asks(u), temperature=t, top_p=asks(torch.full((4,), 0.9, device="cuda")))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with torch.inference_mode():
+        ops.sample(l, u)
