@@ -15,13 +15,17 @@ namespace {
 // ---- root-mean-square norm ---------------------------------------------------------------------------------------------------
 
 // Rows of up to 1,024 columns belong to a wavefront, up to 4,096 to a workgroup of 256, up to 8,192 to one of 512; wider ones are read again.  Rows of up
-// to 2,048 belong to a wavefront as well (32 elements a lane), which needs no barrier, where the result is in 8 bits and where there are enough rows to
-// keep the CUs busy with fewer of them.  us with a wavefront and a workgroup: 65,536 x 2048 in bf16, stream in binary32, forward 295 and 309, backward
-// 407 and 432, in 8 bits 270 and 288; rows in 8 bits of 65,536 x 2048 85 and 140, of 5000 10.3 and 13.4; but 9000 x 1100 forward 21.1 and 19.3,
-// backward 44.5 and 30.8, and 32,768 x 1500 in binary32 forward 161 and 167, backward 156 and 153.  16,384 x 1024 in bf16 forward 21.5 and 23.7, in 8 bits
-// 21.5 and 42.5.
+// to 2,048 belong to a wavefront as well (32 elements a lane), which needs no barrier, where the result is in 8 bits (rows in 8 bits of 65,536 x 2048 85 us
+// with a wavefront, 140 with a workgroup, of 5000 10.3 and 13.4) and, where there are enough rows to keep the CUs busy with fewer of them:
+//   forward from 24,000 rows on.  Times with a wavefront, relative to those with a workgroup, over ten widths and three pairs of types: 8192 rows 1.03 to
+//     1.33, 16,384 0.93 to 1.17 (mean 1.02), 24,000 0.93 to 1.05 (0.99), 32,768 0.86 to 1.03, 65,536 0.81 to 1.00 (2048 columns in bf16, stream in binary32: 312
+//     and 296 us);
+//   backward from 40,000 rows of 1,600 columns on where the stream is in binary32.  The same, 1664 columns: 32,768 rows 1.01 to 1.02, 49,152 0.99, 65,536 0.97
+//     to 0.98; 65,536 rows of 1030 1.10 to 1.28, of 1500 1.00 to 1.03, of 2048 0.94 to 0.95 (bf16 430 and 409 us).  With all in bf16 65,536 rows of 1500 take 1.29, of
+//     1984 1.05, of 2047 1.06 and only those of 2048, where every lane has all its chunks, 0.94.
+// 16,384 x 1024 in bf16 forward 21.5 us with a wavefront and 23.7, in 8 bits 21.5 and 42.5.
 constexpr int64_t kRmsCols = 8192;
-constexpr int64_t kManyRows = 16384, kManyValues = (int64_t)1 << 27;   // from which on a wavefront's rows have up to 2,048 columns, forward and backward
+constexpr int64_t kForwardRows = 24000, kBackwardRows = 40000, kBackwardCols = 1600;
 
 template <class F>
 int with_rms_shape(int64_t cols, bool wavefront, F &&f) {
@@ -39,11 +43,10 @@ unsigned rms_grid(int64_t rows, int tpr) {
     return (unsigned)(groups < 8 * kCus ? groups : 8 * kCus);
 }
 unsigned wide_grid(int64_t rows) { return (unsigned)(rows < 64 * kCus ? rows : 64 * kCus); }
-bool rms_backward_wavefront(int64_t rows, int64_t cols) { return cols <= 1024 || (cols <= 2048 && rows * cols >= kManyValues); }
+bool rms_backward_wavefront(int64_t rows, int64_t cols, int rtype) { return cols <= 1024 || (cols <= 2048 && cols >= kBackwardCols && rows >= kBackwardRows && rtype == SABER_F32); }
 // workgroups of the backward pass, as many as the CUs hold at a time: each leaves a partial row
-int64_t rms_parts(int64_t rows, int64_t cols) {
+int64_t rms_parts(int64_t rows, int64_t cols, bool wavefront) {
     if (cols > kRmsCols) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
-    const bool wavefront = rms_backward_wavefront(rows, cols);
     const int64_t groups = parts_of(rows > 0 ? rows : 1, wavefront ? 4 : 1);
     const int64_t most = (cols <= 1024 ? 3 : wavefront || cols > 4096 ? 2 : 4) * kCus;
     return groups < most ? groups : most;
@@ -110,7 +113,7 @@ extern "C" int saber_rms_norm_forward(const void *x, int64_t x_stride, const voi
             if (q) rms_forward_wide_kernel<T, R, true><<<wide_grid(rows), 1024, 0, st>>>(a);
             else rms_forward_wide_kernel<T, R, false><<<wide_grid(rows), 1024, 0, st>>>(a);
         } else
-            OPS_TRY(with_rms_shape(cols, q || rows >= kManyRows, [&](auto tpr, auto nc) -> int {
+            OPS_TRY(with_rms_shape(cols, q || rows >= kForwardRows, [&](auto tpr, auto nc) -> int {
                 if (q) rms_forward_kernel<T, R, tpr.value, nc.value, true><<<rms_grid(rows, tpr.value), kRmsThreads<tpr.value>, 0, st>>>(a);
                 else rms_forward_kernel<T, R, tpr.value, nc.value, false><<<rms_grid(rows, tpr.value), kRmsThreads<tpr.value>, 0, st>>>(a);
                 return SABER_OK;
@@ -123,7 +126,7 @@ extern "C" int saber_rms_norm_forward(const void *x, int64_t x_stride, const voi
 extern "C" int saber_rms_norm_backward_workspace(int64_t rows, int64_t cols, int64_t *bytes) {
     OPS_TRY(check_rows("saber_rms_norm_backward_workspace", rows, cols, SABER_F32));
     if (!bytes) return fail(SABER_EINVAL, "saber_rms_norm_backward_workspace: bytes is null");
-    *bytes = rms_parts(rows, cols) * cols * 4;
+    *bytes = rms_parts(rows, cols, cols <= 1024) * cols * 4;   // (wider rows that belong to a wavefront have fewer parts)
     return SABER_OK;
 }
 
@@ -146,7 +149,8 @@ extern "C" int saber_rms_norm_backward(const void *dy, int64_t dy_stride, const 
         if (dsum) OPS_TRY(check_pointer(who, "dsum", dsum, size_of(rtype)));
         OPS_TRY(check_pointer(who, "rstd", rstd, 4));
     }
-    const int64_t parts = rows > 0 ? rms_parts(rows, cols) : 0;
+    const bool wavefront = rms_backward_wavefront(rows, cols, rtype);
+    const int64_t parts = rows > 0 ? rms_parts(rows, cols, wavefront) : 0;
     if (dweight && parts) {
         OPS_TRY(check_pointer(who, "workspace", workspace, 16));
         if (workspace_bytes < parts * cols * 4) return fail(SABER_EINVAL, "%s: work space of %lld bytes, %lld are needed", who, (long long)workspace_bytes, (long long)(parts * cols * 4));
@@ -166,7 +170,7 @@ extern "C" int saber_rms_norm_backward(const void *dy, int64_t dy_stride, const 
                 }
                 if (dweight) rms_columns_wide_kernel<T, R><<<dim3((unsigned)parts_of(cols, 2048), (unsigned)parts), 256, 0, st>>>(a);
             } else
-                OPS_TRY(with_rms_shape(cols, rms_backward_wavefront(rows, cols), [&](auto tpr, auto nc) -> int {
+                OPS_TRY(with_rms_shape(cols, wavefront, [&](auto tpr, auto nc) -> int {
                     rms_backward_kernel<T, R, tpr.value, nc.value><<<(unsigned)parts, kRmsThreads<tpr.value>, 0, st>>>(a);
                     return SABER_OK;
                 }));

@@ -1,6 +1,6 @@
 """The operators of a head that answers in the corners of what they accept: temperatures and logits at the ends of binary32, shares that
-fall on a border of whole masses, one tensor as both inputs of a norm, gradients that a call does
-not have."""
+fall on a border of whole masses, norms of one tensor as both inputs and of many rows, gradients that
+a call does not have."""
 import math
 
 import pytest
@@ -104,7 +104,7 @@ def test_sample_no_share_of_very_many_words(equal):
         assert int(word) == at[int(0.999 * left)] and abs(float(p) * left - 1) <= 2 * E, share
 
 
-# ---- one tensor as both inputs of a norm ----------------------------------------------------------------------------------------
+# ---- norms: one tensor as both inputs, many rows ----------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rows,cols", [(10, 64), (33, 1000), (5, 2500), (3, 9000)])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
@@ -128,6 +128,39 @@ def test_rms_norm_gradient_of_one_tensor_as_both(rows, cols, dtype):
     bound = 2 * (HALF[dtype] * ds.abs() + TINY[dtype] + err * (1 + HALF[dtype]))
     assert bool((bound < 0.1 * ds.abs().mean()).all())
     within(leaf.grad, 2 * ds, bound, "gradient of both")
+
+
+@pytest.mark.parametrize("rows,cols,dtype,rtype", [(39999, 1600, F16, F32), (40000, 1600, F16, F32), (40003, 1599, F16, F32), (40001, 2045, BF16, BF16), (40002, 1777, F32, F32)])
+def test_rms_norm_around_the_choice_of_a_variant(rows, cols, dtype, rtype):
+    """Both sides of the sizes from which on a row belongs to a wavefront: every row as the same row by itself, the weight's gradient in 64 bits."""
+    print("rms", rows, cols, dtype, rtype, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rand = lambda t, *s: torch.randn(*s, device="cuda", generator=g).to(t)  # noqa: E731
+    x, res, dy, dsum, w = rand(dtype, rows, cols), rand(rtype, rows, cols), rand(dtype, rows, cols), rand(rtype, rows, cols), 1 + 0.2 * rand(F32, cols)
+    y, saved = pk.ops.rms_norm_forward(x, w, res)
+    dx, dres, dw = pk.ops.rms_norm_backward(dy, saved, dsum)
+    adds = 40.0 + cols / 1024
+    for part in (slice(0, 9), slice(rows // 2, rows // 2 + 9), slice(rows - 9, rows)):
+        z, one = pk.ops.rms_norm_forward(x[part], w, res[part])
+        ex, eres, _ = pk.ops.rms_norm_backward(dy[part], one, dsum[part])
+        assert torch.equal(saved.x[part], one.x)
+        # sums of a row in another order: r is off by half of that, y by it and a step of its type, the gradient's mean by that of the terms
+        rel = (adds + 8) * E
+        step = 2 * HALF[dtype]
+        within(y[part], z, (step + rel) * z.double().abs() + TINY[dtype], "y")
+        s, r = one.x.double(), one.rstd.double()[:, None]
+        h, gw = s * r, dy[part].double() * w.double()
+        size = r * (gw.abs() + h.abs() * (gw * h).abs().mean(1, keepdim=True)) * 3 * rel + 4 * E * eres.double().abs()
+        within(dx[part], ex, step * ex.double().abs() + TINY[dtype] + size, "dx")
+        within(dres[part], eres, 2 * HALF[rtype] * eres.double().abs() + TINY[rtype] + size, "dresidual")
+    dw64, size = (torch.zeros(cols, device="cuda", dtype=torch.float64) for _ in range(2))
+    for lo in range(0, rows, 8192):
+        part = slice(lo, min(rows, lo + 8192))
+        t = dy[part].double() * saved.x[part].double() * saved.rstd[part].double()[:, None]
+        dw64 += t.sum(0)
+        size += t.abs().sum(0)
+    # a lane adds up the rows of its wavefront or workgroup, 512 or 1,024 of these; the rest is joined in some 100 additions
+    within(dw, dw64, HALF[F32] * dw64.abs() + (rows / 512 + 140) * E * size, "dweight")
 
 
 # ---- gradients that a call does not have -----------------------------------------------------------------------------------------
