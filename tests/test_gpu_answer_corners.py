@@ -66,9 +66,39 @@ def test_sample_share_of_whole_masses(words, deep):
         l[i, list(at)] = 0.0
     for temperature in (1.0, 0.25, 8.0):
         for u, share, which, p in ((0.75, 0.5, 0, 1.0), (0.75, 0.501, 1, 0.5), (0.25, 0.501, 0, 0.5), (0.999, 0.0, 0, 1.0)):
-            word, got = pk.ops.sample(dev(l * temperature), torch.full((len(places),), u, device="cuda"), temperature=temperature, top_p=share)
+            word, got = pk.ops.sample(dev(l * temperature), torch.full((len(places),), u, device="cuda"), temperature=temperature, top_p=share, min_p=0.4 * (share == 0.5))
             assert word.tolist() == [at[which] for at in places], (temperature, u, share)
             assert bool((got - p).abs().max() <= 2 * E)
+
+
+@pytest.mark.parametrize("deep,units", [(-31.95, 0.0), (-31.7, 1.0)])
+@pytest.mark.parametrize("min_p", [0.0, 0.2])
+def test_sample_share_between_two_bins(deep, units, min_p):
+    """Two words of different logits, the share such that the first one's mass is just enough, or just not, by what the masses of 100,000 deep words
+    are rounded by, to none or to one unit of 2^-45: which words are left is decided by whole masses, wherever the two are."""
+    words, unit, found = 100000, 2.0 ** -45, 0
+    z = float(torch.tensor(deep, dtype=F32))
+    tail, whole = (words - 2) * math.exp(z), (words - 2) * units * unit
+    places = [(3, 900), (900, 3), (words - 9, words - 5), (7, words - 1)]
+    for i in range(4000):
+        share = float(torch.tensor(0.52 + i * 1e-5, dtype=F32))
+        low = float(torch.tensor(math.log(1 / share - 1), dtype=F32))
+        two = 1 + math.exp(low)
+        exact, rough = (share - 2.0 ** -40) * (two + whole), (share - 2.0 ** -40) * (two + tail)
+        if not min(exact, rough) < 1 - 2e-11 or not max(exact, rough) > 1 + 2e-11:
+            continue
+        found += 1
+        l = torch.full((len(places), words), deep)
+        for k, (a, b) in enumerate(places):
+            l[k, a], l[k, b] = 0.0, low
+        u = torch.where(torch.tensor([a < b for a, b in places]), 0.99, 0.1)
+        word, p = pk.ops.sample(dev(l), dev(u), top_p=share, min_p=min_p)
+        left = 2 if exact > 1 else 1
+        assert word.tolist() == [at[left - 1] for at in places], (share, low, exact - 1, rough - 1)
+        assert bool((p.cpu().double() - (1.0 if left == 1 else math.exp(low) / two)).abs().max() <= 2 * E)
+        if found == 6:
+            break
+    assert found == 6
 
 
 @pytest.mark.parametrize("words", [64, 1024, 8192, 65536])
