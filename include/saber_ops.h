@@ -159,8 +159,9 @@ int saber_rows8_restore(const int8_t *q, int64_t q_stride, const float *scale, i
                         void *x, void *stream);
 
 /*
- * Logits from rows in 8 bits: out_nv = (sum over k of x_nk weight_vk) x_scale_n w_scale_v.  The sums are int32 and exact, the
- * scales are multiplied in binary32 in this order, the result is rounded once.
+ * Logits from rows in 8 bits: out_nv = (sum over k of x_nk weight_vk) x_scale_n w_scale_v.  The sums are int32 and exact; then
+ * a sum is rounded to binary32, multiplied by either scale in this order, each product rounded to binary32, and the result
+ * to dtype.
  *   x [rows][cols], weight [words][cols] as above; values -128 .. 127; out [rows][words] of dtype
  * Errors: EINVAL, ERANGE, EDEVICE.
  */
@@ -174,13 +175,15 @@ int saber_linear8(const int8_t *x, int64_t x_stride, const float *x_scale, const
  *   those of exp z >= min_p; always the first one
  * and the first word, by number, is taken at which the sum of exp z of the words left exceeds u times that of all of them.
  * The masses are sums of whole multiples of 2^-45 (of 2^(ceil(log2 words) - 62) beyond 2^17 words) of the likeliest
- * word's: what is below half of that has none.  The limits are compared in 64 bits; a share of the whole counts as held from
- * 2^-40 of the whole below it.
+ * word's: what is below half of that has none, also where there are so many such words that together they would have
+ * some.  The limits are compared in 64 bits; a share of the whole counts as held from 2^-40 of the whole below it.
+ * u is a binary32, so of 24 bits where torch's rand or the like makes it: a word of less than 2^-24 of the mass left is
+ * drawn only if a multiple of 2^-24 falls on it.
  *   logits [rows][words] of dtype; -inf leaves a word out, infinite ones share all of the mass
  *   temperatures, top_ks (int32, or int64 if top_k64), top_ps, min_ps [rows]: a value per row, or NULL: then temperature,
- *                 top_k, top_p, min_p hold for all rows (and are checked).  A temperature of 0 (or less, or NaN) takes the
- *                 first word of the largest logit, whatever the limits.  As values per row a top_p or min_p below 0
- *                 counts as 0, beyond 1 as 1, and NaN as no limit.
+ *                 top_k, top_p, min_p hold for all rows (and are checked: one below 0 is refused).  A temperature of 0 (as
+ *                 a value per row also less, or NaN) takes the first word of the largest logit, whatever the limits.
+ *                 As values per row a top_p or min_p below 0 counts as 0, beyond 1 as 1, and NaN as no limit.
  *   u [rows]: within [0, 1); what is outside counts as the next number within, NaN as 0
  *   word [rows], p [rows]: the word and its share of the mass left.  A row of which nothing is left (all -inf): -1 and 0.
  *                 One with a NaN: -1 and NaN.

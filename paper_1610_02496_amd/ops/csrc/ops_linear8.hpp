@@ -2,8 +2,9 @@
 // in binary32, rounded once to the type of the output.
 //
 // What bounds it: for few rows the weights' bytes (1 row of 1024 and 100,000 words 19 us, 5.3 TB/s); for many rows the matrix cores and, where the
-// columns are as few as here, what a tile does before and after its steps: 8192 rows of 1000 and 141,000 words 1.60 ms, 1.45 POPS, of which
-// the steps are 0.75, the stores' bytes (2.3 GB) 0.45; with 4096 columns 2.6 POPS.
+// columns are as few as here, what a tile does before and after its steps.  8192 rows and 141,000 words in bf16, 60 calls in a row: 128 columns 0.98 ms, 512 1.21, 1000
+// 1.54 (1.50 POPS), 2048 2.61 (1.82), 4096 4.05 (2.34), 8192 7.27 (2.60): a step of 128 columns is 0.08 to 0.1 ms, all that is not steps 0.9, of which the stores' bytes
+// (2.3 GB) alone are 0.34.  The first calls after a rest take 1.76, as do calls whose inputs change (the clock, by the load of the matrix cores).
 #pragma once
 #include "ops_product.hpp"
 

@@ -17,8 +17,10 @@
 // one of 1,900 of 141,000 (2048 such rows take 3 % longer for it).  A share counts as held from 2^-40 of the whole below it.
 //
 // What bounds it: for many rows the arithmetic in 64 bits, 20 instructions a logit for the histogram and 25 for a word that is left, beside two reads of the
-// row, the second mostly from caches (2048 rows of 141,000 in binary32 with top_p 0.95 450 us, of which two reads alone 330; of top_k 50 335); for few rows
-// a dozen phases of a workgroup that follow from each other, 0.5 to 3 us each (one row of 100,000 with all limits 29 us, two reads 11).
+// row, the second mostly from caches (2048 rows of 141,000 in binary32 with top_p 0.95 440 to 480 us, of which two reads alone 330; of top_k 50 333; four reads, of
+// top_k 5000 and top_p, 730); for few rows one CU's arithmetic and a dozen phases of a workgroup that follow from each other, 0.5 to 3 us each (one row of 100,000
+// with all limits 30 us, with top_p alone 48, with top_k 5000 and top_p 81, two reads 11); for rows of equal logits additions to one word of LDS (1024 rows of
+// 100,000 in bf16 with top_k 50 935 us, 79 for natural ones; one row of binary32 239 and 22).
 #pragma once
 #include "ops_common.hpp"
 
@@ -405,7 +407,7 @@ struct Row {
 
     // Masses of the tiles (if `sums`) of the bins before `bin`, of logits that min_p leaves; and a list of that bin's logits, unless all are
     // listed.  Of a tile's logits few are left, as a rule: a wavefront puts them side by side first, so that it computes 64 masses that count at
-    // a time (2048 rows of 141,000 words in binary32, min_p 0.05: 335 us; without a limit, with the masses of all, 407).
+    // a time (2048 rows of 141,000 words in binary32, min_p 0.05: 335 us; without a limit, with the masses of all, 386).
     __device__ __forceinline__ void sum_and_list(bool sums, int bin) {
         __syncthreads();
         for (int i = tid; i < TILES; i += THREADS) {
@@ -549,8 +551,9 @@ struct Row {
 // A row per workgroup.  It is read once for its largest logit and, if top_k is not small or top_p is given, the first limit's histogram; then, if
 // top_k is small, once to list the few logits that can be left, among them the top_k largest of the threads' own maxima; else once for the masses of
 // its tiles of 512 words and a list of the bin with the border (top_k not small and top_p: both a second time, for top_p).  The word is found
-// in its tile.  (No loop over rows: what the compiler moved out of one did not fit the registers, 690 us instead of 515 for 2048 rows of 141,000 words in
-// binary32 with top_p, 67 instead of 20 for 4096 largest of 5000 in bf16.)
+// in its tile.  A top_k is small up to twice the workgroup's threads: of 2048 rows of 141,000 in binary32 1000 words with top_p 0.9 take 361 us, 1100 669.
+// (No loop over rows: what the compiler moved out of one did not fit the registers and took a third longer for 2048 rows of 141,000 with top_p.  As it is
+// some 45 scalar registers wait in lanes of vector registers, and two vector registers of the variant of 256 threads in memory.)
 template <class T, int THREADS, int TILES>
 __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sample a) {
     __shared__ SampleLds<THREADS, TILES, kList<THREADS>> s;

@@ -231,7 +231,7 @@ namespace {
 constexpr int64_t kMaxCols8 = ((int64_t)1 << 17) - 1;   // products of a sum in int32: each up to 2^14
 
 // The tile of a product of `steps` steps of 128 columns: the rule of the 16-bit products, whose steps and ends take about as long.  Measured in
-// us with 256, 128 and 64 in turn (bf16): 8192 x 1000 x 141,000: 1597, 1694, 2579; 4096 x 1000 x 100,000: 570, 590, 938; 4096 x 777 x 30,011: 179, 165,
+// us with 256, 128 and 64 in turn (bf16), runs of many calls: 8192 x 1000 x 141,000: 1597, 1694, 2579; 4096 x 1000 x 100,000: 570, 590, 938; 4096 x 777 x 30,011: 179, 165,
 // 221; 300 x 777 x 30,011: 26.2, 20.9, 24.4; 61 x 777 x 30,011: 21.2, 9.6, 9.4; 1 x 1024 x 100,000: 41.7, 25.2, 20.9.
 int tile8_of(int64_t m, int64_t n, int64_t steps) {
     auto tiles = [&](int64_t t) { return parts_of(m, t) * parts_of(n, t); };
@@ -285,8 +285,9 @@ namespace {
 constexpr int kFewTiles = 16, kManyTiles = 512;   // of 512 words or more
 constexpr int64_t kMostRows = (int64_t)1 << 21;    // of a launch (of fewer than 2^32 threads)
 // Threads of a workgroup: 256 for many short rows, of which a CU then holds four; 1,024 where there is a CU for every row and the row is long; else
-// 512.  Measured in us with top_p 0.95: 250 rows of 1000 20.0 (256), 19.6 (512); of 8000 in binary32 25.4, 22.3; of 10,000 22.7 (512), 22.5 (1024); 61
-// of 30,011 30.5, 28.5; 250 of 100,000 62.6, 53.5; 300 of 100,000 118, 148; 2048 of 141,000 in binary32 690, 867 (before the loop over rows was gone).
+// 512.  Measured in us with top_p 0.95, with 256, 512 and 1,024 in turn (256 where a row has no more tiles): bf16, 250 rows of 1000 20.2, 19.8, 21.7; 257 22.1,
+// 23.2, 37.1; 1024 rows of 5000 33.7, 47.9, 77.8; with 512 and 1,024: 250 of 10,000 22.5, 22.8; of 20,000 26.8, 26.0; of 100,000 62.3, 52.3; 300 of 100,000 83.9,
+// 97.5; 1024 156, 195; one row of 10,000 in binary32 21.2, 21.8; of 20,000 25.0, 24.1; of 100,000 56.8, 48.2; 2048 rows of 141,000 464, 574.
 constexpr int64_t kFewWords = 20000;
 }
 
